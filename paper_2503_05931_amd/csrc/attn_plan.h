@@ -1,0 +1,114 @@
+// Work lists of ragged attention and the buckets of its bias.  Host code without any GPU call.
+#pragma once
+
+#include <stdint.h>
+
+#include <algorithm>
+#include <cmath>
+#include <vector>
+
+namespace aed {
+
+// Lists are made for the whole chip: two workgroups on each of 256 compute units.
+constexpr int kPlanSlots = 512;
+
+// First distances of a side's logarithmic buckets, half + 1 on: the smallest n with (n / half)^(side - half) >= (max / half)^i.
+// The power is irrational but where it is a whole number, which rounding must not miss.
+inline std::vector<int> bucket_steps(int side, int max_distance) {
+    const int half = side / 2, log_buckets = side - half;
+    std::vector<int> steps;
+    for (int i = 1; i < log_buckets; ++i) {
+        const double x = half * std::pow((double)max_distance / half, (double)i / log_buckets), whole = std::nearbyint(x);
+        steps.push_back((int)(std::fabs(x - whole) < 1e-11 * whole ? whole : std::ceil(x)));
+    }
+    return steps;
+}
+// Bucket by place = key - query + max_distance; max_distance + 1 places, with bidirectional buckets 2 max_distance + 1
+inline std::vector<uint8_t> bucket_places(int buckets, int max_distance, bool bidirectional) {
+    const int side = bidirectional ? buckets / 2 : buckets, half = side / 2;
+    const std::vector<int> steps = bucket_steps(side, max_distance);
+    std::vector<uint8_t> of;
+    for (int at = 0; at <= (bidirectional ? 2 : 1) * max_distance; ++at) {
+        const int n = std::abs(at - max_distance);
+        int b = n;
+        if (n >= half) b = half + (int)(std::upper_bound(steps.begin(), steps.end(), n) - steps.begin());
+        of.push_back((uint8_t)(b + (at > max_distance ? side : 0)));
+    }
+    return of;
+}
+
+struct PlanItem {  // RaggedItem's fields
+    int64_t k_row;
+    int32_t q_row, rows, pos, k_begin, k_end, part;
+};
+struct PlanJoin {
+    int32_t q_row, rows, part, n_parts;
+};
+
+struct AttnPlan {
+    bool few = false;
+    int tile_rows = 0, n_parts = 0;
+    std::vector<PlanItem> forward, dq, dkv;
+    std::vector<PlanJoin> joins;
+    int64_t q_rows = 0;
+};
+
+// tile_many, tile_few: query rows of an item (and keys of one of key gradients)
+inline AttnPlan plan_attention(const int32_t* q_lens, const int32_t* k_lens, const int64_t* k_starts, int batch, int heads, bool causal, bool training,
+                               int tile_many, int tile_few) {
+    AttnPlan p;
+    int most = 0;
+    for (int b = 0; b < batch; ++b) most = std::max(most, (int)q_lens[b]);
+    p.few = most <= tile_few;
+    p.tile_rows = p.few ? tile_few : tile_many;
+    const int step = p.few ? 128 : 64;  // keys that a workgroup takes at once
+    std::vector<PlanItem> whole;
+    int64_t q_row = 0, packed = 0, steps = 0;
+    auto tiles = [&](int tile, std::vector<PlanItem>& to, int b, int64_t k_row) {
+        const int nq = q_lens[b], nk = k_lens[b];
+        for (int q0 = 0; q0 < nq; q0 += tile) {
+            const int rows = std::min(tile, nq - q0), pos = nk - nq + q0;
+            to.push_back(PlanItem{k_row, (int32_t)(q_row + q0), rows, pos, 0, causal ? std::max(0, std::min(nk, pos + rows)) : nk, -1});
+        }
+    };
+    for (int b = 0; b < batch; ++b) {
+        const int nq = q_lens[b], nk = k_lens[b];
+        const int64_t k_row = k_starts ? k_starts[b] : packed;
+        tiles(p.tile_rows, whole, b, k_row);
+        if (training) {
+            tiles(tile_many, p.dq, b, k_row);
+            for (int k0 = 0; k0 < nk; k0 += tile_many) {
+                const int pos = k0 - (nk - nq);
+                p.dkv.push_back(PlanItem{k_row + k0, (int32_t)q_row, std::min(tile_many, nk - k0), pos, causal ? std::max(0, std::min(nq, pos)) : 0, nq, -1});
+            }
+        }
+        q_row += nq;
+        packed += nk;
+    }
+    p.q_rows = q_row;
+    for (const PlanItem& it : whole) steps += (it.k_end + step - 1) / step;
+    // Keys are split where an item would take much longer than its share of the chip, into parts of 256 keys and more.
+    const int64_t share = std::max<int64_t>(256 / step, (steps * heads + kPlanSlots - 1) / kPlanSlots);
+    for (const PlanItem& it : whole) {
+        const int n = (it.k_end + step - 1) / step;
+        if (n < 2 * share) {
+            p.forward.push_back(it);
+            continue;
+        }
+        const int parts = (int)((n + share - 1) / share);
+        p.joins.push_back(PlanJoin{it.q_row, it.rows, p.n_parts, parts});
+        for (int i = 0; i < parts; ++i) {
+            PlanItem part = it;
+            part.k_begin = (int)((int64_t)n * i / parts) * step;
+            part.k_end = std::min(it.k_end, (int)((int64_t)n * (i + 1) / parts) * step);
+            part.part = p.n_parts++;
+            p.forward.push_back(part);
+        }
+    }
+    // the longest first: they end together
+    auto longer = [](const PlanItem& a, const PlanItem& b) { return a.k_end - a.k_begin > b.k_end - b.k_begin; };
+    for (auto* list : {&p.forward, &p.dq, &p.dkv}) std::stable_sort(list->begin(), list->end(), longer);
+    return p;
+}
+
+}  // namespace aed
