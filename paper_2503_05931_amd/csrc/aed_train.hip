@@ -132,8 +132,12 @@ void lay_out(aed_attn& p, const int32_t* q_lens, const int32_t* k_lens, const in
     p.span = (int)of.size();
     for (int i = p.span - 1; i >= 0; --i) {  // a bucket's places lie side by side
         int2& r = range[of[i]];
-        if (r.y == 0) r.y = i + 1;
-        r.x = i;
+        if (r.y == 0) r.y = i + 1 + aed::kAttnMargin;
+        r.x = i + aed::kAttnMargin;
+    }
+    if (p.span > 0) {  // what is beyond an end is the end's
+        range[of.front()].x = 0;
+        range[of.back()].y = p.span + 2 * aed::kAttnMargin;
     }
     p.bucket_of = p.arena.table(of);
     p.bucket_range = p.arena.table(range);
@@ -158,6 +162,7 @@ aed_status to_tensor(const aed_rows* t, const char* name, int64_t rows, int head
         if (strides[i] * es % 16 != 0) return fail(AED_EINVAL, "%s: a stride of %lld elements is no multiple of 16 bytes", name, (long long)strides[i]);
         if (output && (i == 0 ? rows : heads) > 1 && strides[i] < head_dim) return fail(AED_EINVAL, "%s: rows or heads of an output overlap", name);
     }
+    if (strides[0] > aed::kAttnMaxPitch / es) return fail(AED_EUNSUPPORTED, "%s: more than %d bytes between rows", name, aed::kAttnMaxPitch);
     to = aed::AttnTensor{static_cast<char*>(t->data), strides[0] * es, strides[1] * es};
     return AED_OK;
 }

@@ -87,8 +87,8 @@ inline AttnPlan plan_attention(const int32_t* q_lens, const int32_t* k_lens, con
     }
     p.q_rows = q_row;
     for (const PlanItem& it : whole) steps += (it.k_end + step - 1) / step;
-    // Keys are split where an item would take much longer than its share of the chip, into parts of 256 keys and more.
-    const int64_t share = std::max<int64_t>(256 / step, (steps * heads + kPlanSlots - 1) / kPlanSlots);
+    // Keys are split where an item would take much longer than its share of the chip, into parts of 512 keys and more.
+    const int64_t share = std::max<int64_t>(512 / step, (steps * heads + kPlanSlots - 1) / kPlanSlots);
     for (const PlanItem& it : whole) {
         const int n = (it.k_end + step - 1) / step;
         if (n < 2 * share) {

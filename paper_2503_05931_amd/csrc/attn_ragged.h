@@ -30,7 +30,7 @@ struct RaggedArgs {
     const uint8_t* key_mask;  // by key row; nullptr: all keys are seen
     const void* bias;        // [buckets, heads], in the tensors' type
     const uint8_t* bucket_of;  // [span], by key - query + max_distance
-    const int2* bucket_range;  // [buckets]: first of a bucket's places in there, and one past its last
+    const int2* bucket_range;  // [buckets]: first of a bucket's places with the margins on both sides, and one past its last
     float* delta;            // [rows, heads]: sum over a row of gradient times output
     float* part_o;           // [part, heads, tile rows, D]
     float2* part_ml;         // [part, heads, tile rows]: maximum (of scores times log2 e) and sum
@@ -43,6 +43,8 @@ struct RaggedArgs {
 };
 
 constexpr int kAttnRows = 128;  // query rows of an item of many (attn_forward_kernel), keys of an item of key gradients
+constexpr int kAttnMargin = 64;  // places of the bias in LDS beyond both ends of its range
+constexpr int kAttnMaxPitch = 0x40000000 / 64 - 64;  // bytes between rows: 64 of them stay below 2^30, and twice that in 32 bits
 constexpr int kAttnFew = 32;    // and of few (attn_few_kernel)
 
 // few: items of kAttnFew rows.  Each returns hipSuccess or what the launch reported.

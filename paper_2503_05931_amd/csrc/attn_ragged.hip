@@ -12,11 +12,11 @@
 #include "attn_tile.h"
 #include "device_once.h"
 
+#include <type_traits>
+
 namespace aed {
 
 namespace {
-
-constexpr int kKeys = 64;  // keys of a step of the tiled kernels
 
 __device__ __forceinline__ float max_halves(float v) {
     const u32x2 a = swap32(v);
@@ -42,44 +42,44 @@ __device__ __forceinline__ uint64_t seen_from(uint64_t seen, int first, int pos,
     return last >= 63 ? seen : last < 0 ? 0 : seen & ((2ull << last) - 1);
 }
 
-// ---- bias: in LDS by key - query + max_distance, both ends standing for all beyond ----
+// ---- bias: in LDS by key - query + max_distance + kMargin.  Beyond both ends there are kMargin places more, so that a tile of 32 x 32 that
+// touches the range needs no limits; one that does not has a single bucket ----
+constexpr int kMargin = kAttnMargin;
+__device__ __forceinline__ int bias_places(const RaggedArgs& a) { return a.span + 2 * kMargin; }
 template <typename T> __device__ __forceinline__ void bias_to_lds(const RaggedArgs& a, float* w, int head) {
-    for (int i = threadIdx.x; i < a.span; i += blockDim.x)
-        w[i] = kLog2e * to_f32(load_global<T>(static_cast<const T*>(a.bias) + (int64_t)a.bucket_of[i] * a.heads + head));
+    for (int i = threadIdx.x; i < bias_places(a); i += blockDim.x) {
+        const int bucket = a.bucket_of[min(max(i - kMargin, 0), a.span - 1)];
+        w[i] = kLog2e * to_f32(load_global<T>(static_cast<const T*>(a.bias) + (int64_t)bucket * a.heads + head));
+    }
 }
-enum { kInside, kAllFar, kAllNear, kMixed };
-// Where the distances of a tile of 32 keys from `key` on and 32 queries from `pos` on lie.  at: place of the first of either
+// The place of the first of 32 keys from `key` on and the first of 32 queries from `pos` on
+enum { kTouches, kAllFar, kAllNear };
 __device__ __forceinline__ int bias_region(const RaggedArgs& a, int key, int pos, int& at) {
     at = key - pos + a.max_distance;
-    if (at + 31 <= 0) return kAllFar;
-    if (at - 31 >= a.span - 1) return kAllNear;
-    return at - 31 >= 0 && at + 31 <= a.span - 1 ? kInside : kMixed;
+    const int region = at + 31 <= 0 ? kAllFar : at - 31 >= a.span - 1 ? kAllNear : kTouches;
+    at += kMargin;
+    return region;
 }
 // s += bias; STEP 1: the lane is a query (its number r), elements are keys; -1: the other way about
-template <int STEP> __device__ __forceinline__ void add_bias(float* s, const RaggedArgs& a, const float* w, int key, int pos, int r, int h) {
+template <int STEP> __device__ __forceinline__ void add_bias(f32x16& s, const RaggedArgs& a, const float* w, int key, int pos, int r, int h) {
     int at;
     const int region = bias_region(a, key, pos, at);
-    if (region == kAllFar || region == kAllNear) {
-        const float b = w[region == kAllFar ? 0 : a.span - 1];
+    if (region != kTouches) {
+        const float b = w[region == kAllFar ? 0 : bias_places(a) - 1];
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] += b;
         return;
     }
     at += STEP * (4 * h - r);
-    if (region == kInside) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] += w[at + STEP * (8 * (i >> 2) + (i & 3))];
-    } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] += w[min(max(at + STEP * (8 * (i >> 2) + (i & 3)), 0), a.span - 1)];
-    }
+    for (int i = 0; i < 16; ++i) s[i] += w[at + STEP * (8 * (i >> 2) + (i & 3))];
 }
 // Adds the gradients of a tile (lane = query) to sums by distance.  mine: this lane half's own sums, so that no two lanes of an
-// instruction meet and every sum has one order; far, near: what lies at and beyond the ends, kept by lane.
-__device__ __forceinline__ void add_distances(const float* ds, const RaggedArgs& a, float* mine, float& far, float& near, int key, int pos, int r, int h) {
+// instruction meet and every sum has one order; far, near: of tiles beyond the ends, kept by lane.
+__device__ __forceinline__ void add_distances(const f32x16& ds, const RaggedArgs& a, float* mine, float& far, float& near, int key, int pos, int r, int h) {
     int at;
     const int region = bias_region(a, key, pos, at);
-    if (region == kAllFar || region == kAllNear) {
+    if (region != kTouches) {
         float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) sum += ds[i];
@@ -88,58 +88,68 @@ __device__ __forceinline__ void add_distances(const float* ds, const RaggedArgs&
         return;
     }
     at += 4 * h - r;
-    if (region == kInside) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-            __hip_atomic_fetch_add(mine + at + 8 * (i >> 2) + (i & 3), ds[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int n = at + 8 * (i >> 2) + (i & 3);
-            if (n <= 0) far += ds[i];
-            else if (n >= a.span - 1) near += ds[i];
-            else __hip_atomic_fetch_add(mine + n, ds[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-        }
-    }
+    for (int i = 0; i < 16; ++i)
+        __hip_atomic_fetch_add(mine + at + 8 * (i >> 2) + (i & 3), ds[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
 }
 
-// scores of a tile (lane = query): scaled, biased, those of keys that are not seen (bits of `seen`) out of the way
-template <bool BIAS>
-__device__ __forceinline__ void finish_scores(float* s, const f32x16& acc, const RaggedArgs& a, float scale2, const float* w, uint32_t seen, int key, int pos, int r, int h) {
+// nothing is moved across by the compiler
+__device__ __forceinline__ void phase() { __builtin_amdgcn_sched_barrier(0); }
+
+// ends a phase of eight 32 x 32 products among which the vector instructions are dealt out
+template <int FIRST, int EACH> __device__ __forceinline__ void woven() {
+    if constexpr (FIRST > 0) __builtin_amdgcn_sched_group_barrier(0x2, FIRST, 0);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = acc[i] * scale2;
-    if constexpr (BIAS) add_bias<1>(s, a, w, key, pos, r, h);
+    for (int i = 0; i < 8; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);  // a product
+        __builtin_amdgcn_sched_group_barrier(0x2, EACH, 0);  // vector instructions
+    }
+    phase();
+}
+
+// keeps what a branch computes from `v` in the branch: the compiler would rather do it always than jump
+__device__ __forceinline__ void rarely(uint32_t& v) { asm volatile("" : "+v"(v)); }
+
+// scores of a tile (lane = query) from its products: without a bias they stay unscaled (times scale2 later), with one they are whole;
+// those of keys that are not seen (bits of `seen`) out of the way
+template <bool BIAS>
+__device__ __forceinline__ void finish_scores(f32x16& s, const RaggedArgs& a, float scale2, const float* w, uint32_t seen, int key, int pos, int r, int h) {
+    if constexpr (BIAS) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] *= scale2;
+        add_bias<1>(s, a, w, key, pos, r, h);
+    }
     if (__ballot(seen != 0xffffffffu) != 0) {
-        const uint32_t mine = seen >> (4 * h);
+        uint32_t mine = seen >> (4 * h);
+        rarely(mine);
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = (mine >> (8 * (i >> 2) + (i & 3))) & 1 ? s[i] : kNone;
     }
 }
+// exp of a score less `base`, both times log2 e
+template <bool BIAS> __device__ __forceinline__ float weight_of(float s, float scale2, float base) {
+    return __builtin_amdgcn_exp2f(BIAS ? s - base : fmaf(s, scale2, -base));
+}
 
-// Softmax of a lane's row in passing: maximum so far, and the lane half's share of the sum
+// Softmax of a lane's row in passing: maximum so far (times log2 e), and the lane half's share of the sum
 struct Running {
     float m = kNone, l = 0.f;
-    template <int TILES> __device__ __forceinline__ void scale_to(float m_tile, f32x16* acc, float& base) {
-        const float m_new = fmaxf(m, m_tile);
-        base = base_of(m_new);
-        if (__ballot(m_new > m) != 0) {
-            const float alpha = __builtin_amdgcn_exp2f(m - base);
-            l *= alpha;
+    template <int TILES> __device__ __forceinline__ float scale_to(float m_tile, f32x16* acc) {
+        const float m_new = fmaxf(m, m_tile), base = base_of(m_new), alpha = __builtin_amdgcn_exp2f(m - base);
+        l *= alpha;
 #pragma unroll
-            for (int t = 0; t < TILES; ++t) acc[t] *= alpha;
-            m = m_new;
-        }
+        for (int t = 0; t < TILES; ++t) acc[t] *= alpha;
+        m = m_new;
+        return base;
     }
 };
 // one tile of scores to weights; the sum goes to l
-__device__ __forceinline__ void to_weights(float* s, float base, float& l) {
+template <bool BIAS> __device__ __forceinline__ void to_weights(f32x16& s, float scale2, float base, float& l) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        s[i] = __builtin_amdgcn_exp2f(s[i] - base);
-        l += s[i];
-    }
+    for (int i = 0; i < 16; ++i) s[i] = weight_of<BIAS>(s[i], scale2, base);
+    l += ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7])) + (((s[8] + s[9]) + (s[10] + s[11])) + ((s[12] + s[13]) + (s[14] + s[15])));
 }
-__device__ __forceinline__ float max_of(const float* s) {
+__device__ __forceinline__ float max_of(const f32x16& s) {
     float m = s[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) m = fmaxf(m, s[i]);
@@ -155,72 +165,117 @@ template <int TILES> __device__ __forceinline__ void clear(f32x16* acc) {
 
 }  // namespace
 
+namespace {
+
+// Where a wavefront's part of the walk over the keys ends: it has no rows, or they see no further
+__device__ __forceinline__ int end_of(const RaggedArgs& a, const RaggedItem& it, int count, int pos) {
+    return count == 0 ? it.k_begin : a.causal ? min(it.k_end, max(it.k_begin, pos + count)) : it.k_end;
+}
+
+// A workgroup's walk over the keys, kStep of them a step: keys and values from memory to LDS (rows of keys, then of values), two
+// steps' worth: one is worked on while the other is on its way.
+template <typename T, int D> struct Steps {
+    typedef Rows<T, D> R;
+    static constexpr int kBuf = 2 * R::kStep * R::kPitch;
+    const RaggedArgs& a;
+    const RaggedItem& it;
+    const char *kp, *vp;
+    char* lds;
+    int lane;
+    RowFeed<T, D, R::kStep, 4> feed;
+    uint64_t seen = 0, seen_next = 0;  // of the step at hand and of the one on its way
+    int buf = 1;
+    __device__ __forceinline__ Steps(const RaggedArgs& a, const RaggedItem& it, int kv_head, char* lds, int wave, int lane)
+        : a(a), it(it), kp(a.k.p + it.k_row * a.k.row + kv_head * a.k.head), vp(a.v.p + it.k_row * a.v.row + kv_head * a.v.head), lds(lds), lane(lane),
+          feed(lds, wave, lane) {}
+    // requests the step of keys k0 on, into the buffer that is not at hand
+    __device__ __forceinline__ void fetch(int k0) {
+        if (k0 >= it.k_end) return;
+        const int count = it.k_end - k0, to = (buf ^ 1) * kBuf;
+        feed.load(kp + k0 * a.k.row, (int)a.k.row, count, to);
+        feed.load(vp + k0 * a.v.row, (int)a.v.row, count, to + kBuf / 2);
+        seen_next = a.key_mask ? seen_keys(a, it.k_row, k0, it.k_end, lane) : count >= 64 ? ~0ull : (1ull << count) - 1;
+    }
+    // everyone is done with the step at hand; the one on its way is at hand
+    __device__ __forceinline__ void next() {
+        loads_done_barrier();
+        buf ^= 1;
+        seen = seen_next;
+        if (a.key_mask && (seen & R::kAll) != R::kAll) {  // what stands in the place of keys that are not seen may be infinite
+            for (int i = threadIdx.x; i < 2 * R::kStep * R::kChunks; i += 256) {
+                const int row = i / R::kChunks;
+                if (!((seen >> (row & (R::kStep - 1))) & 1)) *reinterpret_cast<typename R::chunk_t*>(lds + buf * kBuf + i * 16) = (typename R::chunk_t)(0);
+            }
+            lds_barrier();
+        }
+    }
+    __device__ __forceinline__ const char* keys() const { return lds + buf * kBuf; }
+    __device__ __forceinline__ const char* values() const { return lds + buf * kBuf + kBuf / 2; }
+};
+
+}  // namespace
+
 // ---------------------------------------------------------------- forward, many rows
-// A workgroup takes 128 query rows of a head, 32 a wavefront, and walks the keys 64 at a time: two buffers in LDS, the next step's keys and
-// values on their way in registers meanwhile.
+// A workgroup takes 128 query rows of a head, 32 a wavefront, and walks the keys.
 template <typename T, int D, bool BIAS> __global__ __launch_bounds__(256, (2 - Rows<T, D>::kWide)) void attn_forward_kernel(RaggedArgs a) {
     typedef Rows<T, D> R;
     extern __shared__ __align__(16) char lds[];
-    constexpr int kBuf = 2 * kKeys * R::kPitch;
-    float* const w = reinterpret_cast<float*>(lds + 2 * kBuf);
+    constexpr int kSub = R::kStep / 32;
+    float* const w = reinterpret_cast<float*>(lds + 2 * Steps<T, D>::kBuf);
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 31, h = lane >> 5;
     const RaggedItem it = a.items[blockIdx.x / a.heads];
     const int head = blockIdx.x % a.heads, row0 = it.q_row + 32 * wave, count = min(max(it.rows - 32 * wave, 0), 32), pos = it.pos + 32 * wave;
-    const int64_t k_head = (int64_t)(head / a.share) * a.k.head, v_head = (int64_t)(head / a.share) * a.v.head;
-    const char* const kp = a.k.p + it.k_row * a.k.row + k_head;
-    const char* const vp = a.v.p + it.k_row * a.v.row + v_head;
-    if constexpr (BIAS) bias_to_lds<T>(a, w, head);
+    Steps<T, D> step(a, it, head / a.share, lds, wave, lane);
+    step.fetch(it.k_begin);
     RowFrag<T, D> q;
     q.load(a.q.p + (int64_t)(row0 + r) * a.q.row + head * a.q.head, r < count, h);
+    if constexpr (BIAS) bias_to_lds<T>(a, w, head);
     f32x16 acc[R::kTiles];
     clear<R::kTiles>(acc);
     Running run;
     const float scale2 = a.scale * kLog2e;
-    RowStage<T, D, kKeys, 256> ks, vs;
-    uint64_t seen = 0;
-    if (it.k_begin < it.k_end) {
-        seen = seen_keys(a, it.k_row, it.k_begin, it.k_end, lane);
-        ks.load(kp + it.k_begin * a.k.row, a.k.row, seen, tid);
-        vs.load(vp + it.k_begin * a.v.row, a.v.row, seen, tid);
-        ks.store(lds, tid);
-        vs.store(lds + kBuf / 2, tid);
+    const int mine_end = end_of(a, it, count, pos);
+    int k0 = it.k_begin;
+    for (; k0 < mine_end; k0 += R::kStep) {
+        step.next();
+        step.fetch(k0 + R::kStep);
+        f32x16 s[kSub];
+        AsRows<T, D> k[kSub];
+        AsColumns<T, D> v[kSub];
+#pragma unroll
+        for (int u = 0; u < kSub; ++u) k[u].load(step.keys(), 32 * u, lane);
+        phase();
+        k[0].dot(s[0], q);
+        phase();
+        v[0].load(step.values(), 0, lane);
+        phase();
+        if constexpr (kSub > 1) k[1].dot(s[1], q);
+        const uint64_t seen = seen_from(step.seen, k0, pos + r, a.causal);
+        float top = kNone;
+#pragma unroll
+        for (int u = 0; u < kSub; ++u) {
+            finish_scores<BIAS>(s[u], a, scale2, w, (uint32_t)(seen >> (32 * u)), k0 + 32 * u, pos, r, h);
+            top = fmaxf(top, max_of(s[u]));
+        }
+        top = max_halves(top);
+        const float base = run.scale_to<R::kTiles>(BIAS ? top : top * scale2, acc);
+        to_weights<BIAS>(s[0], scale2, base, run.l);
+        phase();
+        if constexpr (kSub > 1) v[1].load(step.values(), 32, lane);
+        phase();
+        v[0].add(acc, s[0]);
+        if constexpr (kSub > 1) {
+            to_weights<BIAS>(s[1], scale2, base, run.l);
+            v[1].add(acc, s[1]);
+        }
     }
-    lds_barrier();
-    int buf = 0;
-    for (int k0 = it.k_begin; k0 < it.k_end; k0 += kKeys) {
-        const bool more = k0 + kKeys < it.k_end;
-        uint64_t seen_next = 0;
-        if (more) {
-            seen_next = seen_keys(a, it.k_row, k0 + kKeys, it.k_end, lane);
-            ks.load(kp + (k0 + kKeys) * a.k.row, a.k.row, seen_next, tid);
-            vs.load(vp + (k0 + kKeys) * a.v.row, a.v.row, seen_next, tid);
-        }
-        const char* const kb = lds + buf * kBuf;
-        const char* const vb = kb + kBuf / 2;
-        const uint64_t mine = seen_from(seen, k0, pos + r, a.causal);
-        if (__ballot(mine != 0) != 0 && count > 0) {
-            float s[2][16];
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-                finish_scores<BIAS>(s[u], dot_rows<T, D>(kb, 32 * u, q, lane), a, scale2, w, (uint32_t)(mine >> (32 * u)), k0 + 32 * u, pos, r, h);
-            float base;
-            run.scale_to<R::kTiles>(max_halves(fmaxf(max_of(s[0]), max_of(s[1]))), acc, base);
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                to_weights(s[u], base, run.l);
-                add_weighted<D>(acc, vb, 32 * u, s[u], lane, (const T*)nullptr);
-            }
-        }
-        if (more) {
-            ks.store(lds + (buf ^ 1) * kBuf, tid);
-            vs.store(lds + (buf ^ 1) * kBuf + kBuf / 2, tid);
-        }
-        lds_barrier();
-        seen = seen_next;
-        buf ^= 1;
+    for (; k0 < it.k_end; k0 += R::kStep) {  // the other wavefronts' steps
+        step.next();
+        step.fetch(k0 + R::kStep);
     }
     const float l = sum_halves(run.l);
     if (it.part < 0) {
+        lds_barrier();
         store_tile<T, D>(acc, l > 0.f ? 1.f / l : l, lds + wave * 32 * R::kPitch, a.o.p + (int64_t)row0 * a.o.row + head * a.o.head, a.o.row, count, lane);
         if (h == 0 && r < count) a.lse[(int64_t)(row0 + r) * a.heads + head] = kLn2 * (run.m + __builtin_amdgcn_logf(l));
     } else if (r < count) {
@@ -253,12 +308,13 @@ template <typename T, int D, bool BIAS> __global__ __launch_bounds__(256, (2 - R
     char* const vb = kb + kMine / 2;
     RowStage<T, D, 32, 64> ks, vs;
     uint64_t seen = 0;
-    int k0 = it.k_begin + 32 * wave;
-    if (k0 < it.k_end) {
+    auto fetch = [&](int k0) {
         seen = seen_keys(a, it.k_row, k0, it.k_end, lane);
-        ks.load(kp + k0 * a.k.row, a.k.row, seen, lane);
-        vs.load(vp + k0 * a.v.row, a.v.row, seen, lane);
-    }
+        ks.template load<true>(kp + k0 * a.k.row, (int)a.k.row, it.k_end - k0, seen, lane);
+        vs.template load<true>(vp + k0 * a.v.row, (int)a.v.row, it.k_end - k0, seen, lane);
+    };
+    int k0 = it.k_begin + 32 * wave;
+    if (k0 < it.k_end) fetch(k0);
     RowFrag<T, D> q;
     q.load(a.q.p + (int64_t)(row0 + r) * a.q.row + head * a.q.head, r < count, h);
     if constexpr (BIAS) {
@@ -274,16 +330,17 @@ template <typename T, int D, bool BIAS> __global__ __launch_bounds__(256, (2 - R
         vs.store(vb, lane);
         other_lanes_wrote();
         const uint32_t mine = (uint32_t)seen_from(seen, k0, pos + r, a.causal);
-        if (k0 + 128 < it.k_end) {
-            seen = seen_keys(a, it.k_row, k0 + 128, it.k_end, lane);
-            ks.load(kp + (k0 + 128) * a.k.row, a.k.row, seen, lane);
-            vs.load(vp + (k0 + 128) * a.v.row, a.v.row, seen, lane);
-        }
-        float s[16], base;
-        finish_scores<BIAS>(s, dot_rows<T, D>(kb, 0, q, lane), a, scale2, w, mine, k0, pos, r, h);
-        run.scale_to<R::kTiles>(max_halves(max_of(s)), acc, base);
-        to_weights(s, base, run.l);
-        add_weighted<D>(acc, vb, 0, s, lane, (const T*)nullptr);
+        if (k0 + 128 < it.k_end) fetch(k0 + 128);
+        f32x16 s;
+        AsRows<T, D> k;
+        k.load(kb, 0, lane);
+        k.dot(s, q);
+        finish_scores<BIAS>(s, a, scale2, w, mine, k0, pos, r, h);
+        const float top = max_halves(max_of(s)), base = run.template scale_to<R::kTiles>(BIAS ? top : top * scale2, acc);
+        to_weights<BIAS>(s, scale2, base, run.l);
+        AsColumns<T, D> v;
+        v.load(vb, 0, lane);
+        v.add(acc, s);
         other_lanes_wrote();
     }
     // join: maximum, then the sums scaled to it
@@ -355,25 +412,20 @@ template <typename T, int D> __global__ __launch_bounds__(256) void attn_join_ke
 template <typename T, int D, bool BIAS> __global__ __launch_bounds__(256, (2 - Rows<T, D>::kWide)) void attn_dq_kernel(RaggedArgs a) {
     typedef Rows<T, D> R;
     extern __shared__ __align__(16) char lds[];
-    constexpr int kBuf = 2 * kKeys * R::kPitch;
-    float* const w = reinterpret_cast<float*>(lds + kBuf);
+    float* const w = reinterpret_cast<float*>(lds + 2 * Steps<T, D>::kBuf);
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 31, h = lane >> 5;
-    float* const sums = w + a.span;  // [wavefront, half][span]
+    const int places = bias_places(a);
+    float* const sums = w + places;  // [wavefront, half][places]
     const int item = blockIdx.x / a.heads;
     const RaggedItem it = a.items[item];
     const int head = blockIdx.x % a.heads, row0 = it.q_row + 32 * wave, count = min(max(it.rows - 32 * wave, 0), 32), pos = it.pos + 32 * wave;
-    const int64_t k_head = (int64_t)(head / a.share) * a.k.head, v_head = (int64_t)(head / a.share) * a.v.head;
-    const char* const kp = a.k.p + it.k_row * a.k.row + k_head;
-    const char* const vp = a.v.p + it.k_row * a.v.row + v_head;
-    if constexpr (BIAS) {
-        bias_to_lds<T>(a, w, head);
-        for (int i = tid; i < 8 * a.span; i += 256) sums[i] = 0.f;
-    }
-    RowFrag<T, D> q, d_o;
+    Steps<T, D> step(a, it, head / a.share, lds, wave, lane);
+    step.fetch(it.k_begin);
     const bool live = r < count;
+    RowFrag<T, D> q, d_o;
     q.load(a.q.p + (int64_t)(row0 + r) * a.q.row + head * a.q.head, live, h);
     d_o.load(a.d_o.p + (int64_t)(row0 + r) * a.d_o.row + head * a.d_o.head, live, h);
-    float delta = 0.f, lse2 = kNone;
+    float delta = 0.f, rest = 0.f;
     {
         RowFrag<T, D> o;
         o.load(a.o.p + (int64_t)(row0 + r) * a.o.row + head * a.o.head, live, h);
@@ -382,50 +434,51 @@ template <typename T, int D, bool BIAS> __global__ __launch_bounds__(256, (2 - R
 #pragma unroll
             for (int e = 0; e < 16 / (int)sizeof(T); ++e) delta += to_f32((T)o.c[s][e]) * to_f32((T)d_o.c[s][e]);
         delta = sum_halves(delta);
-        if (live) lse2 = kLog2e * a.lse[(int64_t)(row0 + r) * a.heads + head];
     }
     // a row that sees nothing has lse -inf, and none of its keys' bits are set: its weights become 0 by way of the scores
-    const float base = base_of(lse2), scale2 = a.scale * kLog2e;
+    const float base = live ? base_of(kLog2e * a.lse[(int64_t)(row0 + r) * a.heads + head]) : 0.f;
+    if constexpr (BIAS) {
+        bias_to_lds<T>(a, w, head);
+        for (int i = tid; i < 8 * places; i += 256) sums[i] = 0.f;
+    }
     f32x16 acc[R::kTiles];
     clear<R::kTiles>(acc);
-    float far = 0.f, near = 0.f, rest = 0.f;
-    RowStage<T, D, kKeys, 256> ks, vs;
-    uint64_t seen = 0;
-    if (it.k_begin < it.k_end) {
-        seen = seen_keys(a, it.k_row, it.k_begin, it.k_end, lane);
-        ks.load(kp + it.k_begin * a.k.row, a.k.row, seen, tid);
-        vs.load(vp + it.k_begin * a.v.row, a.v.row, seen, tid);
-    }
-    for (int k0 = it.k_begin; k0 < it.k_end; k0 += kKeys) {
-        ks.store(lds, tid);
-        vs.store(lds + kBuf / 2, tid);
-        lds_barrier();
-        const uint64_t mine = live ? seen_from(seen, k0, pos + r, a.causal) : 0;
-        if (k0 + kKeys < it.k_end) {
-            seen = seen_keys(a, it.k_row, k0 + kKeys, it.k_end, lane);
-            ks.load(kp + (k0 + kKeys) * a.k.row, a.k.row, seen, tid);
-            vs.load(vp + (k0 + kKeys) * a.v.row, a.v.row, seen, tid);
-        }
-        if (__ballot(mine != 0) != 0) {
+    const float scale2 = a.scale * kLog2e;
+    float far = 0.f, near = 0.f;
+    const int mine_end = end_of(a, it, count, pos);
+    int k0 = it.k_begin;
+    for (; k0 < mine_end; k0 += R::kStep) {
+        step.next();
+        step.fetch(k0 + R::kStep);
+        // rows that are not there are all zeros: what they add is too
+        const uint64_t seen = live ? seen_from(step.seen, k0, pos + r, a.causal) : ~0ull;
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                float s[16];
-                finish_scores<BIAS>(s, dot_rows<T, D>(lds, 32 * u, q, lane), a, scale2, w, (uint32_t)(mine >> (32 * u)), k0 + 32 * u, pos, r, h);
-                const f32x16 dp = dot_rows<T, D>(lds + kBuf / 2, 32 * u, d_o, lane);
+        for (int u = 0; u < R::kStep / 32; ++u) {
+            f32x16 s, dp;
+            AsRows<T, D> k, v;
+            AsColumns<T, D> kt;
+            k.load(step.keys(), 32 * u, lane);
+            k.dot(s, q);
+            v.load(step.values(), 32 * u, lane);
+            v.dot(dp, d_o);
+            finish_scores<BIAS>(s, a, scale2, w, (uint32_t)(seen >> (32 * u)), k0 + 32 * u, pos, r, h);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    s[i] = __builtin_amdgcn_exp2f(s[i] - base) * (dp[i] - delta);
-                    rest += s[i];
-                }
-                if constexpr (BIAS) add_distances(s, a, sums + (2 * wave + h) * a.span, far, near, k0 + 32 * u, pos, r, h);
-                add_weighted<D>(acc, lds, 32 * u, s, lane, (const T*)nullptr);
+            for (int i = 0; i < 16; ++i) {
+                s[i] = weight_of<BIAS>(s[i], scale2, base) * (dp[i] - delta);
+                rest += s[i];
             }
+            if constexpr (BIAS) add_distances(s, a, sums + (2 * wave + h) * places, far, near, k0 + 32 * u, pos, r, h);
+            kt.load(step.keys(), 32 * u, lane);
+            kt.add(acc, s);
         }
-        lds_barrier();
     }
+    for (; k0 < it.k_end; k0 += R::kStep) {  // the other wavefronts' steps
+        step.next();
+        step.fetch(k0 + R::kStep);
+    }
+    lds_barrier();
     rest = sum_halves(rest);
     if (live && h == 0) a.delta[(int64_t)(row0 + r) * a.heads + head] = delta + rest;
-    lds_barrier();
     store_tile<T, D>(acc, a.scale, lds + wave * 32 * R::kPitch, a.dq.p + (int64_t)row0 * a.dq.row + head * a.dq.head, a.dq.row, count, lane);
     if constexpr (BIAS) {
         // the ends' sums by wavefront, then the eight sums of a distance, then a bucket's distances, which lie side by side
@@ -433,20 +486,21 @@ template <typename T, int D, bool BIAS> __global__ __launch_bounds__(256, (2 - R
         near = wave_sum(near);
         lds_barrier();
         if (lane == 0) {
-            sums[2 * wave * a.span] += far;
-            sums[2 * wave * a.span + a.span - 1] += near;
+            sums[2 * wave * places] += far;
+            sums[2 * wave * places + places - 1] += near;
         }
         lds_barrier();
-        for (int i = tid; i < a.span; i += 256) {
+        for (int i = tid; i < places; i += 256) {
             float v = 0.f;
-            for (int j = 0; j < 8; ++j) v += sums[j * a.span + i];
+            for (int j = 0; j < 8; ++j) v += sums[j * places + i];
             w[i] = v;
         }
         lds_barrier();
         float* const out = a.part_bias + ((int64_t)item * a.heads + head) * a.buckets;
         for (int b = tid; b < a.buckets; b += 256) {
             float v = 0.f;
-            for (int i = a.bucket_range[b].x; i < a.bucket_range[b].y; ++i) v += w[i];
+            const int2 range = a.bucket_range[b];
+            for (int i = range.x; i < range.y; ++i) v += w[i];
             out[b] = v;
         }
     }
@@ -454,19 +508,38 @@ template <typename T, int D, bool BIAS> __global__ __launch_bounds__(256, (2 - R
 
 // ---------------------------------------------------------------- key and value gradients
 // A workgroup takes 128 keys of a key head, 32 a wavefront (a lane being a key), and walks the query rows of all heads that share it.
-template <typename T, int D, bool BIAS> __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(RaggedArgs a) {
+template <typename T, int D, bool SHAPED> __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(RaggedArgs a) {
     typedef Rows<T, D> R;
-    constexpr int kRows = 64;
+    constexpr int kRows = R::kStep, kBuf = 2 * kRows * R::kPitch;
     extern __shared__ __align__(16) char lds[];
-    constexpr int kBuf = 2 * kRows * R::kPitch;
-    float* const row_lse = reinterpret_cast<float*>(lds + kBuf);  // [kRows], then [kRows] of delta
-    float* const row_delta = row_lse + kRows;
-    float* const w = row_delta + kRows;
+    float* const stats = reinterpret_cast<float*>(lds + 2 * kBuf);  // two buffers of [kRows] lse (times log2 e), [kRows] delta
+    float* const w = stats + 4 * kRows;
     const int kv_heads = a.heads / a.share;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 31, h = lane >> 5;
     const RaggedItem it = a.items[blockIdx.x / kv_heads];
     const int kv_head = blockIdx.x % kv_heads, count = min(max(it.rows - 32 * wave, 0), 32), key0 = it.pos + 32 * wave;
     const int64_t k_row0 = it.k_row + 32 * wave;
+    const RowFeed<T, D, kRows, 4> feed(lds, wave, lane);
+    int head = kv_head * a.share, buf = 1;
+    float stat = 0.f;
+    // requests the step of query rows q0 on, into the buffer that is not at hand
+    auto fetch_stats = [&](int head, int q0) {
+        const int n = it.k_end - q0;
+        if (tid < 2 * kRows) {  // a row that is not there or sees nothing: its weights are 2^-inf
+            const int row = tid & (kRows - 1);
+            stat = tid < kRows ? -kNone : 0.f;
+            if (row < n) {
+                const int64_t at = (int64_t)(it.q_row + q0 + row) * a.heads + head;
+                stat = tid < kRows ? kLog2e * a.lse[at] : a.delta[at];
+                if (stat == kNone) stat = -kNone;
+            }
+        }
+    };
+    if (it.k_begin < it.k_end) {
+        feed.load(a.q.p + (int64_t)(it.q_row + it.k_begin) * a.q.row + head * a.q.head, (int)a.q.row, it.k_end - it.k_begin, 0);
+        feed.load(a.d_o.p + (int64_t)(it.q_row + it.k_begin) * a.d_o.row + head * a.d_o.head, (int)a.d_o.row, it.k_end - it.k_begin, kBuf / 2);
+        fetch_stats(head, it.k_begin);
+    }
     bool live = r < count;
     if (a.key_mask && live) live = load_global<uint8_t>(a.key_mask + k_row0 + r) != 0;
     RowFrag<T, D> k, v;
@@ -476,68 +549,99 @@ template <typename T, int D, bool BIAS> __global__ __launch_bounds__(256, 1) voi
     clear<R::kTiles>(dk);
     clear<R::kTiles>(dv);
     const float scale2 = a.scale * kLog2e;
-    for (int head = kv_head * a.share; head < (kv_head + 1) * a.share; ++head) {
-        if constexpr (BIAS) {
+    for (; head < (kv_head + 1) * a.share; ++head) {
+        if (SHAPED && a.span) {
             lds_barrier();
             bias_to_lds<T>(a, w, head);
         }
-        const char* const qp = a.q.p + (int64_t)it.q_row * a.q.row + head * a.q.head;
-        const char* const gp = a.d_o.p + (int64_t)it.q_row * a.d_o.row + head * a.d_o.head;
-        RowStage<T, D, kRows, 256> qs, gs;
-        float stat = 0.f;
-        auto fetch = [&](int q0) {
-            const int n = it.k_end - q0;
-            const uint64_t there = n >= 64 ? ~0ull : (1ull << n) - 1;
-            qs.load(qp + q0 * a.q.row, a.q.row, there, tid);
-            gs.load(gp + q0 * a.d_o.row, a.d_o.row, there, tid);
-            if (tid < 2 * kRows) {  // a row that is not there or sees nothing: its weights are 2^-inf
-                const int row = tid & (kRows - 1);
-                stat = tid < kRows ? -kNone : 0.f;
-                if (row < n) {
-                    const int64_t at = (int64_t)(it.q_row + q0 + row) * a.heads + head;
-                    stat = tid < kRows ? kLog2e * a.lse[at] : a.delta[at];
-                    if (stat == kNone) stat = -kNone;
-                }
-            }
-        };
-        if (it.k_begin < it.k_end) fetch(it.k_begin);
         for (int q0 = it.k_begin; q0 < it.k_end; q0 += kRows) {
-            qs.store(lds, tid);
-            gs.store(lds + kBuf / 2, tid);
-            if (tid < 2 * kRows) row_lse[tid] = stat;
-            lds_barrier();
-            const int rows = it.k_end - q0;
-            if (q0 + kRows < it.k_end) fetch(q0 + kRows);
+            if (tid < 2 * kRows) stats[(buf ^ 1) * 2 * kRows + tid] = stat;
+            loads_done_barrier();
+            buf ^= 1;
+            int next_q = q0 + kRows, next_head = head;
+            if (next_q >= it.k_end) next_q = it.k_begin, ++next_head;
+            const bool more = next_head < (kv_head + 1) * a.share;
+            const int next_n = it.k_end - next_q, to = (buf ^ 1) * kBuf;
+            const char* const next_qs = a.q.p + (int64_t)(it.q_row + next_q) * a.q.row + next_head * a.q.head;
+            const char* const next_gs = a.d_o.p + (int64_t)(it.q_row + next_q) * a.d_o.row + next_head * a.d_o.head;
+            if (more) fetch_stats(next_head, next_q);
+            // key0 counts in query rows: row i sees the keys up to its own place
+            if (count == 0 || (a.causal && q0 + kRows <= key0)) {
+                if (more) {
+                    feed.load(next_qs, (int)a.q.row, next_n, to);
+                    feed.load(next_gs, (int)a.d_o.row, next_n, to + kBuf / 2);
+                }
+                continue;
+            }
+            constexpr int kPer = RowFeed<T, D, kRows, 4>::kEach * 2 / (kRows / 32) / 2;  // requests of each of the two tensors in a tile of rows
+            auto ask_q = [&](int u) {
+                if (more)
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
+                    for (int i = 0; i < kPer; ++i) feed.one(u * kPer + i, next_qs, (int)a.q.row, next_n, to);
+            };
+            auto ask_g = [&](int u) {
+                if (more)
+#pragma unroll
+                    for (int i = 0; i < kPer; ++i) feed.one(u * kPer + i, next_gs, (int)a.d_o.row, next_n, to + kBuf / 2);
+            };
+            const char* const qs = lds + buf * kBuf;
+            const char* const gs = qs + kBuf / 2;
+            const float* const row_lse = stats + buf * 2 * kRows;
+            const float* const row_delta = row_lse + kRows;
+            // each product's fragments are requested one product ahead
+            AsRows<T, D> qr;
+            qr.load(qs, 0, lane);
+#pragma unroll
+            for (int u = 0; u < kRows / 32; ++u) {
                 const int first = q0 + 32 * u;
-                // key0 counts in query rows: row i sees the keys up to its own place
-                if (32 * u >= rows || count == 0 || (a.causal && first + 31 < key0)) continue;
-                const f32x16 x = dot_rows<T, D>(lds, 32 * u, k, lane);
-                float p[16], ds[16];
-#pragma unroll
-                for (int i = 0; i < 16; ++i) p[i] = x[i] * scale2;
-                if constexpr (BIAS) add_bias<-1>(p, a, w, key0, first, r, h);
-                const f32x16 dp = dot_rows<T, D>(lds + kBuf / 2, 32 * u, v, lane);
-                const int last = a.causal ? key0 + r - first - 4 * h : -4;  // rows before that one do not see the key
+                f32x16 p, ds;
+                f32x4 lse[4], delta[4];
+                AsRows<T, D> gr;
+                AsColumns<T, D> gc, qc;
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    const f32x4 lse = *reinterpret_cast<const f32x4*>(row_lse + 32 * u + 8 * g + 4 * h);
-                    const f32x4 delta = *reinterpret_cast<const f32x4*>(row_delta + 32 * u + 8 * g + 4 * h);
+                    lse[g] = *reinterpret_cast<const f32x4*>(row_lse + 32 * u + 8 * g + 4 * h);
+                    delta[g] = *reinterpret_cast<const f32x4*>(row_delta + 32 * u + 8 * g + 4 * h);
+                }
+                gr.load(gs, 32 * u, lane);
+                phase();
+                qr.dot(p, k);
+                phase();
+                ask_q(u);
+                gc.load(gs, 32 * u, lane);
+                phase();
+                if constexpr (SHAPED) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int i = 4 * g + e;
-                        p[i] = live && 8 * g + e >= last ? __builtin_amdgcn_exp2f(p[i] - lse[e]) : 0.f;
-                        ds[i] = p[i] * (dp[i] - delta[e]);
+                    for (int i = 0; i < 16; ++i) p[i] *= scale2;
+                    if (a.span) add_bias<-1>(p, a, w, key0, first, r, h);
+                    if (a.causal && first < key0 + 31) {  // rows before `last` do not see the lane's key
+                        const int last = key0 + r - first - 4 * h;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) p[i] = 8 * (i >> 2) + (i & 3) >= last ? p[i] : kNone;
                     }
                 }
-                add_weighted<D>(dv, lds + kBuf / 2, 32 * u, p, lane, (const T*)nullptr);
-                add_weighted<D>(dk, lds, 32 * u, ds, lane, (const T*)nullptr);
+                gr.dot(ds, v);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) p[i] = weight_of<SHAPED>(p[i], scale2, lse[i >> 2][i & 3]);
+                woven<0, 6>();
+                ask_g(u);
+                qc.load(qs, 32 * u, lane);
+                phase();
+                gc.add(dv, p);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) ds[i] = p[i] * (ds[i] - delta[i >> 2][i & 3]);
+                woven<4, 7>();
+                if (u + 1 < kRows / 32) qr.load(qs, 32 * (u + 1), lane);
+                phase();
+                qc.add(dk, ds);
             }
-            lds_barrier();
         }
     }
     lds_barrier();
+    if (!live) {  // its weights were those of a key of zeros
+        clear<R::kTiles>(dk);
+        clear<R::kTiles>(dv);
+    }
     char* const scratch = lds + wave * 32 * R::kPitch;
     store_tile<T, D>(dk, a.scale, scratch, a.dk.p + k_row0 * a.dk.row + kv_head * a.dk.head, a.dk.row, count, lane);
     store_tile<T, D>(dv, 1.f, scratch, a.dv.p + k_row0 * a.dv.row + kv_head * a.dv.head, a.dv.row, count, lane);
@@ -555,10 +659,12 @@ template <typename T> __global__ __launch_bounds__(64) void attn_dbias_kernel(Ra
 // ---------------------------------------------------------------- launches
 namespace {
 
-template <typename K> hipError_t launch(K kernel, DeviceOnce& once, int64_t blocks, size_t lds, const RaggedArgs& a, hipStream_t s) {
+size_t bias_bytes(const RaggedArgs& a) { return (a.span + 2 * kMargin) * sizeof(float); }
+
+template <typename K> hipError_t launch(K kernel, DeviceOnce& once, int64_t blocks, int threads, size_t lds, const RaggedArgs& a, hipStream_t s) {
     hipError_t e = once.run([&] { return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024 - 1024); });
     if (e != hipSuccess) return e;
-    kernel<<<dim3((unsigned)blocks), dim3(256), lds, s>>>(a);
+    kernel<<<dim3((unsigned)blocks), dim3(threads), lds, s>>>(a);
     return hipGetLastError();
 }
 // f(type, head size, bias)
@@ -580,9 +686,9 @@ hipError_t launch_attn_forward(const RaggedArgs& a, int head_dim, bool bf16, boo
         constexpr int D = decltype(d)::value;
         constexpr bool B = decltype(bias)::value;
         static DeviceOnce once_few, once_many;
-        const size_t w = B ? a.span * sizeof(float) : 0;
-        if (few) return launch(attn_few_kernel<T, D, B>, once_few, (int64_t)items * a.heads, 4 * 2 * 32 * Rows<T, D>::kPitch + w, a, s);
-        return launch(attn_forward_kernel<T, D, B>, once_many, (int64_t)items * a.heads, 4 * kKeys * Rows<T, D>::kPitch + w, a, s);
+        const size_t w = B ? bias_bytes(a) : 0;
+        if (few) return launch(attn_few_kernel<T, D, B>, once_few, (int64_t)items * a.heads, 256, 4 * 2 * 32 * Rows<T, D>::kPitch + w, a, s);
+        return launch(attn_forward_kernel<T, D, B>, once_many, (int64_t)items * a.heads, 256, 2 * Steps<T, D>::kBuf + w, a, s);
     });
 }
 
@@ -603,18 +709,18 @@ hipError_t launch_attn_dq(const RaggedArgs& a, int head_dim, bool bf16, int item
         constexpr int D = decltype(d)::value;
         constexpr bool B = decltype(bias)::value;
         static DeviceOnce once;
-        return launch(attn_dq_kernel<T, D, B>, once, (int64_t)items * a.heads, 2 * kKeys * Rows<T, D>::kPitch + (B ? 9 * a.span * sizeof(float) : 0), a, s);
+        return launch(attn_dq_kernel<T, D, B>, once, (int64_t)items * a.heads, 256, 2 * Steps<T, D>::kBuf + (B ? 9 * bias_bytes(a) : 0), a, s);
     });
 }
 
 hipError_t launch_attn_dkv(const RaggedArgs& a, int head_dim, bool bf16, int items, hipStream_t s) {
     if (items == 0) return hipSuccess;
-    return by_kind(head_dim, bf16, a.bias != nullptr, [&](auto* t, auto d, auto bias) {
+    return by_kind(head_dim, bf16, a.bias != nullptr || a.causal, [&](auto* t, auto d, auto bias) {
         typedef std::remove_pointer_t<decltype(t)> T;
         constexpr int D = decltype(d)::value;
         constexpr bool B = decltype(bias)::value;
         static DeviceOnce once;
-        return launch(attn_dkv_kernel<T, D, B>, once, (int64_t)items * (a.heads / a.share), 2 * 64 * Rows<T, D>::kPitch + 512 + (B ? a.span * sizeof(float) : 0), a, s);
+        return launch(attn_dkv_kernel<T, D, B>, once, (int64_t)items * (a.heads / a.share), 256, 2 * Steps<T, D>::kBuf + 4 * Rows<T, D>::kStep * sizeof(float) + (B ? bias_bytes(a) : 0), a, s);
     });
 }
 

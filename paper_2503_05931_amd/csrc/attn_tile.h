@@ -23,6 +23,8 @@ template <typename T, int D> struct Rows {
     typedef typename Chunk<T>::type chunk_t;
     static constexpr int kPitch = D * (int)sizeof(T), kChunks = kPitch / 16, kSteps = kChunks / 2, kTiles = D / 32;
     static constexpr int kWide = kPitch > 256;  // a workgroup's rows fill the LDS of half a CU and more: one of them has all its registers
+    static constexpr int kStep = kWide ? 32 : 64;  // rows of a step of the kernels that walk over keys or queries
+    static constexpr uint64_t kAll = kWide ? 0xffffffffull : ~0ull;  // a bit for each of them
     static __device__ __forceinline__ int swap_of(int row) { return ((row & 3) << 1) | ((row >> 2) & 1); }
     static __device__ __forceinline__ int at(int row, int chunk) { return row * kPitch + ((chunk ^ swap_of(row)) << 4); }
 };
@@ -51,75 +53,154 @@ template <typename T, int D> struct RowFrag {
     }
 };
 
-// acc[i][j] = sum over D of a row i in LDS (first .. first + 31 of `rows`) times row j held in registers
-template <typename T, int D> __device__ __forceinline__ f32x16 dot_rows(const char* rows, int first, const RowFrag<T, D>& f, int lane) {
-    f32x16 acc;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) acc[i] = 0.f;
-#pragma unroll
-    for (int s = 0; s < Rows<T, D>::kSteps; ++s)
-        mma_rows(acc, *reinterpret_cast<const typename Chunk<T>::type*>(rows + Rows<T, D>::at(first + (lane & 31), 2 * s + (lane >> 5))), f.c[s]);
-    return acc;
-}
-
-// acc[t] (columns 32 t .. + 31 of D, by the 32 columns of w) += rows^T w: w[i] is the lane's weight of LDS row first + 8 g + 4 h + e,
-// i = 4 g + e, which is how a product of tiles leaves it.  In bfloat16 the weights are rounded here.
-template <int D> __device__ __forceinline__ void add_weighted(f32x16* acc, const char* rows, int first, const float* w, int lane, const bf16_t*) {
+// 32 rows of LDS on their way into products.  bfloat16: load() requests the fragments, so that they travel while the matrix cores are at
+// work on the ones before; float32, whose instructions take 16 times as long over a fragment, reads them at their use.
+//
+// AsRows: acc[i][j] = sum over D of row i of these times row j of the rows held in registers
+template <typename T, int D> struct AsRows;
+template <int D> struct AsRows<bf16_t, D> {
     typedef Rows<bf16_t, D> R;
-    const int i = lane & 15, sub = (lane >> 4) & 1, h = lane >> 5;
-    const char* p = rows + (first + 4 * h + (i >> 2)) * R::kPitch + 8 * (i & 1);
-    const int sw = ((i >> 2) << 1) | h, c0 = 2 * sub + ((i & 3) >> 1);
+    bf16x8 c[R::kSteps];
+    __device__ __forceinline__ void load(const char* rows, int first, int lane) {
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-        bf16x8 b;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) b[e] = (bf16_t)w[8 * s + e];
-#pragma unroll
-        for (int t = 0; t < R::kTiles; ++t) {
-            u32x2 v[2];
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-                v[u] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(
-                                                     p + (16 * s + 8 * u) * R::kPitch + (((4 * t + c0) ^ sw) << 4))));
-            acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, u32x4{v[0][0], v[0][1], v[1][0], v[1][1]}), b, acc[t], 0, 0, 0);
-        }
+        for (int s = 0; s < R::kSteps; ++s) c[s] = *reinterpret_cast<const bf16x8*>(rows + R::at(first + (lane & 31), 2 * s + (lane >> 5)));
     }
-}
-template <int D> __device__ __forceinline__ void add_weighted(f32x16* acc, const char* rows, int first, const float* w, int lane, const float*) {
+    __device__ __forceinline__ void dot(f32x16& acc, const RowFrag<bf16_t, D>& f) const {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[i] = 0.f;
+#pragma unroll
+        for (int s = 0; s < R::kSteps; ++s) mma_rows(acc, c[s], f.c[s]);
+    }
+};
+template <int D> struct AsRows<float, D> {
     typedef Rows<float, D> R;
-    const int r = lane & 31, h = lane >> 5;
+    const char* rows;
+    int row, h;
+    __device__ __forceinline__ void load(const char* rows_, int first, int lane) { rows = rows_, row = first + (lane & 31), h = lane >> 5; }
+    __device__ __forceinline__ void dot(f32x16& acc, const RowFrag<float, D>& f) const {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const int row = 8 * (i >> 2) + 4 * h + (i & 3), sw = ((i & 3) << 1) | h;
+        for (int i = 0; i < 16; ++i) acc[i] = 0.f;
 #pragma unroll
-        for (int t = 0; t < R::kTiles; ++t) {
-            const float v = *reinterpret_cast<const float*>(rows + (first + row) * R::kPitch + (((8 * t + (r >> 2)) ^ sw) << 4) + 4 * (r & 3));
-            acc[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, w[i], acc[t], 0, 0, 0);
+        for (int s = 0; s < R::kSteps; ++s) mma_rows(acc, *reinterpret_cast<const f32x4*>(rows + R::at(row, 2 * s + h)), f.c[s]);
+    }
+};
+// AsColumns: acc[t] (columns 32 t .. + 31 of D, by the 32 columns of w) += rows^T w: w[i] is the lane's weight of row 8 g + 4 h + e,
+// i = 4 g + e, which is how a product of tiles leaves it.  In bfloat16 the weights are rounded here.
+template <typename T, int D> struct AsColumns;
+template <int D> struct AsColumns<bf16_t, D> {
+    typedef Rows<bf16_t, D> R;
+    bf16x8 c[2][R::kTiles];
+    __device__ __forceinline__ void load(const char* rows, int first, int lane) {
+        const int i = lane & 15, sub = (lane >> 4) & 1, h = lane >> 5;
+        const char* p = rows + (first + 4 * h + (i >> 2)) * R::kPitch + 8 * (i & 1);
+        const int sw = ((i >> 2) << 1) | h, c0 = 2 * sub + ((i & 3) >> 1);
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int t = 0; t < R::kTiles; ++t) {
+                u32x2 v[2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+                    v[u] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(
+                                                         p + (16 * s + 8 * u) * R::kPitch + (((4 * t + c0) ^ sw) << 4))));
+                c[s][t] = __builtin_bit_cast(bf16x8, u32x4{v[0][0], v[0][1], v[1][0], v[1][1]});
+            }
+    }
+    __device__ __forceinline__ void add(f32x16* acc, const f32x16& w) const {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            bf16x8 b;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) b[e] = (bf16_t)w[8 * s + e];
+#pragma unroll
+            for (int t = 0; t < R::kTiles; ++t) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(c[s][t], b, acc[t], 0, 0, 0);
         }
     }
-}
+};
+template <int D> struct AsColumns<float, D> {
+    typedef Rows<float, D> R;
+    const char* p;
+    int r, h;
+    __device__ __forceinline__ void load(const char* rows, int first, int lane) { p = rows + first * R::kPitch, r = lane & 31, h = lane >> 5; }
+    __device__ __forceinline__ void add(f32x16* acc, const f32x16& w) const {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int row = 8 * (i >> 2) + 4 * h + (i & 3), sw = ((i & 3) << 1) | h;
+#pragma unroll
+            for (int t = 0; t < R::kTiles; ++t) {
+                const float v = *reinterpret_cast<const float*>(p + row * R::kPitch + (((8 * t + (r >> 2)) ^ sw) << 4) + 4 * (r & 3));
+                acc[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, w[i], acc[t], 0, 0, 0);
+            }
+        }
+    }
+};
 
-// N rows on their way from memory to LDS through the registers of THREADS threads
+// N rows on their way from memory to LDS through the registers of THREADS threads.  Rows that are not there are beyond the end of the
+// descriptor, rows that are not seen are sent there: both come as zeros, whatever stands in their place.
 template <typename T, int D, int N, int THREADS> struct RowStage {
     typedef Rows<T, D> R;
-    static constexpr int kEach = N * R::kChunks / THREADS;
+    static constexpr int kEach = N * R::kChunks / THREADS, kApart = THREADS / R::kChunks;
     static_assert(N * R::kChunks % THREADS == 0 && THREADS % R::kChunks == 0, "a thread keeps its column");
     typename R::chunk_t c[kEach];
-    // live: bit n = row n is there and is seen (others are zeros: what stands in their place may be infinite)
-    __device__ __forceinline__ void load(const char* first, int64_t pitch, uint64_t live, int tid) {
-        const int row = tid / R::kChunks;
-        const char* p = first + row * pitch + (tid % R::kChunks) * 16;
+    // first: the first of `count` >= 1 rows; live: bit n = row n is seen (looked at if MASK)
+    template <bool MASK> __device__ __forceinline__ void load(const char* first, int pitch, int count, uint64_t live, int tid) {
+        const __amdgpu_buffer_rsrc_t rsrc =
+            __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(first), 0, (min(count, N) - 1) * pitch + R::kPitch, 0x20000);
+        const int row = tid / R::kChunks, off = row * pitch + (tid % R::kChunks) * 16;
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            const int n = row + i * (THREADS / R::kChunks);
-            c[i] = (typename R::chunk_t)(0);
-            if ((live >> n) & 1) c[i] = load_global<typename R::chunk_t>(p + (int64_t)i * (THREADS / R::kChunks) * pitch);
+            int at = off;
+            if constexpr (MASK) at = (live >> (row + i * kApart)) & 1 ? at : kBeyond;
+            c[i] = __builtin_bit_cast(typename R::chunk_t, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, i * kApart * pitch, 0));
         }
     }
     __device__ __forceinline__ void store(char* lds, int tid) const {
         const int row = tid / R::kChunks, chunk = tid % R::kChunks;
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) *reinterpret_cast<typename R::chunk_t*>(lds + R::at(row + i * (THREADS / R::kChunks), chunk)) = c[i];
+        for (int i = 0; i < kEach; ++i) *reinterpret_cast<typename R::chunk_t*>(lds + R::at(row + i * kApart, chunk)) = c[i];
+    }
+    static constexpr int kBeyond = 0x40000000;  // past any descriptor's end: a step's rows span less (kAttnMaxPitch)
+};
+// One request: every lane's 16 bytes at base + off go to LDS byte (lds_base + 16 * lane).  base and lds_base are wavefront-uniform.  The
+// compiler does not see the data arrive: loads_done_barrier() waits for it.
+__device__ __forceinline__ void load_to_lds16(const char* base, int off, unsigned lds_base) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n" ::"s"(lds_base), "v"(off), "s"(base) : "memory");
+}
+// This wavefront's loads have arrived and its LDS accesses are done, then the barrier.  The wait is the builtin: the compiler, which keeps
+// count of its own loads, knows that none is left, and does not wait for them (and with them for requests to LDS) in the loop that follows.
+__device__ __forceinline__ void loads_done_barrier() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt 0, lgkmcnt 0
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// N rows from memory to LDS, no registers in between, by the W wavefronts of a workgroup.  A request fills 1 KB of consecutive LDS, so
+// what changes places are the chunks that the lanes ask for.  Rows past `count` get the last one that is there.
+template <typename T, int D, int N, int W> struct RowFeed {
+    typedef Rows<T, D> R;
+    static constexpr int kAtOnce = 64 / R::kChunks, kEach = N / (W * kAtOnce);  // rows of a request, requests of a wavefront
+    static_assert(W * kAtOnce % 8 == 0 && N % (W * kAtOnce) == 0, "a lane's rows agree in what its chunk is");
+    int row, chunk;
+    unsigned lds0;
+    __device__ __forceinline__ RowFeed(const char* lds, int wave, int lane) {
+        row = wave * kAtOnce + lane / R::kChunks;
+        chunk = ((lane % R::kChunks) ^ R::swap_of(row)) * 16;
+        lds0 = (unsigned)(uintptr_t)(const __attribute__((address_space(3))) char*)lds + wave * 1024;
+    }
+    // the i-th of a wavefront's kEach requests
+    __device__ __forceinline__ void one(int i, const char* first, int pitch, int count, int lds_offset) const {
+        load_to_lds16(first, min(row + i * W * kAtOnce, count - 1) * pitch + chunk, lds0 + lds_offset + i * W * 1024);
+    }
+    __device__ __forceinline__ void load(const char* first, int pitch, int count, int lds_offset) const {
+        if (count >= N) {
+            const int off = row * pitch + chunk;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) load_to_lds16(first + (int64_t)i * (W * kAtOnce) * pitch, off, lds0 + lds_offset + i * W * 1024);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) load_to_lds16(first, min(row + i * W * kAtOnce, count - 1) * pitch + chunk, lds0 + lds_offset + i * W * 1024);
+        }
     }
 };
 
