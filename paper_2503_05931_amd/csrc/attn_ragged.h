@@ -43,7 +43,7 @@ struct RaggedArgs {
 };
 
 constexpr int kAttnRows = 128;  // query rows of an item of many (attn_forward_kernel), keys of an item of key gradients
-constexpr int kAttnMargin = 64;  // places of the bias in LDS beyond both ends of its range
+constexpr int kAttnMargin = 72;  // places of the bias in LDS beyond both ends of its range
 constexpr int kAttnMaxPitch = 0x40000000 / 64 - 64;  // bytes between rows: 64 of them stay below 2^30, and twice that in 32 bits
 constexpr int kAttnFew = 32;    // and of few (attn_few_kernel)
 
