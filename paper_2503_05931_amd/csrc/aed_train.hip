@@ -119,7 +119,8 @@ aed_status check_attn(const aed_attn_config* c, const int32_t* q_lens, const int
 
 void lay_out(aed_attn& p, const int32_t* q_lens, const int32_t* k_lens, const int64_t* k_starts, int32_t batch) {
     const aed_attn_config& c = p.cfg;
-    p.plan = aed::plan_attention(q_lens, k_lens, k_starts, batch, c.n_heads, c.causal != 0, c.training != 0, aed::kAttnRows, aed::kAttnFew);
+    p.plan = aed::plan_attention(q_lens, k_lens, k_starts, batch, c.n_heads, c.causal != 0, c.training != 0, aed::kAttnRows,
+                                 c.dtype == 0 && c.head_dim == 128 ? 0 : aed::kAttnPair, aed::kAttnFew);  // wide rows have no pairs
     p.k_rows = 0;
     for (int b = 0; b < batch; ++b) p.k_rows += k_lens[b];
     p.forward = p.arena.table(p.plan.forward);
@@ -342,7 +343,8 @@ aed_status aed_attn_forward(aed_attn* p, const aed_rows* q, const aed_rows* k, c
     if (st != AED_OK) return st;
     const bool bf16 = p->cfg.dtype == 1;
     a.items = items(p, p->forward);
-    hipError_t e = aed::launch_attn_forward(a, p->cfg.head_dim, bf16, p->plan.few, (int)p->plan.forward.size(), p->stream);
+    a.n_items = (int)p->plan.forward.size();
+    hipError_t e = aed::launch_attn_forward(a, p->cfg.head_dim, bf16, p->plan.tile_rows, p->stream);
     if (e == hipSuccess) e = aed::launch_attn_join(a, p->cfg.head_dim, bf16, p->plan.tile_rows, (int)p->plan.joins.size(), p->stream);
     return hip_status(e, "aed_attn_forward");
 }
@@ -365,10 +367,12 @@ aed_status aed_attn_backward(aed_attn* p, const aed_rows* d_out, const aed_rows*
     if ((bias != nullptr) != (d_bias != nullptr)) return fail(AED_EINVAL, bias ? "d_bias is NULL" : "the handle was made without a bias");
     if ((uintptr_t)d_bias % es != 0) return fail(AED_EINVAL, "d_bias is not aligned to its elements");
     a.items = items(p, p->dq);
-    hipError_t e = aed::launch_attn_dq(a, c.head_dim, bf16, (int)p->plan.dq.size(), p->stream);
+    a.n_items = a.bias_items = (int)p->plan.dq.size();
+    a.d_bias = d_bias;
+    hipError_t e = aed::launch_attn_dq(a, c.head_dim, bf16, p->plan.dq_rows, p->stream);
     a.items = items(p, p->dkv);
-    if (e == hipSuccess) e = aed::launch_attn_dkv(a, c.head_dim, bf16, (int)p->plan.dkv.size(), p->stream);
-    if (e == hipSuccess && bias) e = aed::launch_attn_dbias(a, bf16, (int)p->plan.dq.size(), d_bias, p->stream);
+    a.n_items = (int)p->plan.dkv.size();
+    if (e == hipSuccess) e = aed::launch_attn_dkv(a, c.head_dim, bf16, p->stream);
     return hip_status(e, "aed_attn_backward");
 }
 

@@ -46,22 +46,21 @@ struct PlanJoin {
 };
 
 struct AttnPlan {
-    bool few = false;
-    int tile_rows = 0, n_parts = 0;
+    int tile_rows = 0, dq_rows = 0, n_parts = 0;  // query rows of an item, forward and backward
     std::vector<PlanItem> forward, dq, dkv;
     std::vector<PlanJoin> joins;
     int64_t q_rows = 0;
 };
 
-// tile_many, tile_few: query rows of an item (and keys of one of key gradients)
+// tile_many, tile_pair, tile_few: query rows of an item (tile_many: keys of one of key gradients), by the longest sequence's
 inline AttnPlan plan_attention(const int32_t* q_lens, const int32_t* k_lens, const int64_t* k_starts, int batch, int heads, bool causal, bool training,
-                               int tile_many, int tile_few) {
+                               int tile_many, int tile_pair, int tile_few) {
     AttnPlan p;
     int most = 0;
     for (int b = 0; b < batch; ++b) most = std::max(most, (int)q_lens[b]);
-    p.few = most <= tile_few;
-    p.tile_rows = p.few ? tile_few : tile_many;
-    const int step = p.few ? 128 : 64;  // keys that a workgroup takes at once
+    p.dq_rows = most <= tile_pair ? tile_pair : tile_many;
+    p.tile_rows = most <= tile_few ? tile_few : p.dq_rows;
+    const int step = p.tile_rows == tile_few ? 128 : 64;  // keys that a workgroup takes at once
     std::vector<PlanItem> whole;
     int64_t q_row = 0, packed = 0, steps = 0;
     auto tiles = [&](int tile, std::vector<PlanItem>& to, int b, int64_t k_row) {
@@ -76,7 +75,7 @@ inline AttnPlan plan_attention(const int32_t* q_lens, const int32_t* k_lens, con
         const int64_t k_row = k_starts ? k_starts[b] : packed;
         tiles(p.tile_rows, whole, b, k_row);
         if (training) {
-            tiles(tile_many, p.dq, b, k_row);
+            tiles(p.dq_rows, p.dq, b, k_row);
             for (int k0 = 0; k0 < nk; k0 += tile_many) {
                 const int pos = k0 - (nk - nq);
                 p.dkv.push_back(PlanItem{k_row + k0, (int32_t)q_row, std::min(tile_many, nk - k0), pos, causal ? std::max(0, std::min(nq, pos)) : 0, nq, -1});

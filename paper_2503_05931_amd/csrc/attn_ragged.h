@@ -36,22 +36,26 @@ struct RaggedArgs {
     float2* part_ml;         // [part, heads, tile rows]: maximum (of scores times log2 e) and sum
     float* part_bias;        // [item, heads, buckets]
     const RaggedItem* items;
+    int n_items;
+    int bias_items;          // items that part_bias has sums of
+    void* d_bias;            // [buckets, heads]
     const RaggedJoin* joins;
     float scale;
     int heads, share;        // share: query heads to a key head
     int causal, buckets, max_distance, span;
 };
 
-constexpr int kAttnRows = 128;  // query rows of an item of many (attn_forward_kernel), keys of an item of key gradients
+constexpr int kAttnRows = 128;  // query rows of an item of many, keys of an item of key gradients
+constexpr int kAttnPair = 64;   // query rows of an item whose wavefronts share rows in pairs
+constexpr int kAttnFew = 32;    // and of few (attn_few_kernel)
 constexpr int kAttnMargin = 72;  // places of the bias in LDS beyond both ends of its range
 constexpr int kAttnMaxPitch = 0x40000000 / 64 - 64;  // bytes between rows: 64 of them stay below 2^30, and twice that in 32 bits
-constexpr int kAttnFew = 32;    // and of few (attn_few_kernel)
 
-// few: items of kAttnFew rows.  Each returns hipSuccess or what the launch reported.
-hipError_t launch_attn_forward(const RaggedArgs& a, int head_dim, bool bf16, bool few, int items, hipStream_t s);
+// Each returns hipSuccess or what the launch reported.  tile_rows: query rows of an item.
+hipError_t launch_attn_forward(const RaggedArgs& a, int head_dim, bool bf16, int tile_rows, hipStream_t s);
 hipError_t launch_attn_join(const RaggedArgs& a, int head_dim, bool bf16, int tile_rows, int joins, hipStream_t s);
-hipError_t launch_attn_dq(const RaggedArgs& a, int head_dim, bool bf16, int items, hipStream_t s);
-hipError_t launch_attn_dkv(const RaggedArgs& a, int head_dim, bool bf16, int items, hipStream_t s);
-hipError_t launch_attn_dbias(const RaggedArgs& a, bool bf16, int items, void* d_bias, hipStream_t s);
+hipError_t launch_attn_dq(const RaggedArgs& a, int head_dim, bool bf16, int tile_rows, hipStream_t s);
+// and the bias's gradient from what dq's launch left
+hipError_t launch_attn_dkv(const RaggedArgs& a, int head_dim, bool bf16, hipStream_t s);
 
 }  // namespace aed

@@ -195,8 +195,9 @@ __device__ __forceinline__ int end_of(const RaggedArgs& a, const RaggedItem& it,
 }
 
 // A workgroup's walk over the keys, kStep of them a step: keys and values from memory to LDS (rows of keys, then of values), two
-// steps' worth: one is worked on while the other is on its way.
-template <typename T, int D> struct Steps {
+// steps' worth: one is worked on while the other is on its way.  KEYS: keys that are not seen are cleared, not only their values (they
+// enter a product with weights of 0, and may be infinite).
+template <typename T, int D, bool KEYS> struct Steps {
     typedef Rows<T, D> R;
     static constexpr int kBuf = 2 * R::kStep * R::kPitch;
     const RaggedArgs& a;
@@ -223,10 +224,16 @@ template <typename T, int D> struct Steps {
         loads_done_barrier();
         buf ^= 1;
         seen = seen_next;
-        if (a.key_mask && (seen & R::kAll) != R::kAll) {  // what stands in the place of keys that are not seen may be infinite
-            for (int i = threadIdx.x; i < 2 * R::kStep * R::kChunks; i += 256) {
-                const int row = i / R::kChunks;
-                if (!((seen >> (row & (R::kStep - 1))) & 1)) *reinterpret_cast<typename R::chunk_t*>(lds + buf * kBuf + i * 16) = (typename R::chunk_t)(0);
+        if (a.key_mask && (seen & R::kAll) != R::kAll) {
+            constexpr int kThreads = 256 / R::kStep, kEach = R::kPitch / kThreads;  // of a row, and their bytes
+            const int row = threadIdx.x / kThreads;
+            if (!((seen >> row) & 1)) {
+                char* const p = lds + buf * kBuf + row * R::kPitch + threadIdx.x % kThreads * kEach;
+#pragma unroll
+                for (int i = 0; i < kEach; i += 16) {
+                    if constexpr (KEYS) *reinterpret_cast<typename R::chunk_t*>(p + i) = (typename R::chunk_t)(0);
+                    *reinterpret_cast<typename R::chunk_t*>(p + kBuf / 2 + i) = (typename R::chunk_t)(0);
+                }
             }
             lds_barrier();
         }
@@ -238,16 +245,20 @@ template <typename T, int D> struct Steps {
 }  // namespace
 
 // ---------------------------------------------------------------- forward, many rows
-// A workgroup takes 128 query rows of a head, 32 a wavefront, and walks the keys.
-template <typename T, int D, bool BIAS> __global__ __launch_bounds__(256, (2 - Rows<T, D>::kWide)) void attn_forward_kernel(RaggedArgs a) {
+// A workgroup takes 128 query rows of a head, 32 a wavefront, and walks the keys.  PAIR: it takes 64 rows, and two wavefronts share 32 of them,
+// each with 32 keys of a step.
+template <typename T, int D, bool BIAS, bool PAIR> __global__ __launch_bounds__(256, (2 - Rows<T, D>::kWide)) void attn_forward_kernel(RaggedArgs a) {
     typedef Rows<T, D> R;
     extern __shared__ __align__(16) char lds[];
-    constexpr int kSub = R::kStep / 32;
-    float* const w = reinterpret_cast<float*>(lds + 2 * Steps<T, D>::kBuf);
+    constexpr int kJoin = 2 * 64 * R::kTiles * 64 + 1024;  // two wavefronts' sums, and their maxima
+    constexpr int kSub = PAIR ? 1 : R::kStep / 32;  // 32-key tiles of a step
+    static_assert(!PAIR || R::kStep == 64, "a tile for each of two");
+    float* const w = reinterpret_cast<float*>(lds + 2 * Steps<T, D, false>::kBuf);
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 31, h = lane >> 5;
     const RaggedItem it = a.items[blockIdx.x / a.heads];
-    const int head = blockIdx.x % a.heads, row0 = it.q_row + 32 * wave, count = min(max(it.rows - 32 * wave, 0), 32), pos = it.pos + 32 * wave;
-    Steps<T, D> step(a, it, head / a.share, lds, wave, lane);
+    const int group = PAIR ? wave & 1 : wave, tile = PAIR ? wave >> 1 : 0;  // which rows, which keys of a step
+    const int head = blockIdx.x % a.heads, row0 = it.q_row + 32 * group, count = min(max(it.rows - 32 * group, 0), 32), pos = it.pos + 32 * group;
+    Steps<T, D, false> step(a, it, head / a.share, lds, wave, lane);
     step.fetch(it.k_begin);
     RowFrag<T, D> q;
     q.load(a.q.p + (int64_t)(row0 + r) * a.q.row + head * a.q.head, r < count, h);
@@ -265,18 +276,18 @@ template <typename T, int D, bool BIAS> __global__ __launch_bounds__(256, (2 - R
         AsRows<T, D> k[kSub];
         AsColumns<T, D> v[kSub];
 #pragma unroll
-        for (int u = 0; u < kSub; ++u) k[u].load(step.keys(), 32 * u, lane);
+        for (int u = 0; u < kSub; ++u) k[u].load(step.keys(), 32 * (tile + u), lane);
         phase();
         k[0].dot(s[0], q);
         phase();
-        v[0].load(step.values(), 0, lane);
+        v[0].load(step.values(), 32 * tile, lane);
         phase();
         if constexpr (kSub > 1) k[1].dot(s[1], q);
         const uint64_t seen = seen_from(step.seen, k0, pos + r, a.causal);
         float top = kNone;
 #pragma unroll
         for (int u = 0; u < kSub; ++u) {
-            finish_scores<BIAS>(s[u], a, scale2, w, (uint32_t)(seen >> (32 * u)), k0 + 32 * u, pos, r, h);
+            finish_scores<BIAS>(s[u], a, scale2, w, (uint32_t)(seen >> (32 * (tile + u))), k0 + 32 * (tile + u), pos, r, h);
             top = fmaxf(top, max_of(s[u]));
         }
         top = max_halves(top);
@@ -295,13 +306,39 @@ template <typename T, int D, bool BIAS> __global__ __launch_bounds__(256, (2 - R
         step.next();
         step.fetch(k0 + R::kStep);
     }
-    const float l = sum_halves(run.l);
-    if (it.part < 0) {
+    float l = sum_halves(run.l);
+    if constexpr (PAIR) {  // the second wavefront's maximum and sums join the first's
         lds_barrier();
-        store_tile<T, D>(acc, l > 0.f ? 1.f / l : l, lds + wave * 32 * R::kPitch, a.o.p + (int64_t)row0 * a.o.row + head * a.o.head, a.o.row, count, lane);
+        float* const given = reinterpret_cast<float*>(lds) + (group * 64 + lane) * 4;
+        float2* const ml = reinterpret_cast<float2*>(lds + kJoin - 1024) + group * 64 + lane;
+        if (tile == 1) {
+            *ml = float2{run.m, l};
+#pragma unroll
+            for (int t = 0; t < R::kTiles; ++t)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    *reinterpret_cast<f32x4*>(given + (t * 4 + g) * 512) = f32x4{acc[t][4 * g], acc[t][4 * g + 1], acc[t][4 * g + 2], acc[t][4 * g + 3]};
+        }
+        lds_barrier();
+        if (tile == 1) return;
+        const float m = fmaxf(run.m, ml->x), alpha = __builtin_amdgcn_exp2f(run.m - base_of(m)), beta = __builtin_amdgcn_exp2f(ml->x - base_of(m));
+#pragma unroll
+        for (int t = 0; t < R::kTiles; ++t)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const f32x4 v = *reinterpret_cast<const f32x4*>(given + (t * 4 + g) * 512);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[t][4 * g + e] = acc[t][4 * g + e] * alpha + v[e] * beta;
+            }
+        l = l * alpha + ml->y * beta;
+        run.m = m;
+    }
+    if (it.part < 0) {
+        if constexpr (!PAIR) lds_barrier();
+        store_tile<T, D>(acc, l > 0.f ? 1.f / l : l, lds + (PAIR ? kJoin : 0) + group * 32 * R::kPitch, a.o.p + (int64_t)row0 * a.o.row + head * a.o.head, a.o.row, count, lane);
         if (h == 0 && r < count) a.lse[(int64_t)(row0 + r) * a.heads + head] = kLn2 * (run.m + __builtin_amdgcn_logf(l));
     } else if (r < count) {
-        const int64_t at = ((int64_t)it.part * a.heads + head) * kAttnRows + 32 * wave + r;
+        const int64_t at = ((int64_t)it.part * a.heads + head) * (PAIR ? kAttnPair : kAttnRows) + 32 * group + r;
 #pragma unroll
         for (int t = 0; t < R::kTiles; ++t)
 #pragma unroll
@@ -431,17 +468,20 @@ template <typename T, int D> __global__ __launch_bounds__(256) void attn_join_ke
 // The forward kernel's walk with two products to a tile of scores (K Q^T and V dO^T, transposed, a lane being a query) and one
 // more for dQ.  delta is left for the key gradients' kernel, without the error that the rounded output leaves in it: a row's dS add up
 // to 0, so what they do add up to is what delta lacks.
-template <typename T, int D, bool BIAS> __global__ __launch_bounds__(256, (2 - Rows<T, D>::kWide)) void attn_dq_kernel(RaggedArgs a) {
+template <typename T, int D, bool BIAS, bool PAIR> __global__ __launch_bounds__(256, (2 - Rows<T, D>::kWide)) void attn_dq_kernel(RaggedArgs a) {
     typedef Rows<T, D> R;
     extern __shared__ __align__(16) char lds[];
-    float* const w = reinterpret_cast<float*>(lds + 2 * Steps<T, D>::kBuf);
+    constexpr int kJoin = 2 * 64 * R::kTiles * 64 + 512;  // two wavefronts' sums, and of their rows' delta
+    static_assert(!PAIR || R::kStep == 64, "a tile for each of two");
+    float* const w = reinterpret_cast<float*>(lds + 2 * Steps<T, D, true>::kBuf);
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 31, h = lane >> 5;
     const int places = bias_places(a);
     float* const sums = w + places;  // [wavefront, half][places]
     const int item = blockIdx.x / a.heads;
     const RaggedItem it = a.items[item];
-    const int head = blockIdx.x % a.heads, row0 = it.q_row + 32 * wave, count = min(max(it.rows - 32 * wave, 0), 32), pos = it.pos + 32 * wave;
-    Steps<T, D> step(a, it, head / a.share, lds, wave, lane);
+    const int group = PAIR ? wave & 1 : wave, tile = PAIR ? wave >> 1 : 0;  // which rows, which keys of a step
+    const int head = blockIdx.x % a.heads, row0 = it.q_row + 32 * group, count = min(max(it.rows - 32 * group, 0), 32), pos = it.pos + 32 * group;
+    Steps<T, D, true> step(a, it, head / a.share, lds, wave, lane);
     step.fetch(it.k_begin);
     const bool live = r < count;
     RowFrag<T, D> q, d_o;
@@ -475,22 +515,23 @@ template <typename T, int D, bool BIAS> __global__ __launch_bounds__(256, (2 - R
         // rows that are not there are all zeros: what they add is too
         const uint64_t seen = live ? seen_from(step.seen, k0, pos + r, a.causal) : ~0ull;
 #pragma unroll
-        for (int u = 0; u < R::kStep / 32; ++u) {
+        for (int u = 0; u < (PAIR ? 1 : R::kStep / 32); ++u) {
+            const int key = 32 * (tile + u);
             f32x16 s, dp;
             AsRows<T, D> k, v;
             AsColumns<T, D> kt;
-            k.load(step.keys(), 32 * u, lane);
+            k.load(step.keys(), key, lane);
             k.dot(s, q);
-            v.load(step.values(), 32 * u, lane);
+            v.load(step.values(), key, lane);
             v.dot(dp, d_o);
-            finish_scores<BIAS>(s, a, scale2, w, (uint32_t)(seen >> (32 * u)), k0 + 32 * u, pos, r, h);
+            finish_scores<BIAS>(s, a, scale2, w, (uint32_t)(seen >> key), k0 + key, pos, r, h);
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 s[i] = weight_of<BIAS>(s[i], scale2, base) * (dp[i] - delta);
                 rest += s[i];
             }
-            if constexpr (BIAS) add_distances(s, a, sums + (2 * wave + h) * places, far, near, k0 + 32 * u, pos, lane);
-            kt.load(step.keys(), 32 * u, lane);
+            if constexpr (BIAS) add_distances(s, a, sums + (2 * wave + h) * places, far, near, k0 + key, pos, lane);
+            kt.load(step.keys(), key, lane);
             kt.add(acc, s);
         }
     }
@@ -500,8 +541,34 @@ template <typename T, int D, bool BIAS> __global__ __launch_bounds__(256, (2 - R
     }
     lds_barrier();
     rest = sum_halves(rest);
-    if (live && h == 0) a.delta[(int64_t)(row0 + r) * a.heads + head] = delta + rest;
-    store_tile<T, D>(acc, a.scale, lds + wave * 32 * R::kPitch, a.dq.p + (int64_t)row0 * a.dq.row + head * a.dq.head, a.dq.row, count, lane);
+    if constexpr (PAIR) {  // the second wavefront's sums join the first's
+        float* const given = reinterpret_cast<float*>(lds) + (group * 64 + lane) * 4;
+        float* const rests = reinterpret_cast<float*>(lds + kJoin - 512) + group * 64 + lane;
+        if (tile == 1) {
+            *rests = rest;
+#pragma unroll
+            for (int t = 0; t < R::kTiles; ++t)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    *reinterpret_cast<f32x4*>(given + (t * 4 + g) * 512) = f32x4{acc[t][4 * g], acc[t][4 * g + 1], acc[t][4 * g + 2], acc[t][4 * g + 3]};
+        }
+        lds_barrier();
+        if (tile == 0) {
+            rest += *rests;
+#pragma unroll
+            for (int t = 0; t < R::kTiles; ++t)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const f32x4 v = *reinterpret_cast<const f32x4*>(given + (t * 4 + g) * 512);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[t][4 * g + e] += v[e];
+                }
+        }
+    }
+    if (tile == 0) {
+        if (live && h == 0) a.delta[(int64_t)(row0 + r) * a.heads + head] = delta + rest;
+        store_tile<T, D>(acc, a.scale, lds + (PAIR ? kJoin : 0) + group * 32 * R::kPitch, a.dq.p + (int64_t)row0 * a.dq.row + head * a.dq.head, a.dq.row, count, lane);
+    }
     if constexpr (BIAS) {
         // the ends' sums by wavefront, then the eight sums of a distance, then a bucket's distances, which lie side by side
         far = wave_sum(far);
@@ -529,6 +596,20 @@ template <typename T, int D, bool BIAS> __global__ __launch_bounds__(256, (2 - R
 }
 
 // ---------------------------------------------------------------- key and value gradients
+namespace {
+
+// Bias gradient: the items' sums of one bucket and head, by a wavefront
+template <typename T> __device__ __forceinline__ void reduce_bias(const RaggedArgs& a, int which, int lane) {
+    if (which >= a.buckets * a.heads) return;
+    const int b = which / a.heads, head = which % a.heads;
+    float v = 0.f;
+    for (int i = lane; i < a.bias_items; i += 64) v += a.part_bias[((int64_t)i * a.heads + head) * a.buckets + b];
+    v = wave_sum(v);
+    if (lane == 0) static_cast<T*>(a.d_bias)[which] = from_f32<T>(v);
+}
+
+}  // namespace
+
 // A workgroup takes 128 keys of a key head, 32 a wavefront (a lane being a key), and walks the query rows of all heads that share it.
 template <typename T, int D, bool SHAPED> __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(RaggedArgs a) {
     typedef Rows<T, D> R;
@@ -538,6 +619,10 @@ template <typename T, int D, bool SHAPED> __global__ __launch_bounds__(256, 1) v
     float* const w = stats + 4 * kRows;
     const int kv_heads = a.heads / a.share;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 31, h = lane >> 5;
+    if ((int)blockIdx.x >= a.n_items * kv_heads) {  // behind the keys' workgroups: the bias's gradient
+        if constexpr (SHAPED) reduce_bias<T>(a, (blockIdx.x - a.n_items * kv_heads) * 4 + wave, lane);
+        return;
+    }
     const RaggedItem it = a.items[blockIdx.x / kv_heads];
     const int kv_head = blockIdx.x % kv_heads, count = min(max(it.rows - 32 * wave, 0), 32), key0 = it.pos + 32 * wave;
     const int64_t k_row0 = it.k_row + 32 * wave;
@@ -669,24 +754,15 @@ template <typename T, int D, bool SHAPED> __global__ __launch_bounds__(256, 1) v
     store_tile<T, D>(dv, 1.f, scratch, a.dv.p + k_row0 * a.dv.row + kv_head * a.dv.head, a.dv.row, count, lane);
 }
 
-// ---------------------------------------------------------------- bias gradient: the items' sums of one bucket and head
-template <typename T> __global__ __launch_bounds__(64) void attn_dbias_kernel(RaggedArgs a, int items, T* d_bias) {
-    const int b = blockIdx.x, head = blockIdx.y;
-    float v = 0.f;
-    for (int i = threadIdx.x; i < items; i += 64) v += a.part_bias[((int64_t)i * a.heads + head) * a.buckets + b];
-    v = wave_sum(v);
-    if (threadIdx.x == 0) d_bias[(int64_t)b * a.heads + head] = from_f32<T>(v);
-}
-
 // ---------------------------------------------------------------- launches
 namespace {
 
 size_t bias_bytes(const RaggedArgs& a) { return (a.span + 2 * kMargin) * sizeof(float); }
 
-template <typename K> hipError_t launch(K kernel, DeviceOnce& once, int64_t blocks, int threads, size_t lds, const RaggedArgs& a, hipStream_t s) {
+template <typename K> hipError_t launch(K kernel, DeviceOnce& once, int64_t blocks, size_t lds, const RaggedArgs& a, hipStream_t s) {
     hipError_t e = once.run([&] { return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024 - 1024); });
     if (e != hipSuccess) return e;
-    kernel<<<dim3((unsigned)blocks), dim3(threads), lds, s>>>(a);
+    kernel<<<dim3((unsigned)blocks), dim3(256), lds, s>>>(a);
     return hipGetLastError();
 }
 // f(type, head size, bias)
@@ -701,16 +777,20 @@ template <typename F> hipError_t by_kind(int head_dim, bool bf16, bool bias, F f
 
 }  // namespace
 
-hipError_t launch_attn_forward(const RaggedArgs& a, int head_dim, bool bf16, bool few, int items, hipStream_t s) {
-    if (items == 0) return hipSuccess;
+hipError_t launch_attn_forward(const RaggedArgs& a, int head_dim, bool bf16, int tile_rows, hipStream_t s) {
+    if (a.n_items == 0) return hipSuccess;
     return by_kind(head_dim, bf16, a.bias != nullptr, [&](auto* t, auto d, auto bias) {
         typedef std::remove_pointer_t<decltype(t)> T;
         constexpr int D = decltype(d)::value;
         constexpr bool B = decltype(bias)::value;
-        static DeviceOnce once_few, once_many;
-        const size_t w = B ? bias_bytes(a) : 0;
-        if (few) return launch(attn_few_kernel<T, D, B>, once_few, (int64_t)items * a.heads, 256, 4 * 2 * 32 * Rows<T, D>::kPitch + w, a, s);
-        return launch(attn_forward_kernel<T, D, B>, once_many, (int64_t)items * a.heads, 256, 2 * Steps<T, D>::kBuf + w, a, s);
+        typedef Rows<T, D> R;
+        static DeviceOnce once_few, once_pair, once_many;
+        const int64_t blocks = (int64_t)a.n_items * a.heads;
+        const size_t w = B ? bias_bytes(a) : 0, lds = 2 * Steps<T, D, false>::kBuf + w;
+        if (tile_rows == kAttnFew) return launch(attn_few_kernel<T, D, B>, once_few, blocks, 4 * 2 * 32 * R::kPitch + w, a, s);
+        if constexpr (!R::kWide)
+            if (tile_rows == kAttnPair) return launch(attn_forward_kernel<T, D, B, true>, once_pair, blocks, lds, a, s);
+        return launch(attn_forward_kernel<T, D, B, false>, once_many, blocks, lds, a, s);
     });
 }
 
@@ -724,33 +804,31 @@ hipError_t launch_attn_join(const RaggedArgs& a, int head_dim, bool bf16, int ti
     });
 }
 
-hipError_t launch_attn_dq(const RaggedArgs& a, int head_dim, bool bf16, int items, hipStream_t s) {
-    if (items == 0) return hipSuccess;
+hipError_t launch_attn_dq(const RaggedArgs& a, int head_dim, bool bf16, int tile_rows, hipStream_t s) {
+    if (a.n_items == 0) return hipSuccess;
     return by_kind(head_dim, bf16, a.bias != nullptr, [&](auto* t, auto d, auto bias) {
         typedef std::remove_pointer_t<decltype(t)> T;
         constexpr int D = decltype(d)::value;
         constexpr bool B = decltype(bias)::value;
-        static DeviceOnce once;
-        return launch(attn_dq_kernel<T, D, B>, once, (int64_t)items * a.heads, 256, 2 * Steps<T, D>::kBuf + (B ? 9 * bias_bytes(a) : 0), a, s);
+        static DeviceOnce once_pair, once_many;
+        const int64_t blocks = (int64_t)a.n_items * a.heads;
+        const size_t lds = 2 * Steps<T, D, true>::kBuf + (B ? 9 * bias_bytes(a) : 0);
+        if constexpr (!Rows<T, D>::kWide)
+            if (tile_rows == kAttnPair) return launch(attn_dq_kernel<T, D, B, true>, once_pair, blocks, lds, a, s);
+        return launch(attn_dq_kernel<T, D, B, false>, once_many, blocks, lds, a, s);
     });
 }
 
-hipError_t launch_attn_dkv(const RaggedArgs& a, int head_dim, bool bf16, int items, hipStream_t s) {
-    if (items == 0) return hipSuccess;
-    return by_kind(head_dim, bf16, a.bias != nullptr || a.causal, [&](auto* t, auto d, auto bias) {
+hipError_t launch_attn_dkv(const RaggedArgs& a, int head_dim, bool bf16, hipStream_t s) {
+    const int64_t blocks = (int64_t)a.n_items * (a.heads / a.share) + (a.bias ? (a.buckets * a.heads + 3) / 4 : 0);
+    if (blocks == 0) return hipSuccess;
+    return by_kind(head_dim, bf16, a.bias != nullptr || a.causal, [&](auto* t, auto d, auto shaped) {
         typedef std::remove_pointer_t<decltype(t)> T;
         constexpr int D = decltype(d)::value;
-        constexpr bool B = decltype(bias)::value;
+        constexpr bool S = decltype(shaped)::value;
         static DeviceOnce once;
-        return launch(attn_dkv_kernel<T, D, B>, once, (int64_t)items * (a.heads / a.share), 256, 2 * Steps<T, D>::kBuf + 4 * Rows<T, D>::kStep * sizeof(float) + (B ? bias_bytes(a) : 0), a, s);
+        return launch(attn_dkv_kernel<T, D, S>, once, blocks, 2 * Steps<T, D, true>::kBuf + 4 * Rows<T, D>::kStep * sizeof(float) + (S ? bias_bytes(a) : 0), a, s);
     });
-}
-
-hipError_t launch_attn_dbias(const RaggedArgs& a, bool bf16, int items, void* d_bias, hipStream_t s) {
-    const dim3 grid(a.buckets, a.heads);
-    if (bf16) attn_dbias_kernel<bf16_t><<<grid, 64, 0, s>>>(a, items, static_cast<bf16_t*>(d_bias));
-    else attn_dbias_kernel<float><<<grid, 64, 0, s>>>(a, items, static_cast<float*>(d_bias));
-    return hipGetLastError();
 }
 
 }  // namespace aed

@@ -65,7 +65,7 @@ template <int D> struct AsRows<bf16_t, D> {
 #pragma unroll
         for (int s = 0; s < R::kSteps; ++s) c[s] = *reinterpret_cast<const bf16x8*>(rows + R::at(first + (lane & 31), 2 * s + (lane >> 5)));
     }
-    __device__ __forceinline__ void dot(f32x16& acc, const RowFrag<bf16_t, D>& f) const {
+    template <typename F> __device__ __forceinline__ void dot(f32x16& acc, const F& f) const {  // F: RowFrag, or rows of LDS too
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[i] = 0.f;
 #pragma unroll

@@ -103,23 +103,23 @@ template <typename T> __global__ __launch_bounds__(256) void preference_rows_ker
 // -log sigmoid(x)
 __device__ __forceinline__ float loss_of(float x) { return fmaxf(-x, 0.f) + log1pf(expf(-fabsf(x))); }
 
-// One workgroup: a wavefront adds up a pair's two sequences, then the pairs' losses are added.
+// One workgroup: sixteen lanes add up a sequence, 64 sequences at once, then the pairs' losses are added.
 __global__ __launch_bounds__(1024) void preference_pairs_kernel(PreferenceArgs a) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = threadIdx.x & 15;
     __shared__ float part[16];
     float mine = 0.f;
-    for (int p = wave; p < a.pairs; p += 16) {
-        float r[2];
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            float v = 0.f;
-            for (int i = a.seq_start[2 * p + s] + lane; i < a.seq_start[2 * p + s + 1]; i += 64) v += a.gain[i];
-            r[s] = wave_sum(v);
-        }
-        if (lane < 2) a.ratio[2 * p + lane] = lane ? r[1] : r[0];
-        const float x = a.beta * (r[0] - r[1]);
-        mine += (1.f - a.smoothing) * loss_of(x) + (a.smoothing > 0.f ? a.smoothing * loss_of(-x) : 0.f);
+    for (int s = threadIdx.x >> 4; s < 2 * a.pairs; s += 64) {  // both sequences of a pair are a wavefront's
+        const int first = a.seq_start[s], end = a.seq_start[s + 1];
+        float v = 0.f;
+#pragma unroll 8
+        for (int i = first + sub; i < end; i += 16) v += a.gain[i];
+        v = row16_sum(v);
+        if (sub == 0) a.ratio[s] = v;
+        const u32x2 both = swap16(v);  // of lanes l and l ^ 16: the preferred one and the other
+        const float x = a.beta * (bits_f32(both[0]) - bits_f32(both[1]));
+        if ((lane & 31) == 0) mine += (1.f - a.smoothing) * loss_of(x) + (a.smoothing > 0.f ? a.smoothing * loss_of(-x) : 0.f);
     }
+    mine = wave_sum(mine);
     if (lane == 0) part[wave] = mine;
     __syncthreads();
     if (threadIdx.x == 0) {
