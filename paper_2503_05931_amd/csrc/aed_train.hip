@@ -70,7 +70,7 @@ struct aed_attn {
     hipStream_t stream = nullptr;
     aed::AttnPlan plan;
     Arena arena;
-    size_t forward, joins, dq, dkv, bucket_of, bucket_range, part_o, part_ml, delta, part_bias;
+    size_t forward, joins, dq, dkv, zeros, bucket_of, bucket_range, part_o, part_ml, delta, part_bias;
     char* ws = nullptr;
     int64_t k_rows = 0;
     int span = 0;
@@ -112,14 +112,14 @@ aed_status check_attn(const aed_attn_config* c, const int32_t* q_lens, const int
     if (q_rows > kMost || k_rows > kMost) return fail(AED_EUNSUPPORTED, "more than 2^31 - 1 query rows or keys");
     if (c->n_heads > 65535) return fail(AED_EUNSUPPORTED, "more than 65535 heads");
     // a bound on the work items of any list, before any of them is made
-    const int64_t items = std::max(q_rows, k_rows) / aed::kAttnFew + batch + aed::kPlanSlots;
+    const int64_t items = std::max(q_rows, k_rows) / aed::kAttnFew + batch + aed::kPlanSlots;  // (one of few rows at the least)
     if (items * c->n_heads > kMost) return fail(AED_EUNSUPPORTED, "more than 2^31 - 1 workgroups");
     return AED_OK;
 }
 
 void lay_out(aed_attn& p, const int32_t* q_lens, const int32_t* k_lens, const int64_t* k_starts, int32_t batch) {
     const aed_attn_config& c = p.cfg;
-    p.plan = aed::plan_attention(q_lens, k_lens, k_starts, batch, c.n_heads, c.causal != 0, c.training != 0, aed::kAttnRows,
+    p.plan = aed::plan_attention(q_lens, k_lens, k_starts, batch, c.n_heads, c.n_kv_heads, c.causal != 0, c.training != 0, aed::kAttnRows,
                                  c.dtype == 0 && c.head_dim == 128 ? 0 : aed::kAttnPair, aed::kAttnFew);  // wide rows have no pairs
     p.k_rows = 0;
     for (int b = 0; b < batch; ++b) p.k_rows += k_lens[b];
@@ -127,6 +127,7 @@ void lay_out(aed_attn& p, const int32_t* q_lens, const int32_t* k_lens, const in
     p.joins = p.arena.table(p.plan.joins);
     p.dq = p.arena.table(p.plan.dq);
     p.dkv = p.arena.table(p.plan.dkv);
+    p.zeros = p.arena.table(std::vector<char>(512, 0));
     std::vector<uint8_t> of;
     std::vector<int2> range(c.bias_buckets, int2{0, 0});
     if (c.bias_buckets > 0) of = aed::bucket_places(c.bias_buckets, c.bias_max_distance, c.bias_bidirectional != 0);
@@ -184,6 +185,7 @@ aed_status common_args(const aed_attn* p, const aed_rows* q, const aed_rows* k, 
     a.lse = const_cast<float*>(lse);
     a.key_mask = key_mask;
     a.bias = bias;
+    a.zeros = p->ws + p->zeros;
     a.bucket_of = reinterpret_cast<const uint8_t*>(p->ws + p->bucket_of);
     a.bucket_range = reinterpret_cast<const int2*>(p->ws + p->bucket_range);
     a.delta = reinterpret_cast<float*>(p->ws + p->delta);
@@ -372,7 +374,7 @@ aed_status aed_attn_backward(aed_attn* p, const aed_rows* d_out, const aed_rows*
     hipError_t e = aed::launch_attn_dq(a, c.head_dim, bf16, p->plan.dq_rows, p->stream);
     a.items = items(p, p->dkv);
     a.n_items = (int)p->plan.dkv.size();
-    if (e == hipSuccess) e = aed::launch_attn_dkv(a, c.head_dim, bf16, p->stream);
+    if (e == hipSuccess) e = aed::launch_attn_dkv(a, c.head_dim, bf16, p->plan.dkv_keys, p->stream);
     return hip_status(e, "aed_attn_backward");
 }
 

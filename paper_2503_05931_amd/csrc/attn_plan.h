@@ -11,6 +11,7 @@ namespace aed {
 
 // Lists are made for the whole chip: two workgroups on each of 256 compute units.
 constexpr int kPlanSlots = 512;
+constexpr int kPlanPart = 512;  // keys of a part at the least
 
 // First distances of a side's logarithmic buckets, half + 1 on: the smallest n with (n / half)^(side - half) >= (max / half)^i.
 // The power is irrational but where it is a whole number, which rounding must not miss.
@@ -46,20 +47,29 @@ struct PlanJoin {
 };
 
 struct AttnPlan {
-    int tile_rows = 0, dq_rows = 0, n_parts = 0;  // query rows of an item, forward and backward
+    int tile_rows = 0, dq_rows = 0, dkv_keys = 0, n_parts = 0;  // query rows of an item, forward and backward; keys of one of key gradients
     std::vector<PlanItem> forward, dq, dkv;
     std::vector<PlanJoin> joins;
     int64_t q_rows = 0;
 };
 
-// tile_many, tile_pair, tile_few: query rows of an item (tile_many: keys of one of key gradients), by the longest sequence's
-inline AttnPlan plan_attention(const int32_t* q_lens, const int32_t* k_lens, const int64_t* k_starts, int batch, int heads, bool causal, bool training,
+// tile_many, tile_pair (0: there are none), tile_few: query rows of an item, tile_many and tile_pair also keys of one of key gradients
+inline AttnPlan plan_attention(const int32_t* q_lens, const int32_t* k_lens, const int64_t* k_starts, int batch, int heads, int kv_heads, bool causal, bool training,
                                int tile_many, int tile_pair, int tile_few) {
     AttnPlan p;
-    int most = 0;
+    int most = 0, most_keys = 0;
     for (int b = 0; b < batch; ++b) most = std::max(most, (int)q_lens[b]);
-    p.dq_rows = most <= tile_pair ? tile_pair : tile_many;
-    p.tile_rows = most <= tile_few ? tile_few : p.dq_rows;
+    // Items of half the rows, with two wavefronts to 32 of them, where no sequence has more or where whole ones leave compute units idle.
+    int64_t by_rows = 0, by_keys = 0;
+    for (int b = 0; b < batch; ++b) {
+        by_rows += (q_lens[b] + tile_many - 1) / tile_many;
+        by_keys += (k_lens[b] + tile_many - 1) / tile_many;
+        most_keys = std::max(most_keys, (int)k_lens[b]);
+    }
+    p.dq_rows = tile_pair && (most <= tile_pair || by_rows * heads < kPlanSlots / 2) ? tile_pair : tile_many;
+    p.dkv_keys = tile_pair && (most_keys <= tile_pair || by_keys * kv_heads < kPlanSlots / 2) ? tile_pair : tile_many;
+    // (forward, long keys are split instead: 14 tiles of rows against 2000 to 6000 keys take 79 us so, 89 us in items of half the rows)
+    p.tile_rows = most <= tile_few ? tile_few : most_keys < 2 * kPlanPart || most <= tile_pair ? p.dq_rows : tile_many;
     const int step = p.tile_rows == tile_few ? 128 : 64;  // keys that a workgroup takes at once
     std::vector<PlanItem> whole;
     int64_t q_row = 0, packed = 0, steps = 0;
@@ -76,9 +86,9 @@ inline AttnPlan plan_attention(const int32_t* q_lens, const int32_t* k_lens, con
         tiles(p.tile_rows, whole, b, k_row);
         if (training) {
             tiles(p.dq_rows, p.dq, b, k_row);
-            for (int k0 = 0; k0 < nk; k0 += tile_many) {
+            for (int k0 = 0; k0 < nk; k0 += p.dkv_keys) {
                 const int pos = k0 - (nk - nq);
-                p.dkv.push_back(PlanItem{k_row + k0, (int32_t)q_row, std::min(tile_many, nk - k0), pos, causal ? std::max(0, std::min(nq, pos)) : 0, nq, -1});
+                p.dkv.push_back(PlanItem{k_row + k0, (int32_t)q_row, std::min(p.dkv_keys, nk - k0), pos, causal ? std::max(0, std::min(nq, pos)) : 0, nq, -1});
             }
         }
         q_row += nq;
@@ -86,8 +96,9 @@ inline AttnPlan plan_attention(const int32_t* q_lens, const int32_t* k_lens, con
     }
     p.q_rows = q_row;
     for (const PlanItem& it : whole) steps += (it.k_end + step - 1) / step;
-    // Keys are split where an item would take much longer than its share of the chip, into parts of 512 keys and more.
-    const int64_t share = std::max<int64_t>(512 / step, (steps * heads + kPlanSlots - 1) / kPlanSlots);
+    // Keys are split where an item would take much longer than its share of the chip, into parts of kPlanPart keys and more: at
+    // 1.5 workgroups to a slot the parts of unlike rows even out.
+    const int64_t share = std::max<int64_t>(kPlanPart / step, (2 * steps * heads + 3 * kPlanSlots - 1) / (3 * kPlanSlots));
     for (const PlanItem& it : whole) {
         const int n = (it.k_end + step - 1) / step;
         if (n < 2 * share) {

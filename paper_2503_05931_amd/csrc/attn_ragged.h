@@ -28,6 +28,7 @@ struct RaggedArgs {
     AttnTensor q, k, v, o, d_o, dq, dk, dv;
     float* lse;              // [rows, heads]
     const uint8_t* key_mask;  // by key row; nullptr: all keys are seen
+    const char* zeros;       // 512 bytes
     const void* bias;        // [buckets, heads], in the tensors' type
     const uint8_t* bucket_of;  // [span], by key - query + max_distance
     const int2* bucket_range;  // [buckets]: first of a bucket's places with the margins on both sides, and one past its last
@@ -46,7 +47,7 @@ struct RaggedArgs {
 };
 
 constexpr int kAttnRows = 128;  // query rows of an item of many, keys of an item of key gradients
-constexpr int kAttnPair = 64;   // query rows of an item whose wavefronts share rows in pairs
+constexpr int kAttnPair = 64;   // the same where wavefronts share rows or keys in pairs
 constexpr int kAttnFew = 32;    // and of few (attn_few_kernel)
 constexpr int kAttnMargin = 72;  // places of the bias in LDS beyond both ends of its range
 constexpr int kAttnMaxPitch = 0x40000000 / 64 - 64;  // bytes between rows: 64 of them stay below 2^30, and twice that in 32 bits
@@ -56,6 +57,6 @@ hipError_t launch_attn_forward(const RaggedArgs& a, int head_dim, bool bf16, int
 hipError_t launch_attn_join(const RaggedArgs& a, int head_dim, bool bf16, int tile_rows, int joins, hipStream_t s);
 hipError_t launch_attn_dq(const RaggedArgs& a, int head_dim, bool bf16, int tile_rows, hipStream_t s);
 // and the bias's gradient from what dq's launch left
-hipError_t launch_attn_dkv(const RaggedArgs& a, int head_dim, bool bf16, hipStream_t s);
+hipError_t launch_attn_dkv(const RaggedArgs& a, int head_dim, bool bf16, int tile_keys, hipStream_t s);
 
 }  // namespace aed

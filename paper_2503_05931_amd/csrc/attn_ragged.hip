@@ -28,13 +28,26 @@ __device__ __forceinline__ float sum_halves(float v) {
 }
 __device__ __forceinline__ float base_of(float m) { return m == kNone ? 0.f : m; }
 
-// which of the 64 keys from `first` on are there and seen, one bit each
-__device__ __forceinline__ uint64_t seen_keys(const RaggedArgs& a, int64_t k_row, int first, int end, int lane) {
-    const int key = first + lane;
-    bool ok = key < end;
-    if (a.key_mask && ok) ok = load_global<uint8_t>(a.key_mask + k_row + key) != 0;
-    return __ballot(ok);
-}
+// Which of 64 keys are there and seen, a bit each.  A lane's byte of the mask is loaded a step before it is looked at: a wait for it would be
+// one for what was requested in between too.
+struct Seen {
+    const RaggedArgs& a;
+    const uint8_t* mask;  // of the lane's key among the first 64
+    int left;             // keys from the lane's on
+    uint8_t byte = 1;
+    __device__ __forceinline__ Seen(const RaggedArgs& a, const RaggedItem& it, int first, int lane)
+        : a(a), mask(a.key_mask + it.k_row + first + lane), left(it.k_end - first - lane) {
+        if (a.key_mask && left > 0) byte = load_global<uint8_t>(mask);
+    }
+    // the bits of 64 keys; those looked at next time begin `step` keys on
+    __device__ __forceinline__ uint64_t next(int step) {
+        const uint64_t bits = __ballot(left > 0 && byte != 0);
+        left -= step;
+        mask += step;
+        if (a.key_mask && left > 0) byte = load_global<uint8_t>(mask);
+        return bits;
+    }
+};
 // and by a query row at place `pos`
 __device__ __forceinline__ uint64_t seen_from(uint64_t seen, int first, int pos, int causal) {
     if (!causal) return seen;
@@ -145,7 +158,11 @@ __device__ __forceinline__ void finish_scores(f32x16& s, const RaggedArgs& a, fl
         uint32_t mine = seen >> (4 * h);
         rarely(mine);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = (mine >> (8 * (i >> 2) + (i & 3))) & 1 ? s[i] : kNone;
+        for (int i = 0; i < 16; ++i) {  // (a bit spread over 32, and a choice by bits: no condition codes)
+            const unsigned yes = (unsigned)__builtin_amdgcn_sbfe((int)mine, 8 * (i >> 2) + (i & 3), 1);
+            const float x = s[i];
+            s[i] = bits_f32((__builtin_bit_cast(unsigned, x) & yes) | (__builtin_bit_cast(unsigned, kNone) & ~yes));
+        }
     }
 }
 // exp of a score less `base`, both times log2 e
@@ -195,9 +212,8 @@ __device__ __forceinline__ int end_of(const RaggedArgs& a, const RaggedItem& it,
 }
 
 // A workgroup's walk over the keys, kStep of them a step: keys and values from memory to LDS (rows of keys, then of values), two
-// steps' worth: one is worked on while the other is on its way.  KEYS: keys that are not seen are cleared, not only their values (they
-// enter a product with weights of 0, and may be infinite).
-template <typename T, int D, bool KEYS> struct Steps {
+// steps' worth: one is worked on while the other is on its way.
+template <typename T, int D> struct Steps {
     typedef Rows<T, D> R;
     static constexpr int kBuf = 2 * R::kStep * R::kPitch;
     const RaggedArgs& a;
@@ -206,37 +222,31 @@ template <typename T, int D, bool KEYS> struct Steps {
     char* lds;
     int lane;
     RowFeed<T, D, R::kStep, 4> feed;
+    Seen bits;
     uint64_t seen = 0, seen_next = 0;  // of the step at hand and of the one on its way
     int buf = 1;
     __device__ __forceinline__ Steps(const RaggedArgs& a, const RaggedItem& it, int kv_head, char* lds, int wave, int lane)
         : a(a), it(it), kp(a.k.p + it.k_row * a.k.row + kv_head * a.k.head), vp(a.v.p + it.k_row * a.v.row + kv_head * a.v.head), lds(lds), lane(lane),
-          feed(lds, wave, lane) {}
+          feed(lds, wave, lane), bits(a, it, it.k_begin, lane) {}
     // requests the step of keys k0 on, into the buffer that is not at hand
     __device__ __forceinline__ void fetch(int k0) {
         if (k0 >= it.k_end) return;
         const int count = it.k_end - k0, to = (buf ^ 1) * kBuf;
-        feed.load(kp + k0 * a.k.row, (int)a.k.row, count, to);
-        feed.load(vp + k0 * a.v.row, (int)a.v.row, count, to + kBuf / 2);
-        seen_next = a.key_mask ? seen_keys(a, it.k_row, k0, it.k_end, lane) : count >= 64 ? ~0ull : (1ull << count) - 1;
+        seen_next = a.key_mask ? bits.next(R::kStep) : count >= 64 ? ~0ull : (1ull << count) - 1;
+        const char *ks = kp + k0 * a.k.row, *vs = vp + k0 * a.v.row;
+        if (a.key_mask && (seen_next & R::kAll) != R::kAll) {
+            feed.load_seen(ks, (int)a.k.row, seen_next, a.zeros, to);
+            feed.load_seen(vs, (int)a.v.row, seen_next, a.zeros, to + kBuf / 2);
+        } else {
+            feed.load(ks, (int)a.k.row, count, to);
+            feed.load(vs, (int)a.v.row, count, to + kBuf / 2);
+        }
     }
     // everyone is done with the step at hand; the one on its way is at hand
     __device__ __forceinline__ void next() {
         loads_done_barrier();
         buf ^= 1;
         seen = seen_next;
-        if (a.key_mask && (seen & R::kAll) != R::kAll) {
-            constexpr int kThreads = 256 / R::kStep, kEach = R::kPitch / kThreads;  // of a row, and their bytes
-            const int row = threadIdx.x / kThreads;
-            if (!((seen >> row) & 1)) {
-                char* const p = lds + buf * kBuf + row * R::kPitch + threadIdx.x % kThreads * kEach;
-#pragma unroll
-                for (int i = 0; i < kEach; i += 16) {
-                    if constexpr (KEYS) *reinterpret_cast<typename R::chunk_t*>(p + i) = (typename R::chunk_t)(0);
-                    *reinterpret_cast<typename R::chunk_t*>(p + kBuf / 2 + i) = (typename R::chunk_t)(0);
-                }
-            }
-            lds_barrier();
-        }
     }
     __device__ __forceinline__ const char* keys() const { return lds + buf * kBuf; }
     __device__ __forceinline__ const char* values() const { return lds + buf * kBuf + kBuf / 2; }
@@ -253,12 +263,12 @@ template <typename T, int D, bool BIAS, bool PAIR> __global__ __launch_bounds__(
     constexpr int kJoin = 2 * 64 * R::kTiles * 64 + 1024;  // two wavefronts' sums, and their maxima
     constexpr int kSub = PAIR ? 1 : R::kStep / 32;  // 32-key tiles of a step
     static_assert(!PAIR || R::kStep == 64, "a tile for each of two");
-    float* const w = reinterpret_cast<float*>(lds + 2 * Steps<T, D, false>::kBuf);
+    float* const w = reinterpret_cast<float*>(lds + 2 * Steps<T, D>::kBuf);
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 31, h = lane >> 5;
     const RaggedItem it = a.items[blockIdx.x / a.heads];
     const int group = PAIR ? wave & 1 : wave, tile = PAIR ? wave >> 1 : 0;  // which rows, which keys of a step
     const int head = blockIdx.x % a.heads, row0 = it.q_row + 32 * group, count = min(max(it.rows - 32 * group, 0), 32), pos = it.pos + 32 * group;
-    Steps<T, D, false> step(a, it, head / a.share, lds, wave, lane);
+    Steps<T, D> step(a, it, head / a.share, lds, wave, lane);
     step.fetch(it.k_begin);
     RowFrag<T, D> q;
     q.load(a.q.p + (int64_t)(row0 + r) * a.q.row + head * a.q.head, r < count, h);
@@ -367,8 +377,9 @@ template <typename T, int D, bool BIAS> __global__ __launch_bounds__(256, (2 - R
     char* const vb = kb + kMine / 2;
     RowStage<T, D, 32, 64> ks, vs;
     uint64_t seen = 0;
+    Seen bits(a, it, it.k_begin + 32 * wave, lane);
     auto fetch = [&](int k0) {
-        seen = seen_keys(a, it.k_row, k0, it.k_end, lane);
+        seen = bits.next(128);
         ks.template load<true>(kp + k0 * a.k.row, (int)a.k.row, it.k_end - k0, seen, lane);
         vs.template load<true>(vp + k0 * a.v.row, (int)a.v.row, it.k_end - k0, seen, lane);
     };
@@ -473,7 +484,7 @@ template <typename T, int D, bool BIAS, bool PAIR> __global__ __launch_bounds__(
     extern __shared__ __align__(16) char lds[];
     constexpr int kJoin = 2 * 64 * R::kTiles * 64 + 512;  // two wavefronts' sums, and of their rows' delta
     static_assert(!PAIR || R::kStep == 64, "a tile for each of two");
-    float* const w = reinterpret_cast<float*>(lds + 2 * Steps<T, D, true>::kBuf);
+    float* const w = reinterpret_cast<float*>(lds + 2 * Steps<T, D>::kBuf);
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 31, h = lane >> 5;
     const int places = bias_places(a);
     float* const sums = w + places;  // [wavefront, half][places]
@@ -481,7 +492,7 @@ template <typename T, int D, bool BIAS, bool PAIR> __global__ __launch_bounds__(
     const RaggedItem it = a.items[item];
     const int group = PAIR ? wave & 1 : wave, tile = PAIR ? wave >> 1 : 0;  // which rows, which keys of a step
     const int head = blockIdx.x % a.heads, row0 = it.q_row + 32 * group, count = min(max(it.rows - 32 * group, 0), 32), pos = it.pos + 32 * group;
-    Steps<T, D, true> step(a, it, head / a.share, lds, wave, lane);
+    Steps<T, D> step(a, it, head / a.share, lds, wave, lane);
     step.fetch(it.k_begin);
     const bool live = r < count;
     RowFrag<T, D> q, d_o;
@@ -611,9 +622,11 @@ template <typename T> __device__ __forceinline__ void reduce_bias(const RaggedAr
 }  // namespace
 
 // A workgroup takes 128 keys of a key head, 32 a wavefront (a lane being a key), and walks the query rows of all heads that share it.
-template <typename T, int D, bool SHAPED> __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(RaggedArgs a) {
+// PAIR: it takes 64 keys, and two wavefronts share 32 of them, each with 32 rows of a step.
+template <typename T, int D, bool SHAPED, bool PAIR> __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(RaggedArgs a) {
     typedef Rows<T, D> R;
-    constexpr int kRows = R::kStep, kBuf = 2 * kRows * R::kPitch;
+    constexpr int kRows = R::kStep, kBuf = 2 * kRows * R::kPitch, kTilesOf = PAIR ? 1 : kRows / 32;  // 32-row tiles of a step for a wavefront
+    static_assert(!PAIR || kRows == 64, "a tile for each of two");
     extern __shared__ __align__(16) char lds[];
     float* const stats = reinterpret_cast<float*>(lds + 2 * kBuf);  // two buffers of [kRows] lse (times log2 e), [kRows] delta
     float* const w = stats + 4 * kRows;
@@ -624,8 +637,9 @@ template <typename T, int D, bool SHAPED> __global__ __launch_bounds__(256, 1) v
         return;
     }
     const RaggedItem it = a.items[blockIdx.x / kv_heads];
-    const int kv_head = blockIdx.x % kv_heads, count = min(max(it.rows - 32 * wave, 0), 32), key0 = it.pos + 32 * wave;
-    const int64_t k_row0 = it.k_row + 32 * wave;
+    const int kv_head = blockIdx.x % kv_heads, group = PAIR ? wave & 1 : wave, half = PAIR ? wave >> 1 : 0;  // which keys, which rows of a step
+    const int count = min(max(it.rows - 32 * group, 0), 32), key0 = it.pos + 32 * group;
+    const int64_t k_row0 = it.k_row + 32 * group;
     const RowFeed<T, D, kRows, 4> feed(lds, wave, lane);
     int head = kv_head * a.share, buf = 1;
     float stat = 0.f;
@@ -680,7 +694,7 @@ template <typename T, int D, bool SHAPED> __global__ __launch_bounds__(256, 1) v
                 }
                 continue;
             }
-            constexpr int kPer = RowFeed<T, D, kRows, 4>::kEach * 2 / (kRows / 32) / 2;  // requests of each of the two tensors in a tile of rows
+            constexpr int kPer = RowFeed<T, D, kRows, 4>::kEach / kTilesOf;  // requests of each of the two tensors in a tile of rows
             auto ask_q = [&](int u) {
                 if (more)
 #pragma unroll
@@ -697,25 +711,25 @@ template <typename T, int D, bool SHAPED> __global__ __launch_bounds__(256, 1) v
             const float* const row_delta = row_lse + kRows;
             // each product's fragments are requested one product ahead
             AsRows<T, D> qr;
-            qr.load(qs, 0, lane);
+            qr.load(qs, 32 * half, lane);
 #pragma unroll
-            for (int u = 0; u < kRows / 32; ++u) {
-                const int first = q0 + 32 * u;
+            for (int u = 0; u < kTilesOf; ++u) {
+                const int row = 32 * (half + u), first = q0 + row;
                 f32x16 p, ds;
                 f32x4 lse[4], delta[4];
                 AsRows<T, D> gr;
                 AsColumns<T, D> gc, qc;
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    lse[g] = *reinterpret_cast<const f32x4*>(row_lse + 32 * u + 8 * g + 4 * h);
-                    delta[g] = *reinterpret_cast<const f32x4*>(row_delta + 32 * u + 8 * g + 4 * h);
+                    lse[g] = *reinterpret_cast<const f32x4*>(row_lse + row + 8 * g + 4 * h);
+                    delta[g] = *reinterpret_cast<const f32x4*>(row_delta + row + 8 * g + 4 * h);
                 }
-                gr.load(gs, 32 * u, lane);
+                gr.load(gs, row, lane);
                 phase();
                 qr.dot(p, k);
                 phase();
                 ask_q(u);
-                gc.load(gs, 32 * u, lane);
+                gc.load(gs, row, lane);
                 phase();
                 if constexpr (SHAPED) {
 #pragma unroll
@@ -732,13 +746,13 @@ template <typename T, int D, bool SHAPED> __global__ __launch_bounds__(256, 1) v
                 for (int i = 0; i < 16; ++i) p[i] = weight_of<SHAPED>(p[i], scale2, lse[i >> 2][i & 3]);
                 woven<0, 6>();
                 ask_g(u);
-                qc.load(qs, 32 * u, lane);
+                qc.load(qs, row, lane);
                 phase();
                 gc.add(dv, p);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) ds[i] = p[i] * (ds[i] - delta[i >> 2][i & 3]);
                 woven<4, 7>();
-                if (u + 1 < kRows / 32) qr.load(qs, 32 * (u + 1), lane);
+                if (u + 1 < kTilesOf) qr.load(qs, row + 32, lane);
                 phase();
                 qc.add(dk, ds);
             }
@@ -750,8 +764,38 @@ template <typename T, int D, bool SHAPED> __global__ __launch_bounds__(256, 1) v
         clear<R::kTiles>(dv);
     }
     char* const scratch = lds + wave * 32 * R::kPitch;
-    store_tile<T, D>(dk, a.scale, scratch, a.dk.p + k_row0 * a.dk.row + kv_head * a.dk.head, a.dk.row, count, lane);
-    store_tile<T, D>(dv, 1.f, scratch, a.dv.p + k_row0 * a.dv.row + kv_head * a.dv.head, a.dv.row, count, lane);
+    auto put_dk = [&] { store_tile<T, D>(dk, a.scale, scratch, a.dk.p + k_row0 * a.dk.row + kv_head * a.dk.head, a.dk.row, count, lane); };
+    auto put_dv = [&] { store_tile<T, D>(dv, 1.f, scratch, a.dv.p + k_row0 * a.dv.row + kv_head * a.dv.head, a.dv.row, count, lane); };
+    if constexpr (!PAIR) {
+        put_dk();
+        put_dv();
+    } else {  // of two wavefronts with the same keys the first takes the other's dK and gives it its dV
+        auto at = [&](int of, int t, int g) { return reinterpret_cast<f32x4*>(lds) + (t * 4 + g) * 256 + of * 64 + lane; };
+        auto give = [&](const f32x16* x) {
+#pragma unroll
+            for (int t = 0; t < R::kTiles; ++t)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) *at(wave, t, g) = f32x4{x[t][4 * g], x[t][4 * g + 1], x[t][4 * g + 2], x[t][4 * g + 3]};
+        };
+        auto take = [&](f32x16* x) {
+#pragma unroll
+            for (int t = 0; t < R::kTiles; ++t)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const f32x4 v = *at(wave ^ 2, t, g);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[t][4 * g + e] += v[e];
+                }
+        };
+        if (half) give(dk);
+        else give(dv);
+        lds_barrier();
+        if (half) take(dv);
+        else take(dk);
+        lds_barrier();
+        if (half) put_dv();
+        else put_dk();
+    }
 }
 
 // ---------------------------------------------------------------- launches
@@ -786,7 +830,7 @@ hipError_t launch_attn_forward(const RaggedArgs& a, int head_dim, bool bf16, int
         typedef Rows<T, D> R;
         static DeviceOnce once_few, once_pair, once_many;
         const int64_t blocks = (int64_t)a.n_items * a.heads;
-        const size_t w = B ? bias_bytes(a) : 0, lds = 2 * Steps<T, D, false>::kBuf + w;
+        const size_t w = B ? bias_bytes(a) : 0, lds = 2 * Steps<T, D>::kBuf + w;
         if (tile_rows == kAttnFew) return launch(attn_few_kernel<T, D, B>, once_few, blocks, 4 * 2 * 32 * R::kPitch + w, a, s);
         if constexpr (!R::kWide)
             if (tile_rows == kAttnPair) return launch(attn_forward_kernel<T, D, B, true>, once_pair, blocks, lds, a, s);
@@ -812,22 +856,25 @@ hipError_t launch_attn_dq(const RaggedArgs& a, int head_dim, bool bf16, int tile
         constexpr bool B = decltype(bias)::value;
         static DeviceOnce once_pair, once_many;
         const int64_t blocks = (int64_t)a.n_items * a.heads;
-        const size_t lds = 2 * Steps<T, D, true>::kBuf + (B ? 9 * bias_bytes(a) : 0);
+        const size_t lds = 2 * Steps<T, D>::kBuf + (B ? 9 * bias_bytes(a) : 0);
         if constexpr (!Rows<T, D>::kWide)
             if (tile_rows == kAttnPair) return launch(attn_dq_kernel<T, D, B, true>, once_pair, blocks, lds, a, s);
         return launch(attn_dq_kernel<T, D, B, false>, once_many, blocks, lds, a, s);
     });
 }
 
-hipError_t launch_attn_dkv(const RaggedArgs& a, int head_dim, bool bf16, hipStream_t s) {
+hipError_t launch_attn_dkv(const RaggedArgs& a, int head_dim, bool bf16, int tile_keys, hipStream_t s) {
     const int64_t blocks = (int64_t)a.n_items * (a.heads / a.share) + (a.bias ? (a.buckets * a.heads + 3) / 4 : 0);
     if (blocks == 0) return hipSuccess;
     return by_kind(head_dim, bf16, a.bias != nullptr || a.causal, [&](auto* t, auto d, auto shaped) {
         typedef std::remove_pointer_t<decltype(t)> T;
         constexpr int D = decltype(d)::value;
         constexpr bool S = decltype(shaped)::value;
-        static DeviceOnce once;
-        return launch(attn_dkv_kernel<T, D, S>, once, blocks, 2 * Steps<T, D, true>::kBuf + 4 * Rows<T, D>::kStep * sizeof(float) + (S ? bias_bytes(a) : 0), a, s);
+        static DeviceOnce once_pair, once_many;
+        const size_t lds = 2 * Steps<T, D>::kBuf + 4 * Rows<T, D>::kStep * sizeof(float) + (S ? bias_bytes(a) : 0);
+        if constexpr (!Rows<T, D>::kWide)
+            if (tile_keys == kAttnPair) return launch(attn_dkv_kernel<T, D, S, true>, once_pair, blocks, lds, a, s);
+        return launch(attn_dkv_kernel<T, D, S, false>, once_many, blocks, lds, a, s);
     });
 }
 

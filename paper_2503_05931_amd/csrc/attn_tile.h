@@ -166,6 +166,9 @@ template <typename T, int D, int N, int THREADS> struct RowStage {
 __device__ __forceinline__ void load_to_lds16(const char* base, int off, unsigned lds_base) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n" ::"s"(lds_base), "v"(off), "s"(base) : "memory");
 }
+__device__ __forceinline__ void load_to_lds16(const char* p, unsigned lds_base) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n" ::"s"(lds_base), "v"(p) : "memory");
+}
 // This wavefront's loads have arrived and its LDS accesses are done, then the barrier.  The wait is the builtin: the compiler, which keeps
 // count of its own loads, knows that none is left, and does not wait for them (and with them for requests to LDS) in the loop that follows.
 __device__ __forceinline__ void loads_done_barrier() {
@@ -191,6 +194,14 @@ template <typename T, int D, int N, int W> struct RowFeed {
     // the i-th of a wavefront's kEach requests
     __device__ __forceinline__ void one(int i, const char* first, int pitch, int count, int lds_offset) const {
         load_to_lds16(first, min(row + i * W * kAtOnce, count - 1) * pitch + chunk, lds0 + lds_offset + i * W * 1024);
+    }
+    // rows whose bit is not set come from `zeros` (kPitch bytes): what stands in their place may be infinite
+    __device__ __forceinline__ void load_seen(const char* first, int pitch, uint64_t seen, const char* zeros, int lds_offset) const {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int n = row + i * W * kAtOnce;
+            load_to_lds16(((seen >> n) & 1 ? first + (int64_t)n * pitch : zeros) + chunk, lds0 + lds_offset + i * W * 1024);
+        }
     }
     __device__ __forceinline__ void load(const char* first, int pitch, int count, int lds_offset) const {
         if (count >= N) {

@@ -97,6 +97,7 @@ class _Plan:
         with torch.cuda.device(self.device):
             if self.stream is None:
                 self.stream = torch.cuda.current_stream(self.device)
+            self.raw, self.index, self._raw_stream = self.stream.cuda_stream, self.device.index, torch._C._cuda_getCurrentRawStream
             self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
             self._enter()
             _check(create(C.c_void_p(self.workspace.data_ptr()), C.c_void_p(self.stream.cuda_stream), C.byref(self.handle)))
@@ -117,17 +118,18 @@ class _Plan:
     def _enter(self):
         if not self.handle and self._destroy:
             raise _b.AedError(_b.AED_ESTATE, "the plan is closed")
+        if self._raw_stream(self.index) == self.raw:
+            return None
         current = self.torch.cuda.current_stream(self.device)
-        if current != self.stream:
-            self.stream.wait_stream(current)
-            return current
-        return None
+        self.stream.wait_stream(current)
+        return current
 
     def _exit(self, current):
-        if current is not None:
-            current.wait_stream(self.stream)
+        current.wait_stream(self.stream)
 
     def _given(self, t, name, dtype, shape):
+        if t.dtype is dtype and t.shape == shape and t.get_device() == self.index:
+            return t
         if t.dtype != dtype:
             _refuse(f"{name} is {t.dtype}, the plan's is {dtype}")
         if t.device != self.device:
@@ -170,18 +172,24 @@ class Attention(_Plan):
         # rows that the keys' tensors need; packed keys have no others
         self.k_rows = int(kl.sum(dtype=np.int64)) if starts is None else int(np.max(np.where(kl > 0, starts + kl, 0)))
         self.packed = starts is None
+        self._q_shape, self._k_shape, self._lse_shape = (self.q_rows, n_heads, head_dim), (self.k_rows, kv, head_dim), (self.q_rows, n_heads)
+        # arguments of a call: q, k, v, what is returned for the queries, out, d_out, dk, dv
+        self._at = [AedRows() for _ in range(8)]
+        for i, h in ((3, n_heads), (6, kv), (7, kv)):
+            self._at[i].row_stride, self._at[i].head_stride = h * head_dim, head_dim
         self._start(n.value, lambda ws, st, h: self.lib.aed_attn_create(C.byref(self.cfg), pq, pk, ps, len(ql), ws, n.value, st, h),
                     self.lib.aed_attn_destroy)
 
-    def _rows(self, t, name, heads, rows):
-        c = self.cfg
-        self._given(t, name, self.dtype, (None, heads, c.head_dim))
-        if t.shape[0] < rows or (t.shape[0] != rows and (self.packed or heads == c.n_heads and name not in ("k", "v"))):
-            _refuse(f"{name} has {t.shape[0]} rows, expected {rows}")
-        s = t.stride()
-        if s[2] != 1:
+    def _rows(self, to, t, name, heads, rows):
+        shape, (s0, s1, s2) = t.shape, t.stride() if t.dim() == 3 else (0, 0, 0)
+        if (s2 != 1 or t.dtype is not self.dtype or shape[1] != heads or shape[2] != self.cfg.head_dim or t.get_device() != self.index
+                or shape[0] != rows and (shape[0] < rows or self.packed or name not in ("k", "v"))):
+            self._given(t, name, self.dtype, (None, heads, self.cfg.head_dim))
+            if shape[0] != rows:
+                _refuse(f"{name} has {shape[0]} rows, expected {rows}")
             _refuse(f"{name}: the last dimension is not contiguous")
-        return AedRows(t.data_ptr(), s[0], s[1])
+        to.data, to.row_stride, to.head_stride = t.data_ptr(), s0, s1
+        return to
 
     def _side(self, bias, key_mask, k_rows):
         """Pointers of the bias and the mask."""
@@ -200,33 +208,46 @@ class Attention(_Plan):
     def aed_attn_forward(self, q, k, v, bias=None, key_mask=None):
         """Returns (out [query rows, n_heads, head_dim], lse float32 [query rows, n_heads])."""
         torch, c = self.torch, self.cfg
-        rq, rk, rv = (self._rows(q, "q", c.n_heads, self.q_rows), self._rows(k, "k", c.n_kv_heads, self.k_rows),
-                      self._rows(v, "v", c.n_kv_heads, self.k_rows))
-        pb, pm = self._side(bias, key_mask, k.shape[0])
-        out = torch.empty((self.q_rows, c.n_heads, c.head_dim), dtype=self.dtype, device=self.device)
-        lse = torch.empty((self.q_rows, c.n_heads), dtype=torch.float32, device=self.device)
-        ro = AedRows(out.data_ptr(), c.n_heads * c.head_dim, c.head_dim)
+        at, H, G = self._at, c.n_heads, c.n_kv_heads
+        self._rows(at[0], q, "q", H, self.q_rows)
+        self._rows(at[1], k, "k", G, self.k_rows)
+        self._rows(at[2], v, "v", G, self.k_rows)
+        pb, pm = self._side(bias, key_mask, k.shape[0]) if bias is not None or key_mask is not None else (None, None)
+        out = torch.empty(self._q_shape, dtype=self.dtype, device=self.device)
+        lse = torch.empty(self._lse_shape, dtype=torch.float32, device=self.device)
+        at[3].data = out.data_ptr()
         current = self._enter()
-        _check(self.lib.aed_attn_forward(self.handle, rq, rk, rv, pb, pm, ro, lse.data_ptr()))
-        self._exit(current)
+        status = self.lib.aed_attn_forward(self.handle, at[0], at[1], at[2], pb, pm, at[3], lse.data_ptr())
+        if status:
+            _check(status)
+        if current is not None:
+            self._exit(current)
         return out, lse
 
     def aed_attn_backward(self, d_out, q, k, v, out, lse, bias=None, key_mask=None):
         """Returns (dq, dk, dv, d_bias or None) in the shapes of q, k, v and bias."""
         torch, c = self.torch, self.cfg
-        H, G, D = c.n_heads, c.n_kv_heads, c.head_dim
-        given = [self._rows(d_out, "d_out", H, self.q_rows), self._rows(q, "q", H, self.q_rows), self._rows(k, "k", G, self.k_rows),
-                 self._rows(v, "v", G, self.k_rows), self._rows(out, "out", H, self.q_rows)]
-        plse = self._flat(lse, "lse", torch.float32, (self.q_rows, H))
-        pb, pm = self._side(bias, key_mask, k.shape[0])
-        dq = torch.empty((self.q_rows, H, D), dtype=self.dtype, device=self.device)
-        dk, dv = (torch.empty((self.k_rows, G, D), dtype=self.dtype, device=self.device) for _ in range(2))
-        d_bias = torch.empty_like(bias) if bias is not None else None
+        H, G = c.n_heads, c.n_kv_heads
+        at = self._at
+        self._rows(at[0], q, "q", H, self.q_rows)
+        self._rows(at[1], k, "k", G, self.k_rows)
+        self._rows(at[2], v, "v", G, self.k_rows)
+        self._rows(at[4], out, "out", H, self.q_rows)
+        self._rows(at[5], d_out, "d_out", H, self.q_rows)
+        plse = self._flat(lse, "lse", torch.float32, self._lse_shape)
+        pb, pm = self._side(bias, key_mask, k.shape[0]) if bias is not None or key_mask is not None else (None, None)
+        dq = torch.empty(self._q_shape, dtype=self.dtype, device=self.device)
+        dk = torch.empty(self._k_shape, dtype=self.dtype, device=self.device)
+        dv = torch.empty(self._k_shape, dtype=self.dtype, device=self.device)
+        d_bias = None if bias is None else torch.empty_like(bias)
+        at[3].data, at[6].data, at[7].data = dq.data_ptr(), dk.data_ptr(), dv.data_ptr()
         current = self._enter()
-        _check(self.lib.aed_attn_backward(self.handle, *given, plse, pb, pm, AedRows(dq.data_ptr(), H * D, D),
-                                          AedRows(dk.data_ptr(), G * D, D), AedRows(dv.data_ptr(), G * D, D),
-                                          None if d_bias is None else d_bias.data_ptr()))
-        self._exit(current)
+        status = self.lib.aed_attn_backward(self.handle, at[5], at[0], at[1], at[2], at[4], plse, pb, pm, at[3], at[6], at[7],
+                                            None if d_bias is None else d_bias.data_ptr())
+        if status:
+            _check(status)
+        if current is not None:
+            self._exit(current)
         return dq, dk, dv, d_bias
 
     def attend(self, q, k, v, bias=None, key_mask=None):
@@ -266,8 +287,11 @@ class Preference(_Plan):
         ratio = torch.empty(2 * self.pairs, dtype=torch.float32, device=self.device)
         lse = torch.empty((self.rows, 2), dtype=torch.float32, device=self.device)
         current = self._enter()
-        _check(self.lib.aed_preference_forward(self.handle, pz, stride, py, pr, loss.data_ptr(), ratio.data_ptr(), lse.data_ptr()))
-        self._exit(current)
+        status = self.lib.aed_preference_forward(self.handle, pz, stride, py, pr, loss.data_ptr(), ratio.data_ptr(), lse.data_ptr())
+        if status:
+            _check(status)
+        if current is not None:
+            self._exit(current)
         return loss, ratio, lse
 
     def aed_preference_backward(self, logits, labels, ratio, lse, d_loss=None, d_logits=None):
@@ -281,8 +305,11 @@ class Preference(_Plan):
             d_logits = torch.empty((self.rows, self.cfg.vocab), dtype=self.dtype, device=self.device)
         pg, g_stride = self._logits(d_logits, "d_logits")
         current = self._enter()
-        _check(self.lib.aed_preference_backward(self.handle, pz, stride, py, pr, pl, pd, pg, g_stride))
-        self._exit(current)
+        status = self.lib.aed_preference_backward(self.handle, pz, stride, py, pr, pl, pd, pg, g_stride)
+        if status:
+            _check(status)
+        if current is not None:
+            self._exit(current)
         return d_logits
 
     def loss(self, logits, labels, ref_logp):
