@@ -132,12 +132,13 @@ __device__ __forceinline__ void add_distances(const f32x16& ds, const RaggedArgs
 __device__ __forceinline__ void phase() { __builtin_amdgcn_sched_barrier(0); }
 
 // ends a phase of eight 32 x 32 products among which the vector instructions are dealt out
-template <int FIRST, int EACH> __device__ __forceinline__ void woven() {
+template <int FIRST, int READS, int EACH> __device__ __forceinline__ void woven() {
     if constexpr (FIRST > 0) __builtin_amdgcn_sched_group_barrier(0x2, FIRST, 0);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);  // a product
-        __builtin_amdgcn_sched_group_barrier(0x2, EACH, 0);  // vector instructions
+        if constexpr (READS > 0) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);  // reads of LDS
+        if constexpr (EACH > 0) __builtin_amdgcn_sched_group_barrier(0x2, EACH, 0);  // vector instructions
     }
     phase();
 }
@@ -683,27 +684,25 @@ template <typename T, int D, bool SHAPED, bool PAIR> __global__ __launch_bounds_
             if (next_q >= it.k_end) next_q = it.k_begin, ++next_head;
             const bool more = next_head < (kv_head + 1) * a.share;
             const int next_n = it.k_end - next_q, to = (buf ^ 1) * kBuf;
-            const char* const next_qs = a.q.p + (int64_t)(it.q_row + next_q) * a.q.row + next_head * a.q.head;
-            const char* const next_gs = a.d_o.p + (int64_t)(it.q_row + next_q) * a.d_o.row + next_head * a.d_o.head;
+            // after the last step zeros are requested: a branch less among the products
+            const char* const next_qs = more ? a.q.p + (int64_t)(it.q_row + next_q) * a.q.row + next_head * a.q.head : a.zeros;
+            const char* const next_gs = more ? a.d_o.p + (int64_t)(it.q_row + next_q) * a.d_o.row + next_head * a.d_o.head : a.zeros;
+            const int q_pitch = more ? (int)a.q.row : 0, g_pitch = more ? (int)a.d_o.row : 0;
             if (more) fetch_stats(next_head, next_q);
             // key0 counts in query rows: row i sees the keys up to its own place
             if (count == 0 || (a.causal && q0 + kRows <= key0)) {
-                if (more) {
-                    feed.load(next_qs, (int)a.q.row, next_n, to);
-                    feed.load(next_gs, (int)a.d_o.row, next_n, to + kBuf / 2);
-                }
+                feed.load(next_qs, q_pitch, next_n, to);
+                feed.load(next_gs, g_pitch, next_n, to + kBuf / 2);
                 continue;
             }
             constexpr int kPer = RowFeed<T, D, kRows, 4>::kEach / kTilesOf;  // requests of each of the two tensors in a tile of rows
             auto ask_q = [&](int u) {
-                if (more)
 #pragma unroll
-                    for (int i = 0; i < kPer; ++i) feed.one(u * kPer + i, next_qs, (int)a.q.row, next_n, to);
+                for (int i = 0; i < kPer; ++i) feed.one(u * kPer + i, next_qs, q_pitch, next_n, to);
             };
             auto ask_g = [&](int u) {
-                if (more)
 #pragma unroll
-                    for (int i = 0; i < kPer; ++i) feed.one(u * kPer + i, next_gs, (int)a.d_o.row, next_n, to + kBuf / 2);
+                for (int i = 0; i < kPer; ++i) feed.one(u * kPer + i, next_gs, g_pitch, next_n, to + kBuf / 2);
             };
             const char* const qs = lds + buf * kBuf;
             const char* const gs = qs + kBuf / 2;
@@ -724,13 +723,12 @@ template <typename T, int D, bool SHAPED, bool PAIR> __global__ __launch_bounds_
                     lse[g] = *reinterpret_cast<const f32x4*>(row_lse + row + 8 * g + 4 * h);
                     delta[g] = *reinterpret_cast<const f32x4*>(row_delta + row + 8 * g + 4 * h);
                 }
+                phase();
                 gr.load(gs, row, lane);
-                phase();
                 qr.dot(p, k);
-                phase();
+                woven<0, 1, 0>();
                 ask_q(u);
                 gc.load(gs, row, lane);
-                phase();
                 if constexpr (SHAPED) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) p[i] *= scale2;
@@ -744,21 +742,20 @@ template <typename T, int D, bool SHAPED, bool PAIR> __global__ __launch_bounds_
                 gr.dot(ds, v);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) p[i] = weight_of<SHAPED>(p[i], scale2, lse[i >> 2][i & 3]);
-                woven<0, 6>();
+                woven<0, 2, 6>();
                 ask_g(u);
                 qc.load(qs, row, lane);
-                phase();
                 gc.add(dv, p);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) ds[i] = p[i] * (ds[i] - delta[i >> 2][i & 3]);
-                woven<4, 7>();
+                woven<4, 2, 7>();
                 if (u + 1 < kTilesOf) qr.load(qs, row + 32, lane);
-                phase();
                 qc.add(dk, ds);
+                woven<4, 1, 1>();
             }
         }
     }
-    lds_barrier();
+    loads_done_barrier();
     if (!live) {  // its weights were those of a key of zeros
         clear<R::kTiles>(dk);
         clear<R::kTiles>(dv);
