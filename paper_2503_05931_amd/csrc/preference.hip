@@ -163,17 +163,25 @@ template <typename T> __global__ __launch_bounds__(256) void preference_gradient
         return;
     }
     const bool same = ((uintptr_t)(z + part.head) & 15) == 0;  // logits and gradients lie alike to 16 bytes
-    for (int v = lane; v < part.vecs; v += 64) {
-        const int first = part.head + v * N;
-        V x, y;
-        if (same) x = *reinterpret_cast<const V*>(z + first);
-        else {
+    for (int v0 = lane; v0 < part.vecs; v0 += 64 * kStrip) {
+        V x[kStrip];
 #pragma unroll
-            for (int e = 0; e < N; ++e) x[e] = z[first + e];
+        for (int i = 0; i < kStrip; ++i) {
+            const T* const from = z + part.head + min(v0 + 64 * i, part.vecs - 1) * N;
+            if (same) x[i] = *reinterpret_cast<const V*>(from);
+            else {
+#pragma unroll
+                for (int e = 0; e < N; ++e) x[i][e] = from[e];
+            }
         }
 #pragma unroll
-        for (int e = 0; e < N; ++e) y[e] = gradient(to_f32((T)x[e]), first + e);
-        dv[v] = y;
+        for (int i = 0; i < kStrip; ++i) {
+            const int v = v0 + 64 * i;
+            V y;
+#pragma unroll
+            for (int e = 0; e < N; ++e) y[e] = gradient(to_f32((T)x[i][e]), part.head + v * N + e);
+            if (v < part.vecs) dv[v] = y;
+        }
     }
 }
 
