@@ -58,18 +58,27 @@ inline AttnPlan plan_attention(const int32_t* q_lens, const int32_t* k_lens, con
                                int tile_many, int tile_pair, int tile_few) {
     AttnPlan p;
     int most = 0, most_keys = 0;
-    for (int b = 0; b < batch; ++b) most = std::max(most, (int)q_lens[b]);
-    // Items of half the rows, with two wavefronts to 32 of them, where no sequence has more or where whole ones leave compute units idle.
     int64_t by_rows = 0, by_keys = 0;
     for (int b = 0; b < batch; ++b) {
         by_rows += (q_lens[b] + tile_many - 1) / tile_many;
         by_keys += (k_lens[b] + tile_many - 1) / tile_many;
+        most = std::max(most, (int)q_lens[b]);
         most_keys = std::max(most_keys, (int)k_lens[b]);
     }
-    p.dq_rows = tile_pair && (most <= tile_pair || by_rows * heads < kPlanSlots / 2) ? tile_pair : tile_many;
-    p.dkv_keys = tile_pair && (most_keys <= tile_pair || by_keys * kv_heads < kPlanSlots / 2) ? tile_pair : tile_many;
-    // (forward, long keys are split instead: 14 tiles of rows against 2000 to 6000 keys take 79 us so, 89 us in items of half the rows)
-    p.tile_rows = most <= tile_few ? tile_few : most_keys < 2 * kPlanPart || most <= tile_pair ? p.dq_rows : tile_many;
+    // Items of half the rows (keys), with two wavefronts to 32 of them, where twice as many workgroups still find a compute unit each, and
+    // for rows where no sequence has more.  Heads of 128 in bfloat16, 120 rows and keys a sequence, forward / dQ / dK and dV in us: 128 whole items 11.4 /
+    // 13.4 / 13.4, halves 10.4 / 12.5 / 13.2; 136 whole items 11.4 / 13.5 / 13.6, halves 11.7 / 16.0 / 20.6.  64 sequences of 64 rows
+    // and 300 keys, whole 22.8 / 27.1, halves 21.5 / 26.8; of 120 rows and 64 keys, dK and dV whole 24.9, halves 26.2.
+    const bool few_rows = by_rows * heads <= kPlanSlots / 4, few_keys = by_keys * kv_heads <= kPlanSlots / 4;
+    p.dq_rows = tile_pair && (most <= tile_pair || few_rows) ? tile_pair : tile_many;
+    p.dkv_keys = tile_pair && few_keys ? tile_pair : tile_many;
+    // Forward, up to 16 rows (up to all 32 where there are no halves) have a kernel of their own, unless keys are split: 256 sequences of 124 keys,
+    // 1 / 16 / 32 rows, 28.6 / 34.0 / 42.3 us, halves 30.7 / 34.2 / 36.4; 8 of 500 keys, 1 / 32 rows, 11.3 / 13.6, halves 13.9 / 14.4; 5 of 4000
+    // keys, 1 / 16 / 32 rows, 19.9 / 21.8 / 24.8, halves 18.3 / 18.9 / 19.2.  Where keys are split there are items enough without
+    // halves: 14 items of 128 rows against 2000 to 6000 keys take 79 us so, 89 us in halves.
+    const bool split = most_keys >= 2 * kPlanPart;
+    if (tile_pair ? most <= tile_few / 2 && !split : most <= tile_few) p.tile_rows = tile_few;
+    else p.tile_rows = split && most > tile_pair ? tile_many : p.dq_rows;
     const int step = p.tile_rows == tile_few ? 128 : 64;  // keys that a workgroup takes at once
     std::vector<PlanItem> whole;
     int64_t q_row = 0, packed = 0, steps = 0;

@@ -209,10 +209,6 @@ template <int TILES> __device__ __forceinline__ void clear(f32x16* acc) {
         for (int i = 0; i < 16; ++i) acc[t][i] = 0.f;
 }
 
-}  // namespace
-
-namespace {
-
 // Where a wavefront's part of the walk over the keys ends: it has no rows, or they see no further
 __device__ __forceinline__ int end_of(const RaggedArgs& a, const RaggedItem& it, int count, int pos) {
     return count == 0 ? it.k_begin : a.causal ? min(it.k_end, max(it.k_begin, pos + count)) : it.k_end;
@@ -228,7 +224,7 @@ template <typename T, int D> struct Steps {
     const char *kp, *vp;
     char* lds;
     int lane;
-    RowFeed<T, D, R::kStep, 4> feed;
+    RowFeed<T, D, R::kStep> feed;
     Seen bits;
     uint64_t seen = 0, seen_next = 0;  // of the step at hand and of the one on its way
     int buf = 1;
@@ -382,13 +378,13 @@ template <typename T, int D, bool BIAS> __global__ __launch_bounds__(256, (2 - R
     const char* const vp = a.v.p + it.k_row * a.v.row + v_head;
     char* const kb = lds + wave * kMine;
     char* const vb = kb + kMine / 2;
-    RowStage<T, D, 32, 64> ks, vs;
+    RowStage<T, D, 32> ks, vs;
     uint64_t seen = 0;
     Seen bits(a, it, it.k_begin + 32 * wave, lane);
     auto fetch = [&](int k0) {
         seen = bits.next(128);
-        ks.template load<true>(kp + k0 * a.k.row, (int)a.k.row, it.k_end - k0, seen, lane);
-        vs.template load<true>(vp + k0 * a.v.row, (int)a.v.row, it.k_end - k0, seen, lane);
+        ks.load(kp + k0 * a.k.row, (int)a.k.row, it.k_end - k0, seen, lane);
+        vs.load(vp + k0 * a.v.row, (int)a.v.row, it.k_end - k0, seen, lane);
     };
     int k0 = it.k_begin + 32 * wave;
     if (k0 < it.k_end) fetch(k0);
@@ -647,7 +643,7 @@ template <typename T, int D, bool SHAPED, bool PAIR> __global__ __launch_bounds_
     const int kv_head = blockIdx.x % kv_heads, group = PAIR ? wave & 1 : wave, half = PAIR ? wave >> 1 : 0;  // which keys, which rows of a step
     const int count = min(max(it.rows - 32 * group, 0), 32), key0 = it.pos + 32 * group;
     const int64_t k_row0 = it.k_row + 32 * group;
-    const RowFeed<T, D, kRows, 4> feed(lds, wave, lane);
+    const RowFeed<T, D, kRows> feed(lds, wave, lane);
     int head = kv_head * a.share, buf = 1;
     float stat = 0.f;
     // requests the step of query rows q0 on, into the buffer that is not at hand
@@ -701,7 +697,7 @@ template <typename T, int D, bool SHAPED, bool PAIR> __global__ __launch_bounds_
                 feed.load(next_gs, g_pitch, next_n, to + kBuf / 2);
                 continue;
             }
-            constexpr int kPer = RowFeed<T, D, kRows, 4>::kEach / kTilesOf;  // requests of each of the two tensors in a tile of rows
+            constexpr int kPer = RowFeed<T, D, kRows>::kEach / kTilesOf;  // requests of each of the two tensors in a tile of rows
             auto ask_q = [&](int u) {
 #pragma unroll
                 for (int i = 0; i < kPer; ++i) feed.one(u * kPer + i, next_qs, q_pitch, next_n, to);

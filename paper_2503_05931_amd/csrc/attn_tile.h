@@ -65,7 +65,7 @@ template <int D> struct AsRows<bf16_t, D> {
 #pragma unroll
         for (int s = 0; s < R::kSteps; ++s) c[s] = *reinterpret_cast<const bf16x8*>(rows + R::at(first + (lane & 31), 2 * s + (lane >> 5)));
     }
-    template <typename F> __device__ __forceinline__ void dot(f32x16& acc, const F& f) const {  // F: RowFrag, or rows of LDS too
+    __device__ __forceinline__ void dot(f32x16& acc, const RowFrag<bf16_t, D>& f) const {
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[i] = 0.f;
 #pragma unroll
@@ -135,27 +135,26 @@ template <int D> struct AsColumns<float, D> {
     }
 };
 
-// N rows on their way from memory to LDS through the registers of THREADS threads.  Rows that are not there are beyond the end of the
+// N rows on their way from memory to LDS through the registers of a wavefront.  Rows that are not there are beyond the end of the
 // descriptor, rows that are not seen are sent there: both come as zeros, whatever stands in their place.
-template <typename T, int D, int N, int THREADS> struct RowStage {
+template <typename T, int D, int N> struct RowStage {
     typedef Rows<T, D> R;
-    static constexpr int kEach = N * R::kChunks / THREADS, kApart = THREADS / R::kChunks;
-    static_assert(N * R::kChunks % THREADS == 0 && THREADS % R::kChunks == 0, "a thread keeps its column");
+    static constexpr int kEach = N * R::kChunks / 64, kApart = 64 / R::kChunks;
+    static_assert(N * R::kChunks % 64 == 0 && 64 % R::kChunks == 0, "a lane keeps its column");
     typename R::chunk_t c[kEach];
-    // first: the first of `count` >= 1 rows; live: bit n = row n is seen (looked at if MASK)
-    template <bool MASK> __device__ __forceinline__ void load(const char* first, int pitch, int count, uint64_t live, int tid) {
+    // first: the first of `count` >= 1 rows; seen: bit n = row n is
+    __device__ __forceinline__ void load(const char* first, int pitch, int count, uint64_t seen, int lane) {
         const __amdgpu_buffer_rsrc_t rsrc =
             __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(first), 0, (min(count, N) - 1) * pitch + R::kPitch, 0x20000);
-        const int row = tid / R::kChunks, off = row * pitch + (tid % R::kChunks) * 16;
+        const int row = lane / R::kChunks, off = row * pitch + (lane % R::kChunks) * 16;
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            int at = off;
-            if constexpr (MASK) at = (live >> (row + i * kApart)) & 1 ? at : kBeyond;
+            const int at = (seen >> (row + i * kApart)) & 1 ? off : kBeyond;
             c[i] = __builtin_bit_cast(typename R::chunk_t, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, i * kApart * pitch, 0));
         }
     }
-    __device__ __forceinline__ void store(char* lds, int tid) const {
-        const int row = tid / R::kChunks, chunk = tid % R::kChunks;
+    __device__ __forceinline__ void store(char* lds, int lane) const {
+        const int row = lane / R::kChunks, chunk = lane % R::kChunks;
 #pragma unroll
         for (int i = 0; i < kEach; ++i) *reinterpret_cast<typename R::chunk_t*>(lds + R::at(row + i * kApart, chunk)) = c[i];
     }
@@ -178,10 +177,11 @@ __device__ __forceinline__ void loads_done_barrier() {
     asm volatile("" ::: "memory");
 }
 
-// N rows from memory to LDS, no registers in between, by the W wavefronts of a workgroup.  A request fills 1 KB of consecutive LDS, so
+// N rows from memory to LDS, no registers in between, by the four wavefronts of a workgroup.  A request fills 1 KB of consecutive LDS, so
 // what changes places are the chunks that the lanes ask for.  Rows past `count` get the last one that is there.
-template <typename T, int D, int N, int W> struct RowFeed {
+template <typename T, int D, int N> struct RowFeed {
     typedef Rows<T, D> R;
+    static constexpr int W = 4;
     static constexpr int kAtOnce = 64 / R::kChunks, kEach = N / (W * kAtOnce);  // rows of a request, requests of a wavefront
     static_assert(W * kAtOnce % 8 == 0 && N % (W * kAtOnce) == 0, "a lane's rows agree in what its chunk is");
     int row, chunk;
