@@ -171,23 +171,17 @@ template <bool BIAS> __device__ __forceinline__ float weight_of(float s, float s
     return __builtin_amdgcn_exp2f(BIAS ? s - base : fmaf(s, scale2, -base));
 }
 
-// Softmax of a lane's row in passing: what is taken off its scores (times log2 e), and the lane half's share of the sum.  That is a maximum
-// so far, not always the latest: sums are scaled anew only when a tile exceeds it by more than kSlack in some row.  Until then weights reach
-// 2^kSlack, which costs neither float32 sums nor bfloat16 weights a digit.  (Scaled in every step: 185 us instead of 179 on 128
-// utterances of 400 to 500 frames, 64.3 instead of 63.0 on 5 of 2000 to 6000.)
+// Softmax of a lane's row in passing: maximum so far (times log2 e), and the lane half's share of the sum
 struct Running {
     float m = kNone, l = 0.f;
     template <int TILES> __device__ __forceinline__ float scale_to(float m_tile, f32x16* acc) {
-        if (__ballot(m_tile > m + kSlack) != 0) {
-            const float m_new = fmaxf(m, m_tile), alpha = __builtin_amdgcn_exp2f(m - base_of(m_new));
-            l *= alpha;
+        const float m_new = fmaxf(m, m_tile), base = base_of(m_new), alpha = __builtin_amdgcn_exp2f(m - base);
+        l *= alpha;
 #pragma unroll
-            for (int t = 0; t < TILES; ++t) acc[t] *= alpha;
-            m = m_new;
-        }
-        return base_of(m);
+        for (int t = 0; t < TILES; ++t) acc[t] *= alpha;
+        m = m_new;
+        return base;
     }
-    static constexpr float kSlack = 8.f;
 };
 // one tile of scores to weights; the sum goes to l
 template <bool BIAS> __device__ __forceinline__ void to_weights(f32x16& s, float scale2, float base, float& l) {
