@@ -112,7 +112,7 @@ aed_status check_attn(const aed_attn_config* c, const int32_t* q_lens, const int
     if (q_rows > kMost || k_rows > kMost) return fail(AED_EUNSUPPORTED, "more than 2^31 - 1 query rows or keys");
     if (c->n_heads > 65535) return fail(AED_EUNSUPPORTED, "more than 65535 heads");
     // a bound on the work items of any list, before any of them is made
-    const int64_t items = std::max(q_rows, k_rows) / aed::kAttnFew + batch + aed::kPlanSlots;  // (one of few rows at the least)
+    const int64_t items = std::max(q_rows, k_rows) / aed::kAttnFew + batch + aed::kPlanMost;  // (one of few rows at the least)
     if (items * c->n_heads > kMost) return fail(AED_EUNSUPPORTED, "more than 2^31 - 1 workgroups");
     return AED_OK;
 }

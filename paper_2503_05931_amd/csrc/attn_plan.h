@@ -11,7 +11,9 @@ namespace aed {
 
 // Lists are made for the whole chip: two workgroups on each of 256 compute units.
 constexpr int kPlanSlots = 512;
-constexpr int kPlanPart = 512;  // keys of a part at the least
+constexpr int kPlanLong = 1024;  // keys from which on a row's may be split
+constexpr int kPlanPart = 256;   // keys of a part at the least
+constexpr int kPlanMost = 4 * kPlanSlots;  // workgroups up to which splitting is looked at
 
 // First distances of a side's logarithmic buckets, half + 1 on: the smallest n with (n / half)^(side - half) >= (max / half)^i.
 // The power is irrational but where it is a whole number, which rounding must not miss.
@@ -46,6 +48,24 @@ struct PlanJoin {
     int32_t q_row, rows, part, n_parts;
 };
 
+// Microseconds that the forward kernel takes over items of `steps` steps each, split into parts of at most `share`.  A workgroup alone on a compute
+// unit takes `step` a step, one of two 1.6 times as long; starting it 5; the join's launch 2 and 16 ns a part and head.  Measured with 8 heads
+// of 128 in bfloat16 on 12 batches of 1 to 40 sequences, 1 to 448 rows and 1000 to 8000 keys, 0 to 24 parts each: what this finds best takes at
+// most 10 % longer than what was.  (Part counts by the chip's share alone, three workgroups to two slots: up to 20 % longer, as most
+// of the last round of workgroups was idle.)
+inline double walk_time(const std::vector<int>& steps, int64_t share, int heads, double step, bool two_on_a_unit) {
+    int64_t items = 0, parts = 0, longest = 0;
+    for (const int n : steps) {
+        const int64_t of = std::max<int64_t>(1, (n + share - 1) / share);
+        items += of;
+        if (of > 1) parts += of;
+        longest = std::max<int64_t>(longest, (n + of - 1) / of);
+    }
+    const int64_t units = kPlanSlots / 2, round = two_on_a_unit ? kPlanSlots : units, full = items * heads / round, left = items * heads % round;
+    const double both = two_on_a_unit ? 1.6 : 1.0, rounds = (double)full * both + (left == 0 ? 0 : left <= units ? 1.0 : both);
+    return rounds * step * (double)longest + 5.0 * (double)(full + (left > 0)) + (parts > 0 ? 2.0 + 0.016 * (double)(parts * heads) : 0.0);
+}
+
 struct AttnPlan {
     int tile_rows = 0, dq_rows = 0, dkv_keys = 0, n_parts = 0;  // query rows of an item, forward and backward; keys of one of key gradients
     std::vector<PlanItem> forward, dq, dkv;
@@ -76,12 +96,12 @@ inline AttnPlan plan_attention(const int32_t* q_lens, const int32_t* k_lens, con
     // 1 / 16 / 32 rows, 28.6 / 34.0 / 42.3 us, halves 30.7 / 34.2 / 36.4; 8 of 500 keys, 1 / 32 rows, 11.3 / 13.6, halves 13.9 / 14.4; 5 of 4000
     // keys, 1 / 16 / 32 rows, 19.9 / 21.8 / 24.8, halves 18.3 / 18.9 / 19.2.  Where keys are split there are items enough without
     // halves: 14 items of 128 rows against 2000 to 6000 keys take 79 us so, 89 us in halves.
-    const bool split = most_keys >= 2 * kPlanPart;
+    const bool split = most_keys >= kPlanLong;
     if (tile_pair ? most <= tile_few / 2 && !split : most <= tile_few) p.tile_rows = tile_few;
     else p.tile_rows = split && most > tile_pair ? tile_many : p.dq_rows;
     const int step = p.tile_rows == tile_few ? 128 : 64;  // keys that a workgroup takes at once
     std::vector<PlanItem> whole;
-    int64_t q_row = 0, packed = 0, steps = 0;
+    int64_t q_row = 0, packed = 0;
     auto tiles = [&](int tile, std::vector<PlanItem>& to, int b, int64_t k_row) {
         const int nq = q_lens[b], nk = k_lens[b];
         for (int q0 = 0; q0 < nq; q0 += tile) {
@@ -104,13 +124,25 @@ inline AttnPlan plan_attention(const int32_t* q_lens, const int32_t* k_lens, con
         packed += nk;
     }
     p.q_rows = q_row;
-    for (const PlanItem& it : whole) steps += (it.k_end + step - 1) / step;
-    // Keys are split where an item would take much longer than its share of the chip, into parts of kPlanPart keys and more: at
-    // 1.5 workgroups to a slot the parts of unlike rows even out.
-    const int64_t share = std::max<int64_t>(kPlanPart / step, (2 * steps * heads + 3 * kPlanSlots - 1) / (3 * kPlanSlots));
+    std::vector<int> steps;
+    for (const PlanItem& it : whole) steps.push_back((it.k_end + step - 1) / step);
+    const int64_t longest = steps.empty() ? 0 : *std::max_element(steps.begin(), steps.end());
+    int64_t share = std::max<int64_t>(longest, 1);
+    if (longest * step >= kPlanLong && (int64_t)whole.size() * heads <= kPlanMost) {
+        const double step_time = p.tile_rows == tile_pair ? 1.2 : 1.85;  // a wavefront of a pair has half of a step's keys
+        double best = walk_time(steps, share, heads, step_time, tile_pair != 0);
+        for (int64_t parts = 2; longest >= parts * (kPlanPart / step); ++parts) {
+            const int64_t with = (longest + parts - 1) / parts;
+            int64_t items = 0;
+            for (const int n : steps) items += std::max<int64_t>(1, (n + with - 1) / with);
+            if (items * heads > kPlanMost) break;
+            const double time = walk_time(steps, with, heads, step_time, tile_pair != 0);
+            if (time < best) best = time, share = with;
+        }
+    }
     for (const PlanItem& it : whole) {
         const int n = (it.k_end + step - 1) / step;
-        if (n < 2 * share) {
+        if (n <= share) {
             p.forward.push_back(it);
             continue;
         }

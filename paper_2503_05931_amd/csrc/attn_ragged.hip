@@ -5,9 +5,18 @@
 //   dP = dO . V   delta_i = dO_i . O_i   dS = P (dP - delta)   dQ = scale dS K   dK = scale dS^T Q   dV = P^T dO
 //   dw[b] = sum of dS over the pairs of bucket b
 //
-// Exponentials are powers of two: scores and bias carry log2 e.  Scores, softmax and sums are float32; in bfloat16 the weights
-// P and dS are rounded once, where they become an operand of the second product.  No result depends on timing: whatever
-// is added up has one order, and there are no atomics between wavefronts.
+// Exponentials are powers of two: scores and bias carry log2 e.  Scores, softmax and sums are float32.  In bfloat16 the weights P and dS are
+// rounded once, where they become an operand of the second product: that product then runs at 16 times the float32 instructions' rate.  It costs
+// as much as the rounding of the result itself does: outputs that are off by 0.0017 (2-norm, relative) from rounding alone are off by 0.0018 to
+// 0.0020, gradients by 0.0024 to 0.0029 (dQ and dw most: delta comes from the rounded output, see there).  No result depends on timing:
+// whatever is added up has one order, and there are no atomics between wavefronts.
+//
+// Times in this file are the kernels' on an MI355X, bfloat16, 8 heads of 128, for the gradients' lists of four batches:
+//   short  64 utterances, 4 909 rows (12 to 132), 9 021 keys           forward  18 us   dQ  26   dK and dV  34
+//   long  128 utterances, 48 029 rows (300 to 448), 57 196 keys                185       250            386
+//   self, short  64 sequences of 12 to 132 positions, causal, bias              15        29             28
+//   self, long  128 sequences of 8 to 448 positions, causal, bias               70       143            140
+// The products of the long batch are 88, 132 and 176 GFLOP: 475, 528 and 456 TFLOP/s, against 1 240 of a product of 8192 x 8192 x 8192.
 #include "attn_ragged.h"
 #include "attn_tile.h"
 #include "device_once.h"
@@ -90,7 +99,7 @@ template <int STEP> __device__ __forceinline__ void add_bias(f32x16& s, const Ra
 // Sums of a tile's elements (lane = query) by distance, key - query = 4 h - y - 16 + 16 t for lane y of a 16-lane row: the elements of
 // key 8 g + e are shifted along the row by that many lanes (an operand's modifier, not an instruction) so that one distance, modulo 16,
 // stays in a lane; what leaves the row at one end and comes in at the other is 16 further.  (Adding every element to LDS, which
-// takes its lanes' atomics one by one: dQ's kernel 241 us instead of @@ us on 128 sequences of up to 448 positions.)
+// takes its lanes' atomics one by one: dQ's kernel 241 us instead of 143 on the long batch.)
 template <int K> __device__ __forceinline__ void add_shifted(float v, float* sum) {
     constexpr int n = K & 15, m = K >> 4;
     if constexpr (n == 0) {
@@ -143,7 +152,7 @@ template <int FIRST, int READS, int EACH> __device__ __forceinline__ void woven(
     phase();
 }
 
-// keeps what a branch computes from `v` in the branch: the compiler would rather do it always than jump
+// Keeps what a branch computes from `v` in the branch: the compiler would rather do it always than jump
 __device__ __forceinline__ void rarely(uint32_t& v) { asm volatile("" : "+v"(v)); }
 
 // scores of a tile (lane = query) from its products: without a bias they stay unscaled (times scale2 later), with one they are whole;
@@ -253,7 +262,11 @@ template <typename T, int D> struct Steps {
 
 // ---------------------------------------------------------------- forward, many rows
 // A workgroup takes 128 query rows of a head, 32 a wavefront, and walks the keys.  PAIR: it takes 64 rows, and two wavefronts share 32 of them,
-// each with 32 keys of a step.
+// each with 32 keys of a step.  Scores are computed transposed (a lane is a query), so that a lane holds half a row's weights
+// and they enter the second product from where they are.  Of 200 us for 128 utterances of 448 rows and 512 keys, 100 are the two products
+// (their rate is a large product's), 30 the softmax in between, 35 the wait for keys and values and 39 starts and ends; two
+// workgroups share a compute unit to cover one's waits with the other's products, which is why a wavefront has 256 registers and 32 rows: with 64 rows
+// and all registers it was 258 us against 184.  Short batches are bound by starts and ends, a single round of workgroups.
 template <typename T, int D, bool BIAS, bool PAIR> __global__ __launch_bounds__(256, (2 - Rows<T, D>::kWide)) void attn_forward_kernel(RaggedArgs a) {
     typedef Rows<T, D> R;
     extern __shared__ __align__(16) char lds[];
@@ -357,7 +370,9 @@ template <typename T, int D, bool BIAS, bool PAIR> __global__ __launch_bounds__(
 
 // ---------------------------------------------------------------- forward, few rows
 // A workgroup takes up to 32 query rows of a head; its four wavefronts take 32 keys each in turn, through rows of LDS of their own, and
-// join their sums at the end.  The matrix cores are mostly idle here: what counts is that keys and values stream.
+// join their sums at the end.  The matrix cores are mostly idle here: what counts is that keys and values stream.  Bound by memory: one row for
+// each of 256 utterances, 31 792 keys of 8 heads of 128, 131 MB in 26.8 us, 4.9 TB/s (a large copy: 5.1); 64 sequences with 13 696 keys
+// in a cache of 448, with bias, 56 MB in 14.5 us.  One utterance of 100 frames takes 5.3 us, which is a launch and three trips to memory.
 template <typename T, int D, bool BIAS> __global__ __launch_bounds__(256, (2 - Rows<T, D>::kWide)) void attn_few_kernel(RaggedArgs a) {
     typedef Rows<T, D> R;
     extern __shared__ __align__(16) char lds[];
@@ -451,6 +466,8 @@ template <typename T, int D, bool BIAS> __global__ __launch_bounds__(256, (2 - R
 }
 
 // ---------------------------------------------------------------- parts of rows whose keys were split
+// Bound by memory, the parts' sums mostly from the caches that they were just written to: 5 utterances of 1 757 rows and 2000 to 6000 keys 9.5 us
+// behind 64 us of the walks.  Parts stay float32: a sum of parts is rounded once, as an unsplit row's is.
 template <typename T, int D> __global__ __launch_bounds__(256) void attn_join_kernel(RaggedArgs a, int tile_rows) {
     const RaggedJoin j = a.joins[blockIdx.x];
     const int head = blockIdx.y, per = D / 4, at = blockIdx.z * 256 + threadIdx.x;
@@ -474,8 +491,12 @@ template <typename T, int D> __global__ __launch_bounds__(256) void attn_join_ke
 
 // ---------------------------------------------------------------- query gradients, delta, and the bias's
 // The forward kernel's walk with two products to a tile of scores (K Q^T and V dO^T, transposed, a lane being a query) and one
-// more for dQ.  delta is left for the key gradients' kernel, without the error that the rounded output leaves in it: a row's dS add up
-// to 0, so what they do add up to is what delta lacks.
+// more for dQ.  delta comes from the output as it was stored: in bfloat16 its rounding goes into every dS of the row (dQ 0.0024 to 0.0028 off
+// instead of 0.0024).  Without it, delta as the sum of P dP over the keys, the walk would be made twice: five products instead of
+// three.  For the key gradients' kernel delta is left without that error: a row's dS add up to 0, so what they do add up to is
+// what delta lacks.
+// Bound like the forward kernel.  Fragments are read where they are used: read one product ahead, as in the kernel below, they need more than 256
+// registers (424 to 796 us on the long batch instead of 250).  The bias and its gradient make 64 sequences 29 us long instead of 26.
 template <typename T, int D, bool BIAS, bool PAIR> __global__ __launch_bounds__(256, (2 - Rows<T, D>::kWide)) void attn_dq_kernel(RaggedArgs a) {
     typedef Rows<T, D> R;
     extern __shared__ __align__(16) char lds[];
@@ -619,7 +640,14 @@ template <typename T> __device__ __forceinline__ void reduce_bias(const RaggedAr
 }  // namespace
 
 // A workgroup takes 128 keys of a key head, 32 a wavefront (a lane being a key), and walks the query rows of all heads that share it.
-// PAIR: it takes 64 keys, and two wavefronts share 32 of them, each with 32 rows of a step.
+// PAIR: it takes 64 keys, and two wavefronts share 32 of them, each with 32 rows of a step.  Four products to a tile and no sum over
+// workgroups: what heads share is added up here, in order.
+// Two accumulators of 32 keys and the keys and values themselves take 192 registers, so that a wavefront has a SIMD to itself and nothing else
+// covers its waits: operands are requested one product ahead, and their reads and the vector instructions stand among the matrix
+// instructions (386 us on the long batch; requested at their use 426).  Of 400 us for 128 utterances of 448 rows and 512 keys, 331 remain without any
+// request to memory in the loop, 74 of them starts and ends.  Slower: two workgroups a compute unit in 256 registers each 467, eight wavefronts
+// with keys and values in LDS 432, 64 keys a wavefront 499; one workgroup a compute unit that goes on to the next task 401, and 38 instead of
+// 28 us for short causal sequences, which do not end together then.
 template <typename T, int D, bool SHAPED, bool PAIR> __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(RaggedArgs a) {
     typedef Rows<T, D> R;
     constexpr int kRows = R::kStep, kBuf = 2 * kRows * R::kPitch, kTilesOf = PAIR ? 1 : kRows / 32;  // 32-row tiles of a step for a wavefront

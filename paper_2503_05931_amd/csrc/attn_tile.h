@@ -22,7 +22,10 @@ template <> struct Chunk<float> { typedef f32x4 type; };
 template <typename T, int D> struct Rows {
     typedef typename Chunk<T>::type chunk_t;
     static constexpr int kPitch = D * (int)sizeof(T), kChunks = kPitch / 16, kSteps = kChunks / 2, kTiles = D / 32;
-    static constexpr int kWide = kPitch > 256;  // a workgroup's rows fill the LDS of half a CU and more: one of them has all its registers
+    // float32 rows of 128: two steps of 64 of them, keys and values, would take 128 KB and leave too little for a bias and the sums of
+    // its gradient (up to 79 KB).  Steps of 32 fill 64 KB, as those of other rows do at the most, but a wavefront's own rows need twice the
+    // registers: one workgroup has a compute unit's.
+    static constexpr int kWide = kPitch > 256;
     static constexpr int kStep = kWide ? 32 : 64;  // rows of a step of the kernels that walk over keys or queries
     static constexpr uint64_t kAll = kWide ? 0xffffffffull : ~0ull;  // a bit for each of them
     static __device__ __forceinline__ int swap_of(int row) { return ((row & 3) << 1) | ((row >> 2) & 1); }

