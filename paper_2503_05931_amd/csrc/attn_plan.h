@@ -128,7 +128,7 @@ inline AttnPlan plan_attention(const int32_t* q_lens, const int32_t* k_lens, con
     for (const PlanItem& it : whole) steps.push_back((it.k_end + step - 1) / step);
     const int64_t longest = steps.empty() ? 0 : *std::max_element(steps.begin(), steps.end());
     int64_t share = std::max<int64_t>(longest, 1);
-    if (longest * step >= kPlanLong && (int64_t)whole.size() * heads <= kPlanMost) {
+    if (split && (int64_t)whole.size() * heads <= kPlanMost) {
         const double step_time = p.tile_rows == tile_pair ? 1.2 : 1.85;  // a wavefront of a pair has half of a step's keys
         double best = walk_time(steps, share, heads, step_time, tile_pair != 0);
         for (int64_t parts = 2; longest >= parts * (kPlanPart / step); ++parts) {
