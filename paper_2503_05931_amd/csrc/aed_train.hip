@@ -120,7 +120,7 @@ aed_status check_attn(const aed_attn_config* c, const int32_t* q_lens, const int
 void lay_out(aed_attn& p, const int32_t* q_lens, const int32_t* k_lens, const int64_t* k_starts, int32_t batch) {
     const aed_attn_config& c = p.cfg;
     p.plan = aed::plan_attention(q_lens, k_lens, k_starts, batch, c.n_heads, c.n_kv_heads, c.causal != 0, c.training != 0, aed::kAttnRows,
-                                 c.dtype == 0 && c.head_dim == 128 ? 0 : aed::kAttnPair, aed::kAttnFew);  // wide rows have no pairs
+                                 c.dtype == 0 && c.head_dim == 128 ? 0 : aed::kAttnPair, aed::kAttnFew, c.dtype == 1, c.head_dim);  // wide rows have no pairs
     p.k_rows = 0;
     for (int b = 0; b < batch; ++b) p.k_rows += k_lens[b];
     p.forward = p.arena.table(p.plan.forward);

@@ -48,22 +48,35 @@ struct PlanJoin {
     int32_t q_row, rows, part, n_parts;
 };
 
-// Microseconds that the forward kernel takes over items of `steps` steps each, split into parts of at most `share`.  A workgroup alone on a compute
-// unit takes `step` a step, one of two 1.6 times as long; starting it 5; the join's launch 2 and 16 ns a part and head.  Measured with 8 heads
-// of 128 in bfloat16 on 12 batches of 1 to 40 sequences, 1 to 448 rows and 1000 to 8000 keys, 0 to 24 parts each: what this finds best takes at
-// most 10 % longer than what was.  (Part counts by the chip's share alone, three workgroups to two slots: up to 20 % longer, as most
-// of the last round of workgroups was idle.)
-inline double walk_time(const std::vector<int>& steps, int64_t share, int heads, double step, bool two_on_a_unit) {
-    int64_t items = 0, parts = 0, longest = 0;
+// Microseconds of the forward kernel: a step of a workgroup alone on its compute unit, how many times as long it takes if two are there (0: two do
+// not fit), a part and head of the join.  Rows shared in pairs: a wavefront has half of a step's keys, and if there are 32 rows at the most, half of the
+// wavefronts have none, which float32 products leave to the others.
+struct WalkCost {
+    double step, both, part;
+};
+inline WalkCost walk_cost(bool bf16, int head_dim, bool pairs, int most_rows) {
+    const WalkCost c = bf16 ? (head_dim == 128 ? WalkCost{1.85, 1.6, 0.016} : WalkCost{1.15, 1.35, 0.008})
+                            : (head_dim == 128 ? WalkCost{10.3, 0.0, 0.016} : WalkCost{5.0, pairs && most_rows <= 32 ? 1.1 : 1.9, 0.008});
+    return WalkCost{pairs ? 0.6 * c.step : c.step, c.both, c.part};
+}
+// and over items of `steps` steps each, split into parts of at most `share`, longest first: rounds of workgroups, 5 us to start each, 2 us for the
+// join's launch.  Measured on 12 batches of 1 to 40 sequences, 1 to 448 rows and 1000 to 8000 keys, 0 to 24 parts each (8 heads of 128 in bfloat16, and
+// 6 of them in the other kinds): what this finds best takes at most 12 % longer than what was.  (Part counts by the chip's share alone,
+// three workgroups to two slots: up to 30 % longer, as most of the last round of workgroups was idle.)
+inline double walk_time(const std::vector<int>& steps, int64_t share, int heads, const WalkCost& cost) {
+    int64_t items = 0, parts = 0, longest = 0, total = 0;
     for (const int n : steps) {
         const int64_t of = std::max<int64_t>(1, (n + share - 1) / share);
         items += of;
+        total += n;
         if (of > 1) parts += of;
         longest = std::max<int64_t>(longest, (n + of - 1) / of);
     }
-    const int64_t units = kPlanSlots / 2, round = two_on_a_unit ? kPlanSlots : units, full = items * heads / round, left = items * heads % round;
-    const double both = two_on_a_unit ? 1.6 : 1.0, rounds = (double)full * both + (left == 0 ? 0 : left <= units ? 1.0 : both);
-    return rounds * step * (double)longest + 5.0 * (double)(full + (left > 0)) + (parts > 0 ? 2.0 + 0.016 * (double)(parts * heads) : 0.0);
+    if (items == 0) return 0;
+    const int64_t units = kPlanSlots / 2, round = cost.both > 0 ? 2 * units : units, full = items * heads / round, left = items * heads % round;
+    const double both = cost.both > 0 ? cost.both : 1.0, rounds = (double)full * both + (left == 0 ? 0 : left <= units ? 1.0 : both);
+    const double mean = full > 0 ? (double)total / (double)items : (double)longest;
+    return std::max(rounds * mean, (double)longest) * cost.step + 5.0 * (double)(full + (left > 0)) + (parts > 0 ? 2.0 + cost.part * (double)(parts * heads) : 0.0);
 }
 
 struct AttnPlan {
@@ -75,7 +88,7 @@ struct AttnPlan {
 
 // tile_many, tile_pair (0: there are none), tile_few: query rows of an item, tile_many and tile_pair also keys of one of key gradients
 inline AttnPlan plan_attention(const int32_t* q_lens, const int32_t* k_lens, const int64_t* k_starts, int batch, int heads, int kv_heads, bool causal, bool training,
-                               int tile_many, int tile_pair, int tile_few) {
+                               int tile_many, int tile_pair, int tile_few, bool bf16 = true, int head_dim = 128) {
     AttnPlan p;
     int most = 0, most_keys = 0;
     int64_t by_rows = 0, by_keys = 0;
@@ -129,14 +142,14 @@ inline AttnPlan plan_attention(const int32_t* q_lens, const int32_t* k_lens, con
     const int64_t longest = steps.empty() ? 0 : *std::max_element(steps.begin(), steps.end());
     int64_t share = std::max<int64_t>(longest, 1);
     if (split && (int64_t)whole.size() * heads <= kPlanMost) {
-        const double step_time = p.tile_rows == tile_pair ? 1.2 : 1.85;  // a wavefront of a pair has half of a step's keys
-        double best = walk_time(steps, share, heads, step_time, tile_pair != 0);
+        const WalkCost cost = walk_cost(bf16, head_dim, p.tile_rows == tile_pair, most);
+        double best = walk_time(steps, share, heads, cost);
         for (int64_t parts = 2; longest >= parts * (kPlanPart / step); ++parts) {
             const int64_t with = (longest + parts - 1) / parts;
             int64_t items = 0;
             for (const int n : steps) items += std::max<int64_t>(1, (n + with - 1) / with);
             if (items * heads > kPlanMost) break;
-            const double time = walk_time(steps, with, heads, step_time, tile_pair != 0);
+            const double time = walk_time(steps, with, heads, cost);
             if (time < best) best = time, share = with;
         }
     }

@@ -6,9 +6,9 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 def test_sizes_and_splits(tmp_path):
-    exe = str(tmp_path / "attn_split")
+    exe = str(tmp_path / "attn_lists")
     r = subprocess.run(["/opt/rocm/llvm/bin/clang++", "-std=c++17", "-O1", "-Wall", "-fsanitize=undefined", "-fno-sanitize-recover=all", "-I",
-                        os.path.join(ROOT, "paper_2503_05931_amd", "csrc"), os.path.join(ROOT, "tests", "native", "attn_split.cpp"), "-o", exe],
+                        os.path.join(ROOT, "paper_2503_05931_amd", "csrc"), os.path.join(ROOT, "tests", "native", "attn_lists.cpp"), "-o", exe],
                        capture_output=True, text=True)
     assert r.returncode == 0, r.stderr[-4000:]
     r = subprocess.run([exe], capture_output=True, text=True, timeout=120)
