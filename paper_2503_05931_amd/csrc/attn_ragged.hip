@@ -6,17 +6,19 @@
 //   dw[b] = sum of dS over the pairs of bucket b
 //
 // Exponentials are powers of two: scores and bias carry log2 e.  Scores, softmax and sums are float32.  In bfloat16 the weights P and dS are
-// rounded once, where they become an operand of the second product: that product then runs at 16 times the float32 instructions' rate.  It costs
+// rounded, where they become an operand of the second product: that product then runs at 16 times the float32 instructions' rate.  It costs
 // as much as the rounding of the result itself does: outputs that are off by 0.0017 (2-norm, relative) from rounding alone are off by 0.0018 to
-// 0.0020, gradients by 0.0024 to 0.0029 (dQ and dw most: delta comes from the rounded output, see there).  No result depends on timing:
-// whatever is added up has one order, and there are no atomics between wavefronts.
+// 0.0020, dK and dV by 0.0024.  dQ has the error of delta besides (see there), so its weights are rounded to 16 bits, a sum of two bfloat16: 0.0019
+// to 0.0023.  dw, sums of float32 dS with that error, is off by up to 0.0028.  No result depends on timing: whatever is added up has one
+// order, and there are no atomics between wavefronts.
 //
 // Times in this file are the kernels' on an MI355X, bfloat16, 8 heads of 128, for the gradients' lists of four batches:
-//   short  64 utterances, 4 909 rows (12 to 132), 9 021 keys           forward  18 us   dQ  26   dK and dV  34
-//   long  128 utterances, 48 029 rows (300 to 448), 57 196 keys                185       250            386
-//   self, short  64 sequences of 12 to 132 positions, causal, bias              15        29             28
-//   self, long  128 sequences of 8 to 448 positions, causal, bias               70       143            140
-// The products of the long batch are 88, 132 and 176 GFLOP: 475, 528 and 456 TFLOP/s, against 1 240 of a product of 8192 x 8192 x 8192.
+//   short  64 utterances, 4 909 rows (12 to 132), 9 021 keys           forward  18 us   dQ  29   dK and dV  34
+//   long  128 utterances, 48 029 rows (300 to 448), 57 196 keys                185       286            386
+//   self, short  64 sequences of 12 to 132 positions, causal, bias              15        30             28
+//   self, long  128 sequences of 8 to 448 positions, causal, bias               70       148            140
+// The products of the long batch are 88, 176 (one of dQ's three made twice) and 176 GFLOP: 475, 615 and 456 TFLOP/s, against 1 240 of a
+// product of 8192 x 8192 x 8192.
 #include "attn_ragged.h"
 #include "attn_tile.h"
 #include "device_once.h"
@@ -99,7 +101,8 @@ template <int STEP> __device__ __forceinline__ void add_bias(f32x16& s, const Ra
 // Sums of a tile's elements (lane = query) by distance, key - query = 4 h - y - 16 + 16 t for lane y of a 16-lane row: the elements of
 // key 8 g + e are shifted along the row by that many lanes (an operand's modifier, not an instruction) so that one distance, modulo 16,
 // stays in a lane; what leaves the row at one end and comes in at the other is 16 further.  (Adding every element to LDS, which
-// takes its lanes' atomics one by one: dQ's kernel 241 us instead of 143 on the long batch.)
+// takes its lanes' atomics one by one: dQ's kernel 241 us instead of 143, with the plain third product, on the
+// long batch of its own.)
 template <int K> __device__ __forceinline__ void add_shifted(float v, float* sum) {
     constexpr int n = K & 15, m = K >> 4;
     if constexpr (n == 0) {
@@ -491,12 +494,12 @@ template <typename T, int D> __global__ __launch_bounds__(256) void attn_join_ke
 
 // ---------------------------------------------------------------- query gradients, delta, and the bias's
 // The forward kernel's walk with two products to a tile of scores (K Q^T and V dO^T, transposed, a lane being a query) and one
-// more for dQ.  delta comes from the output as it was stored: in bfloat16 its rounding goes into every dS of the row (dQ 0.0024 to 0.0028 off
-// instead of 0.0024).  Without it, delta as the sum of P dP over the keys, the walk would be made twice: five products instead of
-// three.  For the key gradients' kernel delta is left without that error: a row's dS add up to 0, so what they do add up to is
-// what delta lacks.
+// more for dQ.  delta comes from the output as it was stored: in bfloat16 its rounding goes into every dS of the row.  Without it, delta as the
+// sum of P dP over the keys, the walk would be made twice: five products instead of three.  Instead the third product is made with what rounding
+// took off dS as well: dQ 0.0019 to 0.0023 off, 0.0025 to 0.0028 with dS rounded to 8 bits, for 286 us instead of 250 on the long batch.
+// For the key gradients' kernel delta is left without that error: a row's dS add up to 0, so what they do add up to is what delta lacks.
 // Bound like the forward kernel.  Fragments are read where they are used: read one product ahead, as in the kernel below, they need more than 256
-// registers (424 to 796 us on the long batch instead of 250).  The bias and its gradient make 64 sequences 29 us long instead of 26.
+// registers (424 to 796 us on the long batch, with the plain third product).
 template <typename T, int D, bool BIAS, bool PAIR> __global__ __launch_bounds__(256, (2 - Rows<T, D>::kWide)) void attn_dq_kernel(RaggedArgs a) {
     typedef Rows<T, D> R;
     extern __shared__ __align__(16) char lds[];
@@ -560,8 +563,10 @@ template <typename T, int D, bool BIAS, bool PAIR> __global__ __launch_bounds__(
                 rest += s[i];
             }
             if constexpr (BIAS) add_distances(s, a, sums + (2 * wave + h) * places, far, near, k0 + key, pos, lane);
+            phase();
             kt.load(step.keys(), key, lane);
-            kt.add(acc, s);
+            kt.add_finely(acc, s);
+            phase();
         }
     }
     for (; k0 < it.k_end; k0 += R::kStep) {  // the other wavefronts' steps

@@ -119,12 +119,29 @@ template <int D> struct AsColumns<bf16_t, D> {
             for (int t = 0; t < R::kTiles; ++t) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(c[s][t], b, acc[t], 0, 0, 0);
         }
     }
+    // with what rounding took off the weights, too: as good as weights of 16 bits
+    __device__ __forceinline__ void add_finely(f32x16* acc, const f32x16& w) const {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            bf16x8 b, rest;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                b[e] = (bf16_t)w[8 * s + e];
+                rest[e] = (bf16_t)(w[8 * s + e] - (float)b[e]);
+            }
+#pragma unroll
+            for (int t = 0; t < R::kTiles; ++t) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(c[s][t], b, acc[t], 0, 0, 0);
+#pragma unroll
+            for (int t = 0; t < R::kTiles; ++t) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(c[s][t], rest, acc[t], 0, 0, 0);
+        }
+    }
 };
 template <int D> struct AsColumns<float, D> {
     typedef Rows<float, D> R;
     const char* p;
     int r, h;
     __device__ __forceinline__ void load(const char* rows, int first, int lane) { p = rows + first * R::kPitch, r = lane & 31, h = lane >> 5; }
+    __device__ __forceinline__ void add_finely(f32x16* acc, const f32x16& w) const { add(acc, w); }
     __device__ __forceinline__ void add(f32x16* acc, const f32x16& w) const {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
