@@ -210,7 +210,7 @@ struct aed_preference {
     aed_preference_config cfg;
     hipStream_t stream = nullptr;
     Arena arena;
-    size_t seq_of, seq_start, gain;
+    size_t seq_of, seq_start, arrived, gain;
     char* ws = nullptr;
     int rows = 0, pairs = 0;
 };
@@ -245,6 +245,7 @@ void lay_out(aed_preference& p, const int32_t* seq_lens, int32_t n_pairs) {
     p.pairs = n_pairs;
     p.seq_of = p.arena.table(of);
     p.seq_start = p.arena.table(start);
+    p.arrived = p.arena.table(std::vector<int32_t>(1, 0));
     p.gain = p.arena.scratch((size_t)p.rows * sizeof(float));
 }
 
@@ -265,6 +266,7 @@ aed_status preference_args(const aed_preference* p, const void* logits, int64_t 
     a.ratio = const_cast<float*>(ratio);
     a.lse = reinterpret_cast<float2*>(const_cast<float*>(lse));
     a.gain = reinterpret_cast<float*>(p->ws + p->gain);
+    a.arrived = reinterpret_cast<int32_t*>(p->ws + p->arrived);
     a.seq_of = reinterpret_cast<const int32_t*>(p->ws + p->seq_of);
     a.seq_start = reinterpret_cast<const int32_t*>(p->ws + p->seq_start);
     a.rows = p->rows;

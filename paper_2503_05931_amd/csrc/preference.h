@@ -14,6 +14,7 @@ struct PreferenceArgs {
     float *loss, *ratio;
     float2* lse;              // [rows]: maximum, log of the sum of exponentials relative to it
     float* gain;              // [rows]: log-probability of the label less the reference's
+    int32_t* arrived;         // workgroups, 0 between calls
     const int32_t* seq_of;    // [rows]
     const int32_t* seq_start;  // [2 pairs + 1]
     const float* d_loss;
