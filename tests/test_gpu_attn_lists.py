@@ -77,3 +77,38 @@ def test_scores_that_grow_or_fall_along_the_keys(slope, rows):
     e = float(66 * most * 2 ** -24)
     assert float(((out - want).abs() - 2 * e * size).max()) <= 5e-6 * float(want.abs().max())
     assert float((lse - want_lse).abs().max()) <= 2 * e
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("head", [64, 128])
+@pytest.mark.parametrize("form", ["whole", "halves", "few", "split", "bias"])
+def test_what_masked_places_hold_does_not_matter(form, head, dtype):
+    """The same bits, whatever masked keys and values are: NaN, infinities, the type's largest."""
+    from paper_2503_05931_amd import training as T
+    n, top, keys, heads = dict(whole=(18, 132, 150, 8), halves=(5, 100, 70, 2), few=(20, 3, 200, 8), split=(4, 70, 1500, 2), bias=(18, 132, 0, 8))[form]
+    q, k = lengths(n, top, max(keys, 1), 3)
+    k = k if keys else q
+    training = form != "split"
+    plan = T.Attention(q, k, heads, head, dtype, causal=form == "bias", bias_buckets=16 if form == "bias" else 0, bias_max_distance=64, training=training)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    rnd = lambda *s: torch.randn(s, generator=g, device="cuda").to(dtype)
+    x, kk, vv, d, bias = rnd(sum(q), heads, head), rnd(sum(k), heads, head), rnd(sum(k), heads, head), rnd(sum(q), heads, head), rnd(16, heads)
+    mask = (torch.rand(sum(k), generator=g, device="cuda") > 0.3).to(torch.uint8)
+    if form == "split":
+        mask[100:700] = 0
+    seen = []
+    for bad in (0.0, float("nan"), float("inf"), -float("inf"), torch.finfo(dtype).max):
+        a, b = kk.clone(), vv.clone()
+        a[mask == 0] = bad
+        b[mask == 0] = bad
+        extra = dict(bias=bias if form == "bias" else None, key_mask=mask)
+        out, lse = plan.aed_attn_forward(x, a, b, **extra)
+        got = [out, lse]
+        if training:
+            got += [t for t in plan.aed_attn_backward(d, x, a, b, out, lse, **extra) if t is not None]
+        seen.append([t.clone() for t in got])
+        assert all(torch.isfinite(t.float()).all() for i, t in enumerate(seen[-1]) if i != 1)
+        assert all(torch.equal(s, t) for s, t in zip(seen[0], seen[-1]))
+        if training:
+            assert (seen[-1][3][mask == 0] == 0).all() and (seen[-1][4][mask == 0] == 0).all()
+    torch.cuda.synchronize()
