@@ -72,9 +72,9 @@ typedef struct aed_rows {
 } aed_rows;
 
 /* Bytes of device workspace for a batch of these lengths.
- * Errors: AED_EINVAL (NULL, struct_size, a negative length or start, batch <
- * 1, heads, flags, a bias that the rule above does not allow, training with
- * k_starts), AED_EUNSUPPORTED (head_dim, buckets or distance above the limits,
+ * Errors: AED_EINVAL (NULL, struct_size, a negative length or start, a start
+ * above 2^38, batch < 1, heads, flags, a bias that the rule above does not
+ * allow, training with k_starts), AED_EUNSUPPORTED (head_dim, buckets or distance above the limits,
  * more than 2^31 - 1 rows, keys or workgroups). */
 aed_status aed_attn_workspace_bytes(const aed_attn_config *cfg, const int32_t *q_lens, const int32_t *k_lens,
                                     const int64_t *k_starts /*or NULL*/, int32_t batch, size_t *bytes);

@@ -38,6 +38,7 @@ template <typename F> aed_status guarded(F f) {
 }
 
 constexpr int64_t kMost = 0x7fffffff;
+constexpr int64_t kMostStart = (int64_t)1 << 38;  // times the bytes between rows (kAttnMaxPitch, 2^24 less a few): below 2^62
 size_t rounded(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Tables that go to the workspace's beginning in one copy, then scratch
@@ -72,7 +73,7 @@ struct aed_attn {
     Arena arena;
     size_t forward, joins, dq, dkv, zeros, bucket_of, bucket_range, part_o, part_ml, delta, part_bias;
     char* ws = nullptr;
-    int64_t k_rows = 0;
+    int64_t k_rows = 0;  // rows that the keys' tensors have: up to the last one that is read
     int span = 0;
 };
 
@@ -101,7 +102,7 @@ aed_status check_attn(const aed_attn_config* c, const int32_t* q_lens, const int
     for (int b = 0; b < batch; ++b) {
         if (q_lens[b] < 0) return fail(AED_EINVAL, "q_lens[%d] = %d", b, q_lens[b]);
         if (k_lens[b] < 0) return fail(AED_EINVAL, "k_lens[%d] = %d", b, k_lens[b]);
-        if (k_starts && k_starts[b] < 0) return fail(AED_EINVAL, "k_starts[%d] is negative", b);
+        if (k_starts && (k_starts[b] < 0 || k_starts[b] > kMostStart)) return fail(AED_EINVAL, "k_starts[%d] is negative or too large", b);
         q_rows += q_lens[b];
         k_rows += k_lens[b];
     }
@@ -122,7 +123,10 @@ void lay_out(aed_attn& p, const int32_t* q_lens, const int32_t* k_lens, const in
     p.plan = aed::plan_attention(q_lens, k_lens, k_starts, batch, c.n_heads, c.n_kv_heads, c.causal != 0, c.training != 0, aed::kAttnRows,
                                  c.dtype == 0 && c.head_dim == 128 ? 0 : aed::kAttnPair, aed::kAttnFew, c.dtype == 1, c.head_dim);  // wide rows have no pairs
     p.k_rows = 0;
-    for (int b = 0; b < batch; ++b) p.k_rows += k_lens[b];
+    for (int b = 0; b < batch; ++b) {
+        if (!k_starts) p.k_rows += k_lens[b];
+        else if (k_lens[b] > 0) p.k_rows = std::max(p.k_rows, k_starts[b] + k_lens[b]);
+    }
     p.forward = p.arena.table(p.plan.forward);
     p.joins = p.arena.table(p.plan.joins);
     p.dq = p.arena.table(p.plan.dq);
