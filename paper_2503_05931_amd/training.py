@@ -250,7 +250,7 @@ class Attention(_Plan):
         return dq, dk, dv, d_bias
 
     def attend(self, q, k, v, bias=None, key_mask=None):
-        """The output, for torch's autograd."""
+        """The output, for torch's autograd (once: second derivatives are refused)."""
         return _autograd()[0].apply(self, q, k, v, bias, key_mask)
 
 
@@ -311,7 +311,7 @@ class Preference(_Plan):
         return d_logits
 
     def loss(self, logits, labels, ref_logp):
-        """The loss, for torch's autograd."""
+        """The loss, for torch's autograd (once: second derivatives are refused)."""
         return _autograd()[1].apply(self, logits, labels, ref_logp)
 
 
@@ -324,6 +324,23 @@ def _autograd():
     if _functions is None:
         import torch
 
+        class Once(torch.autograd.Function):
+            """A gradient that the library made from the other arguments.  It is a constant to autograd, so what would need its own gradient is refused.
+            (torch's once_differentiable does so only where the incoming gradient has a graph: not for a loss's, which is 1.)"""
+
+            @staticmethod
+            def forward(ctx, gradient, *made_from):
+                return gradient.detach()
+
+            @staticmethod
+            def backward(ctx, *_):
+                raise RuntimeError("second derivatives of attention and of the preference loss are not computed")
+
+        def once(gradients, *made_from):
+            if not torch.is_grad_enabled():  # on only under create_graph
+                return gradients
+            return tuple(None if g is None else Once.apply(g, *made_from) for g in gradients)
+
         class Attend(torch.autograd.Function):
             @staticmethod
             def forward(ctx, plan, q, k, v, bias, key_mask):
@@ -335,10 +352,11 @@ def _autograd():
             @staticmethod
             def backward(ctx, d_out):
                 q, k, v, out, lse, bias, key_mask = ctx.saved_tensors
+                given = d_out, q, k, v, bias
                 if d_out.stride(-1) != 1 or d_out.data_ptr() % 16 or any(n * d_out.element_size() % 16 for n in d_out.stride()[:2]):
                     d_out = d_out.contiguous()
-                dq, dk, dv, d_bias = ctx.plan.aed_attn_backward(d_out, q, k, v, out, lse, bias, key_mask)
-                return None, dq, dk, dv, d_bias, None
+                gradients = ctx.plan.aed_attn_backward(d_out, q, k, v, out, lse, bias, key_mask)
+                return None, *once(gradients, *given), None
 
         class Loss(torch.autograd.Function):
             @staticmethod
@@ -351,7 +369,8 @@ def _autograd():
             @staticmethod
             def backward(ctx, d_loss):
                 logits, labels, ratio, lse = ctx.saved_tensors
-                return None, ctx.plan.aed_preference_backward(logits, labels, ratio, lse, d_loss.contiguous()), None, None
+                gradient = ctx.plan.aed_preference_backward(logits, labels, ratio, lse, d_loss.contiguous())
+                return None, *once((gradient,), d_loss, logits), None, None
 
         _functions = Attend, Loss
     return _functions
