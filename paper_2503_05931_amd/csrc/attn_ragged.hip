@@ -529,8 +529,9 @@ template <typename T, int D, bool BIAS, bool PAIR> __global__ __launch_bounds__(
             for (int e = 0; e < 16 / (int)sizeof(T); ++e) delta += to_f32((T)o.c[s][e]) * to_f32((T)d_o.c[s][e]);
         delta = sum_halves(delta);
     }
-    // a row that sees nothing has lse -inf, and none of its keys' bits are set: its weights become 0 by way of the scores
-    const float base = live ? base_of(kLog2e * a.lse[(int64_t)(row0 + r) * a.heads + head]) : 0.f;
+    // a row that sees nothing has lse -inf, and none of its keys' bits are set: its weights become 0 by way of the scores; those of a row that is
+    // not there are 2^-inf, as its scores are the bias, of any size
+    const float base = live ? base_of(kLog2e * a.lse[(int64_t)(row0 + r) * a.heads + head]) : -kNone;
     if constexpr (BIAS) {
         bias_to_lds<T>(a, w, head);
         for (int i = tid; i < 8 * places; i += 256) sums[i] = 0.f;
@@ -544,7 +545,7 @@ template <typename T, int D, bool BIAS, bool PAIR> __global__ __launch_bounds__(
     for (; k0 < mine_end; k0 += R::kStep) {
         step.next();
         step.fetch(k0 + R::kStep);
-        // rows that are not there are all zeros: what they add is too
+        // (rows that are not there have weights of zero without a mask)
         const uint64_t seen = live ? seen_from(step.seen, k0, pos + r, a.causal) : ~0ull;
 #pragma unroll
         for (int u = 0; u < (PAIR ? 1 : R::kStep / 32); ++u) {
