@@ -59,7 +59,10 @@ typedef struct aed_attn_config {
 /* Buckets of a side (all of the table, or half of it): with half = side / 2,
  * distances below half have a bucket each; bucket half + i begins at the first
  * distance n with (n / half)^(side - half) >= (bias_max_distance / half)^i.  A
- * side has 2 buckets or more and bias_max_distance > half. */
+ * side has 2 buckets or more and bias_max_distance > half.
+ * An entry of minus infinity takes its pairs out, as the masks do; finite ones
+ * beyond 2.35e38 in size count as that.  Weights add up to one whatever the
+ * size of a row's bias, forward and backward. */
 
 /* Rows of n_heads (or n_kv_heads) vectors of head_dim elements: element (row,
  * head, c) at data + row * row_stride + head * head_stride + c, strides in

@@ -71,7 +71,7 @@ struct aed_attn {
     hipStream_t stream = nullptr;
     aed::AttnPlan plan;
     Arena arena;
-    size_t forward, joins, dq, dkv, zeros, bucket_of, bucket_range, part_o, part_ml, delta, part_bias;
+    size_t forward, joins, dq, dkv, zeros, bucket_of, bucket_range, part_o, part_ml, delta, large, part_bias;
     char* ws = nullptr;
     int64_t k_rows = 0;  // rows that the keys' tensors have: up to the last one that is read
     int span = 0;
@@ -151,6 +151,7 @@ void lay_out(aed_attn& p, const int32_t* q_lens, const int32_t* k_lens, const in
     p.part_o = p.arena.scratch(part_rows * c.head_dim * sizeof(float));
     p.part_ml = p.arena.scratch(part_rows * sizeof(float2));
     p.delta = p.arena.scratch(c.training ? (size_t)p.plan.q_rows * c.n_heads * sizeof(float) : 0);
+    p.large = p.arena.scratch(c.training && c.bias_buckets ? (size_t)p.plan.q_rows * c.n_heads * sizeof(float2) : 0);
     p.part_bias = p.arena.scratch(c.training ? p.plan.dq.size() * c.n_heads * c.bias_buckets * sizeof(float) : 0);
 }
 
@@ -193,6 +194,7 @@ aed_status common_args(const aed_attn* p, const aed_rows* q, const aed_rows* k, 
     a.bucket_of = reinterpret_cast<const uint8_t*>(p->ws + p->bucket_of);
     a.bucket_range = reinterpret_cast<const int2*>(p->ws + p->bucket_range);
     a.delta = reinterpret_cast<float*>(p->ws + p->delta);
+    a.large = reinterpret_cast<float2*>(p->ws + p->large);
     a.part_o = reinterpret_cast<float*>(p->ws + p->part_o);
     a.part_ml = reinterpret_cast<float2*>(p->ws + p->part_ml);
     a.part_bias = reinterpret_cast<float*>(p->ws + p->part_bias);

@@ -35,6 +35,7 @@ struct RaggedArgs {
     float* delta;            // [rows, heads]: sum over a row of gradient times output
     float* part_o;           // [part, heads, tile rows, D]
     float2* part_ml;         // [part, heads, tile rows]: maximum (of scores times log2 e) and sum
+    float2* large;           // [rows, heads], with a bias, of rows with a large lse: maximum of the scores times log2 e, log2 of the weights' sum
     float* part_bias;        // [item, heads, buckets]
     const RaggedItem* items;
     int n_items;

@@ -46,8 +46,10 @@ struct Seen {
     const uint8_t* mask;  // of the lane's key among the first 64
     int left;             // keys from the lane's on
     uint8_t byte = 1;
-    __device__ __forceinline__ Seen(const RaggedArgs& a, const RaggedItem& it, int first, int lane)
-        : a(a), mask(a.key_mask + it.k_row + first + lane), left(it.k_end - first - lane) {
+    __device__ __forceinline__ Seen(const RaggedArgs& a, const RaggedItem& it, int first, int lane) : a(a) { start(it, first, lane); }
+    __device__ __forceinline__ void start(const RaggedItem& it, int first, int lane) {
+        mask = a.key_mask + it.k_row + first + lane;
+        left = it.k_end - first - lane;
         if (a.key_mask && left > 0) byte = load_global<uint8_t>(mask);
     }
     // the bits of 64 keys; those looked at next time begin `step` keys on
@@ -73,9 +75,15 @@ __device__ __forceinline__ int bias_places(const RaggedArgs& a) { return a.span 
 template <typename T> __device__ __forceinline__ void bias_to_lds(const RaggedArgs& a, float* w, int head) {
     for (int i = threadIdx.x; i < bias_places(a); i += blockDim.x) {
         const int bucket = a.bucket_of[min(max(i - kMargin, 0), a.span - 1)];
-        w[i] = kLog2e * to_f32(load_global<T>(static_cast<const T*>(a.bias) + (int64_t)bucket * a.heads + head));
+        const float b = to_f32(load_global<T>(static_cast<const T*>(a.bias) + (int64_t)bucket * a.heads + head));
+        // a finite entry stays one, times log2 e too: minus infinity is for keys that are not seen
+        w[i] = fabsf(b) < -kNone ? fminf(fmaxf(kLog2e * b, -__FLT_MAX__), __FLT_MAX__) : b;
     }
 }
+// Rows all of whose keys have a large bias, one that is as good as a mask where there are others.  What a float32 of that size is off by is no small
+// part of a weight exp(s - lse): from -1e7 on the weights of such a row are off by whole factors.  The forward kernel is not concerned: its sum is one of its own
+// weights.  The gradients' take maximum and log of the sum apart for rows whose lse is beyond a thousand; up to there it is off by 2^-14.
+__device__ __forceinline__ bool is_large(float lse) { return fabsf(lse) > 1024.f && fabsf(lse) < -kNone; }
 // The place of the first of 32 keys from `key` on and the first of 32 queries from `pos` on
 enum { kTouches, kAllFar, kAllNear };
 __device__ __forceinline__ int bias_region(const RaggedArgs& a, int key, int pos, int& at) {
@@ -250,6 +258,12 @@ template <typename T, int D> struct Steps {
             feed.load(ks, (int)a.k.row, count, to);
             feed.load(vs, (int)a.v.row, count, to + kBuf / 2);
         }
+    }
+    // from the beginning again; everyone is done with the last step, and none is on its way
+    __device__ __forceinline__ void again() {
+        bits.start(it, it.k_begin, lane);
+        buf = 1;
+        fetch(it.k_begin);
     }
     // everyone is done with the step at hand; the one on its way is at hand
     __device__ __forceinline__ void next() {
@@ -500,6 +514,59 @@ template <typename T, int D> __global__ __launch_bounds__(256) void attn_join_ke
 // For the key gradients' kernel delta is left without that error: a row's dS add up to 0, so what they do add up to is what delta lacks.
 // Bound like the forward kernel.  Fragments are read where they are used: read one product ahead, as in the kernel below, they need more than 256
 // registers (424 to 796 us on the long batch, with the plain third product).
+namespace {
+
+// Maximum (times log2 e) and sum of a lane's row, as the forward kernel finds them, in a walk of its own; the first step is on its way, before and after.
+// Rows that are not there have weights that nobody looks at.
+template <typename T, int D, bool PAIR>
+__device__ __forceinline__ float2 top_and_sum(const RaggedArgs& a, const RaggedItem& it, Steps<T, D>& step, const RowFrag<T, D>& q, const float* w, float2* joined,
+                                              int mine_end, int pos, int tile, int wave, int lane) {
+    typedef Rows<T, D> R;
+    const int r = lane & 31, h = lane >> 5;
+    const float scale2 = a.scale * kLog2e;
+    float m = kNone, l = 0.f;
+    for (int k0 = it.k_begin; k0 < it.k_end; k0 += R::kStep) {
+        step.next();
+        step.fetch(k0 + R::kStep);
+        if (k0 >= mine_end) continue;
+        const uint64_t seen = seen_from(step.seen, k0, pos + r, a.causal);
+#pragma unroll 1
+        for (int u = 0; u < (PAIR ? 1 : R::kStep / 32); ++u) {
+            const int key = 32 * (tile + u);
+            f32x16 s;
+            AsRows<T, D> k;
+            k.load(step.keys(), key, lane);
+            k.dot(s, q);
+            finish_scores<true>(s, a, scale2, w, (uint32_t)(seen >> key), k0 + key, pos, r, h);
+            const float top = fmaxf(m, max_of(s)), base = base_of(top);
+            l *= __builtin_amdgcn_exp2f(m - base);
+            m = top;
+            to_weights<true>(s, scale2, base, l);
+        }
+    }
+    auto join = [&](float m2, float l2) {
+        const float top = fmaxf(m, m2), base = base_of(top);
+        l = l * __builtin_amdgcn_exp2f(m - base) + l2 * __builtin_amdgcn_exp2f(m2 - base);
+        m = top;
+    };
+    const u32x2 ms = swap32(m), ls = swap32(l);
+    m = bits_f32(ms[0]), l = bits_f32(ls[0]);
+    join(bits_f32(ms[1]), bits_f32(ls[1]));
+    lds_barrier();
+    if constexpr (PAIR) {  // the two wavefronts with the same rows
+        joined[wave * 64 + lane] = float2{m, l};
+        lds_barrier();
+        const float2 first = joined[(wave & 1) * 64 + lane], second = joined[(wave | 2) * 64 + lane];
+        m = first.x, l = first.y;  // both join them in the same order
+        join(second.x, second.y);
+        lds_barrier();
+    }
+    step.again();
+    return float2{m, l};
+}
+
+}  // namespace
+
 template <typename T, int D, bool BIAS, bool PAIR> __global__ __launch_bounds__(256, (2 - Rows<T, D>::kWide)) void attn_dq_kernel(RaggedArgs a) {
     typedef Rows<T, D> R;
     extern __shared__ __align__(16) char lds[];
@@ -531,16 +598,31 @@ template <typename T, int D, bool BIAS, bool PAIR> __global__ __launch_bounds__(
     }
     // a row that sees nothing has lse -inf, and none of its keys' bits are set: its weights become 0 by way of the scores; those of a row that is
     // not there are 2^-inf, as its scores are the bias, of any size
-    const float base = live ? base_of(kLog2e * a.lse[(int64_t)(row0 + r) * a.heads + head]) : -kNone;
+    const float lse = live ? a.lse[(int64_t)(row0 + r) * a.heads + head] : 0.f, scale2 = a.scale * kLog2e;
+    float base = live ? base_of(kLog2e * lse) : -kNone;
+    const int mine_end = end_of(a, it, count, pos);
+    bool large = false;  // the workgroup has rows with a large lse: scores are taken from `tops`, and `base` is what is left to take away
+    __shared__ float tops[BIAS ? 4 * 32 : 1];
     if constexpr (BIAS) {
         bias_to_lds<T>(a, w, head);
         for (int i = tid; i < 8 * places; i += 256) sums[i] = 0.f;
+        __shared__ int any[4];
+        const bool mine = __ballot(is_large(lse)) != 0;
+        if (lane == 0) any[wave] = mine;
+        lds_barrier();
+        large = __builtin_amdgcn_readfirstlane(any[0] | any[1] | any[2] | any[3]) != 0;
+        if (large) {
+            float2 of = top_and_sum<T, D, PAIR>(a, it, step, q, w, reinterpret_cast<float2*>(lds), mine_end, pos, tile, wave, lane);
+            of = is_large(lse) ? float2{of.x, of.y > 0.f ? __builtin_amdgcn_logf(of.y) : 0.f} : float2{base, 0.f};
+            if (h == 0) tops[wave * 32 + r] = of.x;
+            other_lanes_wrote();
+            base = of.y;
+            if (is_large(lse) && h == 0 && tile == 0) a.large[(int64_t)(row0 + r) * a.heads + head] = of;
+        }
     }
     f32x16 acc[R::kTiles];
     clear<R::kTiles>(acc);
-    const float scale2 = a.scale * kLog2e;
     float far = 0.f, near = 0.f;
-    const int mine_end = end_of(a, it, count, pos);
     int k0 = it.k_begin;
     for (; k0 < mine_end; k0 += R::kStep) {
         step.next();
@@ -558,6 +640,11 @@ template <typename T, int D, bool BIAS, bool PAIR> __global__ __launch_bounds__(
             v.load(step.values(), key, lane);
             v.dot(dp, d_o);
             finish_scores<BIAS>(s, a, scale2, w, (uint32_t)(seen >> key), k0 + key, pos, r, h);
+            if (BIAS && large) {
+                const float top = tops[wave * 32 + r];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = fminf(s[i] - top, 0.f);
+            }
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 s[i] = weight_of<BIAS>(s[i], scale2, base) * (dp[i] - delta);
@@ -645,6 +732,8 @@ template <typename T> __device__ __forceinline__ void reduce_bias(const RaggedAr
 
 }  // namespace
 
+constexpr int kLargeFlags = 4;  // places of LDS
+
 // A workgroup takes 128 keys of a key head, 32 a wavefront (a lane being a key), and walks the query rows of all heads that share it.
 // PAIR: it takes 64 keys, and two wavefronts share 32 of them, each with 32 rows of a step.  Four products to a tile and no sum over
 // workgroups: what heads share is added up here, in order.
@@ -660,7 +749,9 @@ template <typename T, int D, bool SHAPED, bool PAIR> __global__ __launch_bounds_
     static_assert(!PAIR || kRows == 64, "a tile for each of two");
     extern __shared__ __align__(16) char lds[];
     float* const stats = reinterpret_cast<float*>(lds + 2 * kBuf);  // two buffers of [kRows] lse (times log2 e), [kRows] delta
-    float* const w = stats + 4 * kRows;
+    float* const tops = stats + 4 * kRows;                          // two of [kRows], of steps that have rows with a large lse:
+    int* const large = reinterpret_cast<int*>(tops + 2 * kRows);    // whether these have; lse is what is left then to take away
+    float* const w = tops + 2 * kRows + kLargeFlags;
     const int kv_heads = a.heads / a.share;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 31, h = lane >> 5;
     if ((int)blockIdx.x >= a.n_items * kv_heads) {  // behind the keys' workgroups: the bias's gradient
@@ -682,10 +773,29 @@ template <typename T, int D, bool SHAPED, bool PAIR> __global__ __launch_bounds_
             stat = tid < kRows ? -kNone : 0.f;
             if (row < n) {
                 const int64_t at = (int64_t)(it.q_row + q0 + row) * a.heads + head;
-                stat = tid < kRows ? kLog2e * a.lse[at] : a.delta[at];
-                if (stat == kNone) stat = -kNone;
+                stat = tid < kRows ? a.lse[at] : a.delta[at];
             }
         }
+    };
+    auto put_stats = [&](int head, int q0) {
+        if (tid >= 2 * kRows) return;
+        const int to = buf ^ 1;
+        float x = stat;
+        if (tid < kRows) {
+            x = kLog2e * stat;
+            if (x == kNone) x = -kNone;
+            if (SHAPED && a.span) {
+                const bool some = __ballot(is_large(stat)) != 0;
+                if (tid == 0) large[to] = some;
+                if (some) {
+                    float2 of = {x, 0.f};
+                    if (is_large(stat)) of = a.large[(int64_t)(it.q_row + q0 + tid) * a.heads + head];
+                    tops[to * kRows + tid] = of.x;
+                    x = of.y;
+                }
+            }
+        }
+        stats[to * 2 * kRows + tid] = x;
     };
     if (it.k_begin < it.k_end) {
         feed.load(a.q.p + (int64_t)(it.q_row + it.k_begin) * a.q.row + head * a.q.head, (int)a.q.row, it.k_end - it.k_begin, 0);
@@ -707,7 +817,7 @@ template <typename T, int D, bool SHAPED, bool PAIR> __global__ __launch_bounds_
             bias_to_lds<T>(a, w, head);
         }
         for (int q0 = it.k_begin; q0 < it.k_end; q0 += kRows) {
-            if (tid < 2 * kRows) stats[(buf ^ 1) * 2 * kRows + tid] = stat;
+            put_stats(head, q0);
             loads_done_barrier();
             buf ^= 1;
             int next_q = q0 + kRows, next_head = head;
@@ -738,6 +848,7 @@ template <typename T, int D, bool SHAPED, bool PAIR> __global__ __launch_bounds_
             const char* const gs = qs + kBuf / 2;
             const float* const row_lse = stats + buf * 2 * kRows;
             const float* const row_delta = row_lse + kRows;
+            const int some_large = SHAPED && a.span ? large[buf] : 0;
             // each product's fragments are requested one product ahead
             AsRows<T, D> qr;
             qr.load(qs, 32 * half, lane);
@@ -762,7 +873,13 @@ template <typename T, int D, bool SHAPED, bool PAIR> __global__ __launch_bounds_
                 if constexpr (SHAPED) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) p[i] *= scale2;
-                    if (a.span) add_bias<-1>(p, a, w, key0, first, r, h);
+                    if (a.span) {
+                        add_bias<-1>(p, a, w, key0, first, r, h);
+                        if (__builtin_amdgcn_readfirstlane(some_large)) {
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) p[i] = fminf(p[i] - tops[buf * kRows + row + 8 * (i >> 2) + 4 * h + (i & 3)], 0.f);
+                        }
+                    }
                     if (a.causal && first < key0 + 31) {  // rows before `last` do not see the lane's key
                         const int last = key0 + r - first - 4 * h;
 #pragma unroll
@@ -898,7 +1015,7 @@ hipError_t launch_attn_dkv(const RaggedArgs& a, int head_dim, bool bf16, int til
         constexpr int D = decltype(d)::value;
         constexpr bool S = decltype(shaped)::value;
         static DeviceOnce once_pair, once_many;
-        const size_t lds = 2 * Steps<T, D>::kBuf + 4 * Rows<T, D>::kStep * sizeof(float) + (S ? bias_bytes(a) : 0);
+        const size_t lds = 2 * Steps<T, D>::kBuf + (6 * Rows<T, D>::kStep + kLargeFlags) * sizeof(float) + (S ? bias_bytes(a) : 0);
         if constexpr (!Rows<T, D>::kWide)
             if (tile_keys == kAttnPair) return launch(attn_dkv_kernel<T, D, S, true>, once_pair, blocks, lds, a, s);
         return launch(attn_dkv_kernel<T, D, S, false>, once_many, blocks, lds, a, s);

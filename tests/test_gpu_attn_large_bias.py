@@ -1,7 +1,8 @@
 """Bias tables whose entries are large: weights stay weights, forward and backward, whatever the size of a row's scores.
 
-Bounds.  u = 2^-24.  A score is a product of head_dim terms and one rounding at its own size S, its exponent two more; so a weight is off by
-e = 2 u (head_dim P + 6 S) of itself, P the largest sum of |q_c k_c| times the scale.  Rows whose scores are beyond a thousand have queries of zeros
+Bounds.  u = 2^-24.  A score is a product of head_dim terms and one rounding at its own size S, its exponent two more; the weights' sum is one of n
+terms, its logarithm, of size log2 n, is good to an ulp, and so are the weight's power of two and its product: a weight is off by
+e = 2 u (head_dim P + 6 S + log2 n + 3) + n u of itself, P the largest sum of |q_c k_c| times the scale.  Rows whose scores are beyond a thousand have queries of zeros
 here: their scores are table entries, exactly, and S does not enter.  What is made of the weights is off by as much of the same formulas with magnitudes in
 the place of numbers, and by u for each of the terms that are added up.  bfloat16: 2^-8 more for the weights, the output in delta, and the result.
 """
@@ -40,7 +41,7 @@ def expected(x, q_lens, k_lens, dtype, causal, max_distance, bidirectional):
             s = torch.where(seen, q[qs, h] @ k[ks, g].T * scale + w[place, h], torch.full((), -math.inf, dtype=torch.float64))
             top = s.max(1, keepdim=True).values if nk else torch.full((nq, 1), -math.inf, dtype=torch.float64)
             size = torch.where(top.abs() < 1e3, top.abs() + 30, torch.zeros(()))  # (what is 30 below the top has no weight)
-            e = 2 * u * (D * scale * (q[qs, h].abs() @ k[ks, g].abs().T).amax(1, keepdim=True) + 6 * size) if nk else top
+            e = 2 * u * (D * scale * (q[qs, h].abs() @ k[ks, g].abs().T).amax(1, keepdim=True) + 6 * size + math.log2(nk) + 3) + nk * u if nk else top
             p = torch.exp(s - torch.where(top == -math.inf, 0.0, top))
             total = p.sum(1, keepdim=True)
             p = p / torch.where(total == 0, 1.0, total)
@@ -99,3 +100,75 @@ def test_a_constant_of_a_hundred(lens, causal, bidirectional, heads, kv_heads, h
     x = make(lens, lens, heads, kv_heads, head, dtype, buckets=8, seed=21)
     x["bias"] = (x["bias"] + 100).to(TYPE[dtype])
     check(x, lens, lens, dtype, causal, 20, bidirectional)
+
+
+def whole(x, value):
+    """The same entry for all distances; queries of zeros: a row's scores are equal."""
+    x["bias"][:] = value
+    x["q"][:] = 0
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("heads,kv_heads,head", [(2, 2, 64), (4, 2, 128)])
+@pytest.mark.parametrize("causal,bidirectional", FORMS)
+@pytest.mark.parametrize("value", ["lowest", "largest", -1e9, -1e6, 3e4])
+def test_rows_that_see_a_large_bias_only(value, causal, bidirectional, heads, kv_heads, head, dtype):
+    """Every key of a row has the same large bias: equal weights that add up to one, and their gradients."""
+    q_lens, k_lens = [70, 1, 150], [70, 40, 130]
+    value = {"lowest": torch.finfo(TYPE[dtype]).min, "largest": torch.finfo(TYPE[dtype]).max}.get(value, value)
+    x = make(q_lens, k_lens, heads, kv_heads, head, dtype, buckets=8, masked=0.2, seed=22)
+    whole(x, value)
+    check(x, q_lens, k_lens, dtype, causal, 20, bidirectional)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("heads,kv_heads,head", [(2, 2, 64), (4, 2, 128)])
+@pytest.mark.parametrize("causal,bidirectional", FORMS)
+@pytest.mark.parametrize("value", ["lowest", -1e9])
+@pytest.mark.parametrize("many", [False, True])
+def test_a_bucket_as_good_as_masked(many, value, causal, bidirectional, heads, kv_heads, head, dtype):
+    """The bucket of the query's own place has a value that no other key's weight survives beside, and rows that see no other key: the first of a causal
+    sequence, the first of a sequence whose keys behind the query share that bucket, and rows whose other keys are masked."""
+    lens = [90, 1, 2, 64, 133] + [131, 140, 5, 64] * (9 if many else 0)  # many: whole items, not halves
+    x = make(lens, lens, heads, kv_heads, head, dtype, buckets=8, seed=23)
+    x["bias"][0] = torch.finfo(TYPE[dtype]).min if value == "lowest" else value
+    if bidirectional:
+        x["bias"][4] = x["bias"][0]
+    x["key_mask"] = torch.ones(sum(lens), dtype=torch.uint8)
+    x["key_mask"][20:70] = 0
+    x["key_mask"][:12] = 0  # causal: rows up to the 20th see keys 12 on, rows 12 itself only
+    at = 0
+    for n in lens:  # rows that see keys of that bucket only have scores that are equal
+        far = torch.arange(n)[:, None] - torch.arange(n)[None, :]
+        seen = (far >= 0 if causal else torch.ones((n, n), dtype=torch.bool)) & (x["key_mask"][at:at + n] != 0)[None, :]
+        other = seen & ((far != 0) if bidirectional or causal else far > 0)
+        x["q"][at:at + n][~other.any(1)] = 0
+        at += n
+    check(x, lens, lens, dtype, causal, 20, bidirectional)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("head", [64, 128])
+@pytest.mark.parametrize("q_lens,k_lens", [([1, 1, 1], [5, 300, 64]), ([3, 16], [40, 200]), ([40, 100], [1500, 1100]), ([1], [5000])], ids=str)
+def test_equal_scores_in_the_other_forms(q_lens, k_lens, head, dtype):
+    """Few rows, split keys: the mean of the values, and its lse."""
+    from paper_2503_05931_amd import training as T
+    x = make(q_lens, k_lens, 2, 2, head, dtype, buckets=8, masked=0.2, seed=24)
+    whole(x, torch.finfo(TYPE[dtype]).min)
+    plan = T.Attention(q_lens, k_lens, 2, head, TYPE[dtype], bias_buckets=8, bias_max_distance=20, training=False)
+    d = dev(x)
+    got = plan.aed_attn_forward(d["q"], d["k"], d["v"], bias=d["bias"], key_mask=d["key_mask"])
+    want = expected(x, q_lens, k_lens, dtype, False, 20, False)
+    for n, g in zip(("out", "lse"), got):
+        g = g.double().cpu()
+        same = (g == want[n][0]) | ((g - want[n][0]).abs() <= want[n][1])
+        assert bool(same.all()), (n, g[~same][:4], want[n][0][~same][:4])
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_minus_infinity_is_not_seen(dtype):
+    """An entry of minus infinity takes its pairs out: rows that see no others are rows that see nothing."""
+    lens = [50, 33]
+    x = make(lens, lens, 2, 2, 64, dtype, buckets=8, seed=25)
+    x["bias"][0] = -math.inf
+    check(x, lens, lens, dtype, True)
