@@ -78,7 +78,9 @@ typedef struct aed_rows {
  * Errors: AED_EINVAL (NULL, struct_size, a negative length or start, a start
  * above 2^38, batch < 1, heads, flags, a bias that the rule above does not
  * allow, training with k_starts), AED_EUNSUPPORTED (head_dim, buckets or distance above the limits,
- * more than 2^31 - 1 rows, keys or workgroups). */
+ * more than 2^31 - 1 rows or keys, more than 2^24 - 1 workgroups in a launch:
+ * items of 128 rows or keys of a sequence, 64 in small batches, 32 where no
+ * sequence has more rows, times heads). */
 aed_status aed_attn_workspace_bytes(const aed_attn_config *cfg, const int32_t *q_lens, const int32_t *k_lens,
                                     const int64_t *k_starts /*or NULL*/, int32_t batch, size_t *bytes);
 
@@ -125,7 +127,7 @@ typedef struct aed_preference_config {
 } aed_preference_config;
 
 /* seq_lens: HOST int32[2 n_pairs], rows of every sequence, 0 or more.
- * Errors: AED_EINVAL, AED_EUNSUPPORTED (more than 2^31 - 1 rows). */
+ * Errors: AED_EINVAL, AED_EUNSUPPORTED (more than 2^26 - 4 rows). */
 aed_status aed_preference_workspace_bytes(const aed_preference_config *cfg, const int32_t *seq_lens, int32_t n_pairs, size_t *bytes);
 aed_status aed_preference_create(const aed_preference_config *cfg, const int32_t *seq_lens, int32_t n_pairs, void *workspace,
                                  size_t workspace_bytes, void *hip_stream, aed_preference **out);

@@ -112,16 +112,16 @@ aed_status check_attn(const aed_attn_config* c, const int32_t* q_lens, const int
         if (q_lens[b] > (1 << 30) || k_lens[b] > (1 << 30)) return fail(AED_EUNSUPPORTED, "a length above 2^30");
     if (q_rows > kMost || k_rows > kMost) return fail(AED_EUNSUPPORTED, "more than 2^31 - 1 query rows or keys");
     if (c->n_heads > 65535) return fail(AED_EUNSUPPORTED, "more than 65535 heads");
-    // a bound on the work items of any list, before any of them is made
-    const int64_t items = std::max(q_rows, k_rows) / aed::kAttnFew + batch + aed::kPlanMost;  // (one of few rows at the least)
-    if (items * c->n_heads > kMost) return fail(AED_EUNSUPPORTED, "more than 2^31 - 1 workgroups");
     return AED_OK;
 }
 
-void lay_out(aed_attn& p, const int32_t* q_lens, const int32_t* k_lens, const int64_t* k_starts, int32_t batch) {
+aed_status lay_out(aed_attn& p, const int32_t* q_lens, const int32_t* k_lens, const int64_t* k_starts, int32_t batch) {
     const aed_attn_config& c = p.cfg;
     p.plan = aed::plan_attention(q_lens, k_lens, k_starts, batch, c.n_heads, c.n_kv_heads, c.causal != 0, c.training != 0, aed::kAttnRows,
                                  c.dtype == 0 && c.head_dim == 128 ? 0 : aed::kAttnPair, aed::kAttnFew, c.dtype == 1, c.head_dim);  // wide rows have no pairs
+    const int64_t reduce = c.training ? ((int64_t)c.bias_buckets * c.n_heads + 3) / 4 : 0;  // workgroups of the bias's gradient, in the launch of the keys'
+    if (std::max(p.plan.forward_groups, std::max(p.plan.dq_groups, p.plan.dkv_groups + reduce)) > aed::kPlanGrid)
+        return fail(AED_EUNSUPPORTED, "more than 2^24 - 1 workgroups in a launch");
     p.k_rows = 0;
     for (int b = 0; b < batch; ++b) {
         if (!k_starts) p.k_rows += k_lens[b];
@@ -153,6 +153,7 @@ void lay_out(aed_attn& p, const int32_t* q_lens, const int32_t* k_lens, const in
     p.delta = p.arena.scratch(c.training ? (size_t)p.plan.q_rows * c.n_heads * sizeof(float) : 0);
     p.large = p.arena.scratch(c.training && c.bias_buckets ? (size_t)p.plan.q_rows * c.n_heads * sizeof(float2) : 0);
     p.part_bias = p.arena.scratch(c.training ? p.plan.dq.size() * c.n_heads * c.bias_buckets * sizeof(float) : 0);
+    return AED_OK;
 }
 
 // rows: how many the tensor has
@@ -237,7 +238,7 @@ aed_status check_preference(const aed_preference_config* c, const int32_t* seq_l
         if (seq_lens[i] < 0) return fail(AED_EINVAL, "seq_lens[%d] = %d", i, seq_lens[i]);
         rows += seq_lens[i];
     }
-    if (rows > kMost - 4) return fail(AED_EUNSUPPORTED, "more than 2^31 - 5 rows");
+    if (rows > 4 * aed::kPlanGrid) return fail(AED_EUNSUPPORTED, "more than 2^26 - 4 rows");  // four to a workgroup
     return AED_OK;
 }
 
@@ -314,11 +315,11 @@ aed_status aed_attn_workspace_bytes(const aed_attn_config* cfg, const int32_t* q
                                     size_t* bytes) {
     return guarded([&] {
         if (!bytes) return fail(AED_EINVAL, "bytes is NULL");
-        const aed_status st = check_attn(cfg, q_lens, k_lens, k_starts, batch);
+        aed_status st = check_attn(cfg, q_lens, k_lens, k_starts, batch);
         if (st != AED_OK) return st;
         aed_attn p;
         p.cfg = *cfg;
-        lay_out(p, q_lens, k_lens, k_starts, batch);
+        if ((st = lay_out(p, q_lens, k_lens, k_starts, batch)) != AED_OK) return st;
         *bytes = p.arena.total;
         return AED_OK;
     });
@@ -329,15 +330,19 @@ aed_status aed_attn_create(const aed_attn_config* cfg, const int32_t* q_lens, co
     return guarded([&] {
         if (!out) return fail(AED_EINVAL, "out is NULL");
         *out = nullptr;
-        const aed_status st = check_attn(cfg, q_lens, k_lens, k_starts, batch);
+        aed_status st = check_attn(cfg, q_lens, k_lens, k_starts, batch);
         if (st != AED_OK) return st;
         aed_attn* p = new aed_attn;
         try {
             p->cfg = *cfg;
-            lay_out(*p, q_lens, k_lens, k_starts, batch);
+            st = lay_out(*p, q_lens, k_lens, k_starts, batch);
         } catch (...) {
             delete p;
             throw;
+        }
+        if (st != AED_OK) {
+            delete p;
+            return st;
         }
         return start(p, workspace, workspace_bytes, hip_stream, out);
     });

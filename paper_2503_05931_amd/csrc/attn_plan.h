@@ -14,6 +14,7 @@ constexpr int kPlanSlots = 512;
 constexpr int kPlanLong = 1024;  // keys from which on a row's may be split
 constexpr int kPlanPart = 256;   // keys of a part at the least
 constexpr int kPlanMost = 4 * kPlanSlots;  // workgroups up to which splitting is looked at
+constexpr int64_t kPlanGrid = 0xffffffffll / 256;  // workgroups of 256 that a launch may have: its threads are counted in 32 bits
 
 // First distances of a side's logarithmic buckets, half + 1 on: the smallest n with (n / half)^(side - half) >= (max / half)^i.
 // The power is irrational but where it is a whole number, which rounding must not miss.
@@ -84,6 +85,7 @@ struct AttnPlan {
     std::vector<PlanItem> forward, dq, dkv;
     std::vector<PlanJoin> joins;
     int64_t q_rows = 0;
+    int64_t forward_groups = 0, dq_groups = 0, dkv_groups = 0;  // workgroups of unsplit lists; above kPlanGrid in any of them there are no lists
 };
 
 // tile_many, tile_pair (0: there are none), tile_few: query rows of an item, tile_many and tile_pair also keys of one of key gradients
@@ -112,6 +114,14 @@ inline AttnPlan plan_attention(const int32_t* q_lens, const int32_t* k_lens, con
     const bool split = most_keys >= kPlanLong;
     if (tile_pair ? most <= tile_few / 2 && !split : most <= tile_few) p.tile_rows = tile_few;
     else p.tile_rows = split && most > tile_pair ? tile_many : p.dq_rows;
+    auto count = [&](const int32_t* lens, int tile) {
+        int64_t n = 0;
+        for (int b = 0; b < batch; ++b) n += (lens[b] + (int64_t)tile - 1) / tile;
+        return n;
+    };
+    p.forward_groups = count(q_lens, p.tile_rows) * heads;
+    if (training) p.dq_groups = count(q_lens, p.dq_rows) * heads, p.dkv_groups = count(k_lens, p.dkv_keys) * kv_heads;
+    if (std::max(p.forward_groups, std::max(p.dq_groups, p.dkv_groups)) > kPlanGrid) return p;
     const int step = p.tile_rows == tile_few ? 128 : 64;  // keys that a workgroup takes at once
     std::vector<PlanItem> whole;
     int64_t q_row = 0, packed = 0;
