@@ -39,6 +39,7 @@ template <typename F> aed_status guarded(F f) {
 
 constexpr int64_t kMost = 0x7fffffff;
 constexpr int64_t kMostStart = (int64_t)1 << 38;  // times the bytes between rows (kAttnMaxPitch, 2^24 less a few): below 2^62
+constexpr int64_t kMostStride = (int64_t)1 << 38;  // elements; in bytes and times the heads (2^16) below 2^57
 size_t rounded(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Tables that go to the workspace's beginning in one copy, then scratch
@@ -166,7 +167,7 @@ aed_status to_tensor(const aed_rows* t, const char* name, int64_t rows, int head
     if ((uintptr_t)t->data % 16 != 0) return fail(AED_EINVAL, "%s is not aligned to 16 bytes", name);
     const int64_t strides[2] = {rows > 1 ? t->row_stride : 0, heads > 1 ? t->head_stride : 0};
     for (int i = 0; i < 2; ++i) {
-        if (strides[i] < 0 || strides[i] > (INT64_MAX >> 36)) return fail(AED_EINVAL, "%s: a stride is negative or too large", name);
+        if (strides[i] < 0 || strides[i] > kMostStride) return fail(AED_EINVAL, "%s: a stride is negative or above 2^38", name);
         if (strides[i] * es % 16 != 0) return fail(AED_EINVAL, "%s: a stride of %lld elements is no multiple of 16 bytes", name, (long long)strides[i]);
         if (output && (i == 0 ? rows : heads) > 1 && strides[i] < head_dim) return fail(AED_EINVAL, "%s: rows or heads of an output overlap", name);
     }

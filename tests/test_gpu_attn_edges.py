@@ -25,3 +25,38 @@ def test_one_key_in_the_whole_batch(k_lens, slots, rows, heads, kv_heads, head, 
     x["key_mask"] = torch.ones(6 * capacity, dtype=torch.uint8)
     x["key_mask"][0] = 0
     check(x, q_lens, k_lens, dtype, k_starts=slots * capacity, training=False)
+
+
+def apart(t, row, head):
+    """A copy of [rows, heads, D] with these strides; what lies between holds anything."""
+    rows, heads, _ = t.shape
+    place = torch.empty((rows - 1) * row + (heads - 1) * head + t.shape[2], dtype=t.dtype, device="cuda")
+    far = place.as_strided(t.shape, (row, head, 1))
+    far.copy_(t)
+    return far
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("head_stride", [(1 << 27) + 8, (1 << 30) + 64])
+def test_heads_far_apart(head_stride, dtype):
+    """Heads outermost, as in a tensor of a million rows or more: byte offsets past 32 bits."""
+    lens = [33, 40]
+    x = make(lens, lens, 2, 2, 64, dtype, seed=26)
+    d = {n: None if t is None else apart(t.cuda(), 64, head_stride) if t.dim() == 3 else t.cuda() for n, t in x.items()}
+    check(x, lens, lens, dtype, causal=True, on=d)
+
+
+@pytest.mark.parametrize("rows", [1, 40])
+def test_a_cache_past_32_bits(rows):
+    """Slots 2^25 rows into a cache: 4.3 GB from its beginning."""
+    slot, k_lens = 1 << 25, [200, 1]
+    starts = np.array([slot, slot + 300])
+    x = make([rows] * 2, k_lens, 2, 2, 64, "bf16", seed=27, k_rows=501)
+    d = {n: None if t is None else t.cuda() for n, t in x.items()}
+    for n in ("k", "v"):
+        wide = torch.empty((slot + 501, 2, 64), dtype=torch.bfloat16, device="cuda")
+        wide[slot:] = d[n]
+        d[n] = wide
+    from paper_2503_05931_amd import training as T
+    plan = T.Attention([rows] * 2, k_lens, 2, 64, torch.bfloat16, k_starts=starts, training=False)
+    check(x, [rows] * 2, k_lens, "bf16", k_starts=starts - slot, training=False, plan=plan, on=d)
