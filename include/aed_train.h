@@ -68,7 +68,8 @@ typedef struct aed_attn_config {
  * head, c) at data + row * row_stride + head * head_stride + c, strides in
  * elements.  DEVICE pointer, aligned to 16 bytes, strides multiples of 16
  * bytes, not negative and at most 2^38 (0 in an input: the same vector for
- * all), rows less than 16 MiB apart (else AED_EUNSUPPORTED).  A part of a wider product's result is given by its strides, without a copy. */
+ * all; vectors of an output share no element), rows less than 16 MiB apart
+ * (else AED_EUNSUPPORTED).  A part of a wider product's result is given by its strides, without a copy. */
 typedef struct aed_rows {
     void *data;
     int64_t row_stride, head_stride;

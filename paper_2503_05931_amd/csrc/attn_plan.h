@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstdlib>
 #include <vector>
 
 namespace aed {
@@ -39,6 +40,16 @@ inline std::vector<uint8_t> bucket_places(int buckets, int max_distance, bool bi
         of.push_back((uint8_t)(b + (at > max_distance ? side : 0)));
     }
     return of;
+}
+
+// Whether two of rows x heads vectors of `length` elements, `row` and `head` elements apart, share one.  Strides are not negative.
+inline bool vectors_overlap(int64_t rows, int64_t row, int64_t heads, int64_t head, int64_t length) {
+    if ((rows > 1 && row < length) || (heads > 1 && head < length)) return true;
+    if (rows <= 1 || heads <= 1 || row >= (heads - 1) * head + length || head >= (rows - 1) * row + length) return false;  // one inside the other's gaps
+    for (int64_t h = 1; h < heads; ++h)  // the rows whose first vectors are next to head h of row 0
+        for (int64_t r = h * head / row; r <= h * head / row + 1; ++r)
+            if (r >= 1 && r < rows && std::abs(r * row - h * head) < length) return true;
+    return false;
 }
 
 struct PlanItem {  // RaggedItem's fields

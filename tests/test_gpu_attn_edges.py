@@ -60,3 +60,20 @@ def test_a_cache_past_32_bits(rows):
     from paper_2503_05931_amd import training as T
     plan = T.Attention([rows] * 2, k_lens, 2, 64, torch.bfloat16, k_starts=starts, training=False)
     check(x, [rows] * 2, k_lens, "bf16", k_starts=starts - slot, training=False, plan=plan, on=d)
+
+
+def test_outputs_whose_vectors_share_elements_are_refused():
+    import ctypes as C
+    from paper_2503_05931_amd import binding, training as T
+    x = make([3, 4], [3, 4], 2, 2, 64, "bf16", seed=28)
+    d = {n: t.cuda() for n, t in x.items() if t is not None}
+    plan = T.Attention([3, 4], [3, 4], 2, 64, torch.bfloat16, training=False)
+    out, lse = plan.aed_attn_forward(d["q"], d["k"], d["v"])
+    wide = torch.zeros(7 * 512, dtype=torch.bfloat16, device="cuda")
+    rows = [T.AedRows(d[n].data_ptr(), 128, 64) for n in ("q", "k", "v")]
+    for row, head, status in ((64, 64, binding.AED_EINVAL), (128, 128, binding.AED_EINVAL), (128, 96, binding.AED_EINVAL), (64, 448, 0), (128, 64, 0), (512, 72, 0)):
+        to = T.AedRows(wide.data_ptr(), row, head)
+        assert plan.lib.aed_attn_forward(plan.handle, *rows, None, None, to, C.c_void_p(lse.data_ptr())) == status, (row, head)
+        torch.cuda.synchronize()
+        if status == 0:
+            assert torch.equal(wide.as_strided((7, 2, 64), (row, head, 1)), out)
