@@ -116,7 +116,7 @@ class _Plan:
         except Exception:
             pass
 
-    # inputs come from torch's current stream, and what follows there uses the results
+    # inputs come from torch's current stream, and what follows there uses the results; of a call that fails, the memory that they were to have
     def _enter(self):
         if not self.handle and self._destroy:
             raise _b.AedError(_b.AED_ESTATE, "the plan is closed")
@@ -219,10 +219,10 @@ class Attention(_Plan):
         at[3].data = out.data_ptr()
         current = self._enter()
         status = self.lib.aed_attn_forward(self.handle, at[0], at[1], at[2], pb, pm, at[3], lse.data_ptr())
-        if status:
-            _check(status)
         if current is not None:
             self._exit(current)
+        if status:
+            _check(status)
         return out, lse
 
     def aed_attn_backward(self, d_out, q, k, v, out, lse, bias=None, key_mask=None):
@@ -243,10 +243,10 @@ class Attention(_Plan):
         current = self._enter()
         status = self.lib.aed_attn_backward(self.handle, at[5], at[0], at[1], at[2], at[4], plse, pb, pm, at[3], at[6], at[7],
                                             None if d_bias is None else d_bias.data_ptr())
-        if status:
-            _check(status)
         if current is not None:
             self._exit(current)
+        if status:
+            _check(status)
         return dq, dk, dv, d_bias
 
     def attend(self, q, k, v, bias=None, key_mask=None):
@@ -286,10 +286,10 @@ class Preference(_Plan):
         loss, ratio, lse = new(()), new(2 * self.pairs), new((self.rows, 2))
         current = self._enter()
         status = self.lib.aed_preference_forward(self.handle, pz, stride, py, pr, loss.data_ptr(), ratio.data_ptr(), lse.data_ptr())
-        if status:
-            _check(status)
         if current is not None:
             self._exit(current)
+        if status:
+            _check(status)
         return loss, ratio, lse
 
     def aed_preference_backward(self, logits, labels, ratio, lse, d_loss=None, d_logits=None):
@@ -304,10 +304,10 @@ class Preference(_Plan):
         pg, g_stride = self._logits(d_logits, "d_logits")
         current = self._enter()
         status = self.lib.aed_preference_backward(self.handle, pz, stride, py, pr, pl, pd, pg, g_stride)
-        if status:
-            _check(status)
         if current is not None:
             self._exit(current)
+        if status:
+            _check(status)
         return d_logits
 
     def loss(self, logits, labels, ref_logp):
