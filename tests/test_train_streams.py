@@ -47,7 +47,7 @@ def plan(kind, monkeypatch, **kw):
     p.stream, p.raw, p.index = Stream(rec, 5), 5, -1
     p._f32 = torch.empty(0)
     p._raw_stream = lambda index: rec.stream
-    p._get_device = lambda: rec.device
+    p._get_device, p._only = lambda: rec.device, False
     monkeypatch.setattr(T, "_lib", lambda: types.SimpleNamespace(aed_train_last_error=lambda: b"a launch failed"))
     return p, rec
 
@@ -110,3 +110,20 @@ def test_the_plans_own_stream_waits_for_nothing(make, call, monkeypatch):
     call(p)
     assert rec.done == [("call", -1)]
 
+
+@pytest.mark.parametrize("make,call", CALLS)
+@pytest.mark.parametrize("status", [0, -4])
+@pytest.mark.parametrize("stream", [5, 7])
+def test_calls_are_made_on_the_plans_device(make, call, status, stream, monkeypatch):
+    """Another device is current: the default stream's number is the same on all, and would be that device's."""
+    p, rec = make(monkeypatch, status=status, device=0, stream=stream)
+    if status:
+        with pytest.raises(binding.AedError):
+            call(p)
+    else:
+        call(p)
+    assert ("call", -1) in rec.done and rec.device == 0
+    p.close()
+    assert rec.done[-1] == ("destroy", -1) and rec.device == 0
+    with pytest.raises(binding.AedError):
+        call(p)
