@@ -8,8 +8,8 @@
 // Exponentials are powers of two: scores and bias carry log2 e.  Scores, softmax and sums are float32.  In bfloat16 the weights P and dS are
 // rounded, where they become an operand of the second product: that product then runs at 16 times the float32 instructions' rate.  It costs
 // as much as the rounding of the result itself does: outputs that are off by 0.0017 (2-norm, relative) from rounding alone are off by 0.0018 to
-// 0.0020, dK and dV by 0.0024.  dQ has the error of delta besides (see there), so its weights are rounded to 16 bits, a sum of two bfloat16: 0.0019
-// to 0.0023.  dw, sums of float32 dS with that error, is off by up to 0.0028.  No result depends on timing: whatever is added up has one
+// 0.0020, dK and dV by 0.0024.  dQ's weights are rounded to 16 bits, a sum of two bfloat16, as it may have an error of delta besides (see there): 0.0017
+// to 0.0018.  dw, sums of float32 dS, has its own rounding only.  No result depends on timing: whatever is added up has one
 // order, and there are no atomics between wavefronts.
 //
 // Times in this file are the kernels' on an MI355X, bfloat16, 8 heads of 128, for the gradients' lists of four batches:
@@ -242,6 +242,7 @@ template <typename T, int D> struct Steps {
     Seen bits;
     uint64_t seen = 0, seen_next = 0;  // of the step at hand and of the one on its way
     int buf = 1;
+    bool there = false;  // all of the walk is in LDS
     __device__ __forceinline__ Steps(const RaggedArgs& a, const RaggedItem& it, int kv_head, char* lds, int wave, int lane)
         : a(a), it(it), kp(a.k.p + it.k_row * a.k.row + kv_head * a.k.head), vp(a.v.p + it.k_row * a.v.row + kv_head * a.v.head), lds(lds), lane(lane),
           feed(lds, wave, lane), bits(a, it, it.k_begin, lane) {}
@@ -250,6 +251,7 @@ template <typename T, int D> struct Steps {
         if (k0 >= it.k_end) return;
         const int count = it.k_end - k0, to = (buf ^ 1) * kBuf;
         seen_next = a.key_mask ? bits.next(R::kStep) : count >= 64 ? ~0ull : (1ull << count) - 1;
+        if (there) return;
         const char *ks = kp + k0 * a.k.row, *vs = vp + k0 * a.v.row;
         if (a.key_mask && (seen_next & R::kAll) != R::kAll) {
             feed.load_seen(ks, (int)a.k.row, seen_next, a.zeros, to);
@@ -259,10 +261,11 @@ template <typename T, int D> struct Steps {
             feed.load(vs, (int)a.v.row, count, to + kBuf / 2);
         }
     }
-    // from the beginning again; everyone is done with the last step, and none is on its way
-    __device__ __forceinline__ void again() {
+    // from the beginning again; everyone is done with the last step, and none is on its way.  whole: both buffers still hold a walk of two steps
+    __device__ __forceinline__ void again(bool whole) {
         bits.start(it, it.k_begin, lane);
         buf = 1;
+        there = whole;
         fetch(it.k_begin);
     }
     // everyone is done with the step at hand; the one on its way is at hand
@@ -508,10 +511,15 @@ template <typename T, int D> __global__ __launch_bounds__(256) void attn_join_ke
 
 // ---------------------------------------------------------------- query gradients, delta, and the bias's
 // The forward kernel's walk with two products to a tile of scores (K Q^T and V dO^T, transposed, a lane being a query) and one
-// more for dQ.  delta comes from the output as it was stored: in bfloat16 its rounding goes into every dS of the row.  Without it, delta as the
-// sum of P dP over the keys, the walk would be made twice: five products instead of three.  Instead the third product is made with what rounding
-// took off dS as well: dQ 0.0019 to 0.0023 off, 0.0025 to 0.0028 with dS rounded to 8 bits, for 286 us instead of 250 on the long batch.
-// For the key gradients' kernel delta is left without that error: a row's dS add up to 0, so what they do add up to is what delta lacks.
+// more for dQ, which in bfloat16 is made with what rounding took off dS as well (250 us instead of 286 on the long batch without it).
+// delta: from the output as it was stored, whose rounding to bfloat16 goes into every dS of the row, or as the sum of P dP over the keys, in a walk of
+// its own before: five products instead of three.  The rounding counts where few keys have the weight, as the output is as large as a value then, and in
+// the bias's gradient, where it adds up over a bucket: self-attention of 8 to 34 positions has dQ off by 0.0025 to 0.0031 and dw by up to 0.0032 with it, and by
+// the 0.0017 of the result's own rounding without.  So bfloat16 makes the first walk if there is a bias (long batch of its own 168 us, 154 without) and
+// where the keys, up to 128, stay in LDS for the second (short batch 28.5 us, 28.7 without).  Other walks take the stored output, with
+// 300 keys and more dQ is 0.0017 to 0.0018 off (long batch 280 us, 390 with two walks; short 28.5, with two walks for all 36.9).  It is up to 0.005 off if
+// attention is so sharp that a row has the weight of two keys.
+// For the key gradients' kernel delta is left without that error in any case: a row's dS add up to 0, so what they do add up to is what delta lacks.
 // Bound like the forward kernel.  Fragments are read where they are used: read one product ahead, as in the kernel below, they need more than 256
 // registers (424 to 796 us on the long batch, with the plain third product).
 namespace {
@@ -561,7 +569,7 @@ __device__ __forceinline__ float2 top_and_sum(const RaggedArgs& a, const RaggedI
         join(second.x, second.y);
         lds_barrier();
     }
-    step.again();
+    step.again(false);
     return float2{m, l};
 }
 
@@ -586,8 +594,10 @@ template <typename T, int D, bool BIAS, bool PAIR> __global__ __launch_bounds__(
     RowFrag<T, D> q, d_o;
     q.load(a.q.p + (int64_t)(row0 + r) * a.q.row + head * a.q.head, live, h);
     d_o.load(a.d_o.p + (int64_t)(row0 + r) * a.d_o.row + head * a.d_o.head, live, h);
+    constexpr bool kRounded = sizeof(T) == 2;  // outputs are
+    const bool resident = it.k_end - it.k_begin <= 2 * R::kStep, twice = kRounded && (BIAS || resident);  // (the rule's figures are above)
     float delta = 0.f, rest = 0.f;
-    {
+    if (!twice) {
         RowFrag<T, D> o;
         o.load(a.o.p + (int64_t)(row0 + r) * a.o.row + head * a.o.head, live, h);
 #pragma unroll
@@ -602,15 +612,14 @@ template <typename T, int D, bool BIAS, bool PAIR> __global__ __launch_bounds__(
     float base = live ? base_of(kLog2e * lse) : -kNone;
     const int mine_end = end_of(a, it, count, pos);
     bool large = false;  // the workgroup has rows with a large lse: scores are taken from `tops`, and `base` is what is left to take away
-    __shared__ float tops[BIAS ? 4 * 32 : 1];
+    __shared__ float tops[BIAS ? 4 * 32 : 1], exchanged[BIAS || (PAIR && kRounded) ? 4 * 32 : 1];  // (together what launch() leaves of a compute unit's LDS)
     if constexpr (BIAS) {
         bias_to_lds<T>(a, w, head);
         for (int i = tid; i < 8 * places; i += 256) sums[i] = 0.f;
-        __shared__ int any[4];
         const bool mine = __ballot(is_large(lse)) != 0;
-        if (lane == 0) any[wave] = mine;
+        if (lane == 0) exchanged[wave] = mine ? 1.f : 0.f;
         lds_barrier();
-        large = __builtin_amdgcn_readfirstlane(any[0] | any[1] | any[2] | any[3]) != 0;
+        large = __ballot(exchanged[lane & 3] != 0.f) != 0;
         if (large) {
             float2 of = top_and_sum<T, D, PAIR>(a, it, step, q, w, reinterpret_cast<float2*>(lds), mine_end, pos, tile, wave, lane);
             of = is_large(lse) ? float2{of.x, of.y > 0.f ? __builtin_amdgcn_logf(of.y) : 0.f} : float2{base, 0.f};
@@ -620,6 +629,46 @@ template <typename T, int D, bool BIAS, bool PAIR> __global__ __launch_bounds__(
             if (is_large(lse) && h == 0 && tile == 0) a.large[(int64_t)(row0 + r) * a.heads + head] = of;
         }
     }
+    // the step at hand: which keys the lane's row sees (rows that are not there have weights of zero without a mask), and of a tile the weights' scores and dP
+    auto seen_at = [&](int k0) { return live ? seen_from(step.seen, k0, pos + r, a.causal) : ~0ull; };
+    auto products = [&](f32x16& s, f32x16& dp, int k0, int key, uint64_t seen) {
+        AsRows<T, D> k, v;
+        k.load(step.keys(), key, lane);
+        k.dot(s, q);
+        v.load(step.values(), key, lane);
+        v.dot(dp, d_o);
+        finish_scores<BIAS>(s, a, scale2, w, (uint32_t)(seen >> key), k0 + key, pos, r, h);
+        if (BIAS && large) {
+            const float top = tops[wave * 32 + r];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = fminf(s[i] - top, 0.f);
+        }
+    };
+    if constexpr (kRounded) {
+        if (twice) {  // delta, from a walk of its own
+            for (int k0 = it.k_begin; k0 < it.k_end; k0 += R::kStep) {
+                step.next();
+                step.fetch(k0 + R::kStep);
+                if (k0 >= mine_end) continue;
+                const uint64_t seen = seen_at(k0);
+#pragma unroll 1
+                for (int u = 0; u < (PAIR ? 1 : R::kStep / 32); ++u) {
+                    f32x16 s, dp;
+                    products(s, dp, k0, 32 * (tile + u), seen);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) delta = fmaf(weight_of<BIAS>(s[i], scale2, base), dp[i], delta);
+                }
+            }
+            delta = sum_halves(delta);
+            lds_barrier();
+            if constexpr (PAIR) {  // two wavefronts have the same rows
+                if (h == 0) exchanged[wave * 32 + r] = delta;
+                lds_barrier();
+                delta = exchanged[group * 32 + r] + exchanged[(group + 2) * 32 + r];
+            }
+            step.again(resident);
+        }
+    }
     f32x16 acc[R::kTiles];
     clear<R::kTiles>(acc);
     float far = 0.f, near = 0.f;
@@ -627,28 +676,17 @@ template <typename T, int D, bool BIAS, bool PAIR> __global__ __launch_bounds__(
     for (; k0 < mine_end; k0 += R::kStep) {
         step.next();
         step.fetch(k0 + R::kStep);
-        // (rows that are not there have weights of zero without a mask)
-        const uint64_t seen = live ? seen_from(step.seen, k0, pos + r, a.causal) : ~0ull;
+        const uint64_t seen = seen_at(k0);
 #pragma unroll
         for (int u = 0; u < (PAIR ? 1 : R::kStep / 32); ++u) {
             const int key = 32 * (tile + u);
             f32x16 s, dp;
-            AsRows<T, D> k, v;
             AsColumns<T, D> kt;
-            k.load(step.keys(), key, lane);
-            k.dot(s, q);
-            v.load(step.values(), key, lane);
-            v.dot(dp, d_o);
-            finish_scores<BIAS>(s, a, scale2, w, (uint32_t)(seen >> key), k0 + key, pos, r, h);
-            if (BIAS && large) {
-                const float top = tops[wave * 32 + r];
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = fminf(s[i] - top, 0.f);
-            }
+            products(s, dp, k0, key, seen);
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 s[i] = weight_of<BIAS>(s[i], scale2, base) * (dp[i] - delta);
-                rest += s[i];
+                if constexpr (!(kRounded && BIAS)) rest += s[i];
             }
             if constexpr (BIAS) add_distances(s, a, sums + (2 * wave + h) * places, far, near, k0 + key, pos, lane);
             phase();
