@@ -135,6 +135,17 @@ template <int D> struct AsColumns<bf16_t, D> {
             for (int t = 0; t < R::kTiles; ++t) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(c[s][t], rest, acc[t], 0, 0, 0);
         }
     }
+    // and that alone
+    __device__ __forceinline__ void add_rest(f32x16* acc, const f32x16& w) const {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            bf16x8 rest;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) rest[e] = (bf16_t)(w[8 * s + e] - (float)(bf16_t)w[8 * s + e]);
+#pragma unroll
+            for (int t = 0; t < R::kTiles; ++t) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(c[s][t], rest, acc[t], 0, 0, 0);
+        }
+    }
 };
 template <int D> struct AsColumns<float, D> {
     typedef Rows<float, D> R;
