@@ -5,8 +5,8 @@
  * bias) and the preference loss on pairs of transcripts.
  *
  * Conventions are those of aed.h: row-major, dtype 0 float32 / 1 bfloat16,
- * sums, softmax and statistics in float32; the caller owns all memory, the
- * library allocates none on the device; lengths are HOST arrays that are read
+ * scores, softmax, statistics and sums in float32; the caller owns all memory,
+ * the library allocates none on the device; lengths are HOST arrays that are read
  * by create; work is enqueued on the stream given at create and calls return
  * after enqueueing; errors are aed_status codes found on the host before any
  * launch; the same calls give the same bits.
@@ -14,7 +14,8 @@
  * A handle belongs to one batch's lengths and is kept for all layers and for
  * forward and backward: create copies its work lists into the workspace.  Its
  * calls are launches only (no allocation, copy or wait), so they can be
- * recorded in a graph.  One handle = one stream = one host thread.
+ * recorded in a graph (the handle and its workspace outlive it).  One handle =
+ * one stream = one host thread.
  */
 #ifndef AED_TRAIN_H
 #define AED_TRAIN_H
@@ -40,7 +41,15 @@ const char *aed_train_last_error(void);
  * k_len - q_len: the last query row stands at the last key.  A row that sees
  * nothing has output 0, lse -inf and adds nothing to any gradient.  Keys and
  * values that are masked or beyond a length are never used, whatever they hold.
- * Heads: query head h reads key head h / (n_heads / n_kv_heads). */
+ * (by key_mask; what a causal row does not see has weight 0 and has to be
+ * finite, and so have the queries and gradients of rows that see nothing.)
+ * Heads: query head h reads key head h / (n_heads / n_kv_heads).
+ * With bfloat16 tensors the weights p are rounded to bfloat16 where they enter
+ * the products with v and d_out, and their gradients where they enter those
+ * with q (16 bits in those with k, and in small batches of few rows).  Against
+ * exact arithmetic, in the 2-norm: outputs 0.002, dk and dv 0.0024; dq and
+ * d_bias have the 0.0017 of their own rounding (dq more where more than 128
+ * keys and no bias meet very sharp attention). */
 typedef struct aed_attn aed_attn; /* opaque */
 
 typedef struct aed_attn_config {
@@ -142,7 +151,7 @@ aed_status aed_preference_destroy(aed_preference *plan);
 aed_status aed_preference_forward(aed_preference *plan, const void *logits, int64_t row_stride, const int32_t *labels,
                                   const float *ref_logp, float *loss, float *ratio, float *lse);
 
-/* d_logits: [rows, vocab] in the logits' type, d_row_stride elements between rows; may be the logits themselves.
+/* d_logits: [rows, vocab] in the logits' type, d_row_stride elements between rows; may be the logits themselves, otherwise apart from them.
  * ratio and lse are aed_preference_forward's; d_loss: DEVICE float32[1], the gradient by the loss, or NULL = 1. */
 aed_status aed_preference_backward(aed_preference *plan, const void *logits, int64_t row_stride, const int32_t *labels,
                                    const float *ratio, const float *lse, const float *d_loss, void *d_logits, int64_t d_row_stride);

@@ -13,12 +13,12 @@
 // order, and there are no atomics between wavefronts.
 //
 // Times in this file are the kernels' on an MI355X, bfloat16, 8 heads of 128, for the gradients' lists of four batches:
-//   short  64 utterances, 4 909 rows (12 to 132), 9 021 keys           forward  18 us   dQ  29   dK and dV  34
-//   long  128 utterances, 48 029 rows (300 to 448), 57 196 keys                185       286            386
-//   self, short  64 sequences of 12 to 132 positions, causal, bias              15        30             28
-//   self, long  128 sequences of 8 to 448 positions, causal, bias               70       148            140
-// The products of the long batch are 88, 176 (one of dQ's three made twice) and 176 GFLOP: 475, 615 and 456 TFLOP/s, against 1 240 of a
-// product of 8192 x 8192 x 8192.
+//   short  64 utterances, 4 909 rows (12 to 132), 9 021 keys           forward  19 us   dQ  28   dK and dV  33
+//   long  128 utterances, 48 029 rows (300 to 448), 57 196 keys                189       280            384
+//   self, short  64 sequences of 12 to 132 positions, causal, bias              15        32             28
+//   self, long  128 sequences of 8 to 448 positions, causal, bias               72       176            144
+// (those of the long batches move by 5 % and more with the card's clocks.)  The products of the long batch are 88, 132 and 176 GFLOP: 466, 471 and 458
+// TFLOP/s, against 1 240 of a product of 8192 x 8192 x 8192; the second one of dQ's three, for the rest of dS, is not counted.
 #include "attn_ragged.h"
 #include "attn_tile.h"
 #include "device_once.h"
@@ -283,10 +283,10 @@ template <typename T, int D> struct Steps {
 // ---------------------------------------------------------------- forward, many rows
 // A workgroup takes 128 query rows of a head, 32 a wavefront, and walks the keys.  PAIR: it takes 64 rows, and two wavefronts share 32 of them,
 // each with 32 keys of a step.  Scores are computed transposed (a lane is a query), so that a lane holds half a row's weights
-// and they enter the second product from where they are.  Of 200 us for 128 utterances of 448 rows and 512 keys, 100 are the two products
-// (their rate is a large product's), 30 the softmax in between, 35 the wait for keys and values and 39 starts and ends; two
+// and they enter the second product from where they are.  128 utterances of 448 rows and 512 keys take 199 to 212 us; of the 202 that an earlier form
+// took, 100 were the two products (their rate is a large product's), 30 the softmax in between, 35 the wait for keys and values and 39 starts and ends.  Two
 // workgroups share a compute unit to cover one's waits with the other's products, which is why a wavefront has 256 registers and 32 rows: with 64 rows
-// and all registers it was 258 us against 184.  Short batches are bound by starts and ends, a single round of workgroups.
+// and all registers it was 258 us against the same form's 184.  Short batches are bound by starts and ends, a single round of workgroups.
 template <typename T, int D, bool BIAS, bool PAIR> __global__ __launch_bounds__(256, (2 - Rows<T, D>::kWide)) void attn_forward_kernel(RaggedArgs a) {
     typedef Rows<T, D> R;
     extern __shared__ __align__(16) char lds[];
@@ -511,14 +511,14 @@ template <typename T, int D> __global__ __launch_bounds__(256) void attn_join_ke
 
 // ---------------------------------------------------------------- query gradients, delta, and the bias's
 // The forward kernel's walk with two products to a tile of scores (K Q^T and V dO^T, transposed, a lane being a query) and one
-// more for dQ, which in bfloat16 is made with what rounding took off dS as well (250 us instead of 286 on the long batch without it).
+// more for dQ, which in bfloat16 is made with what rounding took off dS as well (280 us on the long batch; an earlier form 286, 250 without it).
 // delta: from the output as it was stored, whose rounding to bfloat16 goes into every dS of the row, or as the sum of P dP over the keys, in a walk of
 // its own before: five products instead of three.  The rounding counts where few keys have the weight, as the output is as large as a value then, and in
 // the bias's gradient, where it adds up over a bucket: self-attention of 8 to 34 positions has dQ off by 0.0025 to 0.0031 and dw by up to 0.0032 with it, and by
-// the 0.0017 of the result's own rounding without.  So bfloat16 makes the first walk if there is a bias (long batch of its own 168 us, 154 without) and
+// the 0.0017 of the result's own rounding without.  So bfloat16 makes the first walk if there is a bias (long batch of its own 168 to 176 us, 154 without) and
 // where the keys, up to 128, stay in LDS for the second (short batch 28.5 us, 28.7 without).  Other walks take the stored output, with
-// 300 keys and more dQ is 0.0017 to 0.0018 off (long batch 280 us, 390 with two walks; short 28.5, with two walks for all 36.9).  It is up to 0.005 off if
-// attention is so sharp that a row has the weight of two keys.
+// 300 keys and more dQ is 0.0017 to 0.0018 off (long batch 280 us, 390 with two walks; short 28.5, with two walks for all 36.9).  By float64 arithmetic with
+// an output so rounded it would be 0.003 to 0.005 off if attention were so sharp that a row has the weight of two or three keys among 448.
 // For the key gradients' kernel delta is left without that error in any case: a row's dS add up to 0, so what they do add up to is what delta lacks.
 // Bound like the forward kernel.  Fragments are read where they are used: read one product ahead, as in the kernel below, they need more than 256
 // registers (424 to 796 us on the long batch, with the plain third product).
@@ -777,7 +777,7 @@ constexpr int kLargeFlags = 4;  // places of LDS
 // workgroups: what heads share is added up here, in order.
 // Two accumulators of 32 keys and the keys and values themselves take 192 registers, so that a wavefront has a SIMD to itself and nothing else
 // covers its waits: operands are requested one product ahead, and their reads and the vector instructions stand among the matrix
-// instructions (386 us on the long batch; requested at their use 426).  Of 400 us for 128 utterances of 448 rows and 512 keys, 331 remain without any
+// instructions (384 us on the long batch; requested at their use 426).  128 utterances of 448 rows and 512 keys take 364 to 382 us; of an earlier form's 400, 331 remain without any
 // request to memory in the loop, 74 of them starts and ends.  Slower: two workgroups a compute unit in 256 registers each 467, eight wavefronts
 // with keys and values in LDS 432, 64 keys a wavefront 499; one workgroup a compute unit that goes on to the next task 401, and 38 instead of
 // 28 us for short causal sequences, which do not end together then.

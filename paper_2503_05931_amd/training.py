@@ -3,7 +3,7 @@ sequence, forward and backward, and the preference loss on pairs of transcripts.
 
 Argument marshalling only; a missing library raises.  Tensors are torch tensors on the device.  A plan works on the stream
 that was current when it was made, or on `stream`; a call under another current stream waits for that one's work and lets it
-wait for the results.
+wait for the results.  A graph that holds a plan's calls needs the plan for as long as it is replayed.
 """
 from __future__ import annotations
 
