@@ -170,8 +170,8 @@ aed_status to_tensor(const aed_rows* t, const char* name, int64_t rows, int head
         if (strides[i] < 0 || strides[i] > kMostStride) return fail(AED_EINVAL, "%s: a stride is negative or above 2^38", name);
         if (strides[i] * es % 16 != 0) return fail(AED_EINVAL, "%s: a stride of %lld elements is no multiple of 16 bytes", name, (long long)strides[i]);
     }
-    if (output && aed::vectors_overlap(rows, strides[0], heads, strides[1], head_dim)) return fail(AED_EINVAL, "%s: rows or heads of an output overlap", name);
     if (strides[0] > aed::kAttnMaxPitch / es) return fail(AED_EUNSUPPORTED, "%s: more than %d bytes between rows", name, aed::kAttnMaxPitch);
+    if (output && aed::vectors_overlap(rows, strides[0], heads, strides[1], head_dim)) return fail(AED_EINVAL, "%s: rows or heads of an output overlap", name);
     to = aed::AttnTensor{static_cast<char*>(t->data), strides[0] * es, strides[1] * es};
     return AED_OK;
 }

@@ -42,7 +42,8 @@ inline std::vector<uint8_t> bucket_places(int buckets, int max_distance, bool bi
     return of;
 }
 
-// Whether two of rows x heads vectors of `length` elements, `row` and `head` elements apart, share one.  Strides are not negative.
+// Whether two of rows x heads vectors of `length` elements, `row` and `head` elements apart, share one.  Strides are not negative, and rows x row and
+// heads x head below 2^62.
 inline bool vectors_overlap(int64_t rows, int64_t row, int64_t heads, int64_t head, int64_t length) {
     if ((rows > 1 && row < length) || (heads > 1 && head < length)) return true;
     if (rows <= 1 || heads <= 1 || row >= (heads - 1) * head + length || head >= (rows - 1) * row + length) return false;  // one inside the other's gaps

@@ -61,6 +61,7 @@ def preference():
     return HostPreference().loss(z, torch.tensor([1, 2], dtype=torch.int32), torch.zeros(2)), z
 
 
+@pytest.mark.filterwarnings("ignore:Using backward")
 @pytest.mark.parametrize("form", [squares, row, preference])
 def test_second_derivatives_are_refused(form):
     """Gradients are made by the library: a term made of them has no gradient of its own, and says so."""
