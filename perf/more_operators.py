@@ -143,7 +143,7 @@ def prepare(case, seed):
     scored[0] = True
     s["weights"] = scored / scored.sum()
     if own:
-        s["plan"] = vocabulary.Distillation(rows, vocab, case["top"], dtype, temperature=case["temperature"])
+        s["plan"] = vocabulary.Distillation(vocab, case["top"], dtype, temperature=case["temperature"])
     return s
 
 
@@ -172,7 +172,7 @@ def _own_distill(s):
     loss, row_loss, stats = plan.aed_distill_forward(*given, rest=s["rest"], weights=s["weights"])
     if not s["case"]["training"]:
         return {"loss": loss, "row_loss": row_loss}
-    d_logits = plan.aed_distill_backward(*given, stats, rest=s["rest"], weights=s["weights"])
+    d_logits = plan.aed_distill_backward(*given, stats, weights=s["weights"])
     return {"loss": loss, "row_loss": row_loss, "d_logits": d_logits}
 
 
