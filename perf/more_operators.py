@@ -168,11 +168,11 @@ def _own_top(s):
 
 
 def _own_distill(s):
-    plan, given = s["plan"], (s["logits"], s["values"], s["ids"])
-    loss, row_loss, stats = plan.aed_distill_forward(*given, rest=s["rest"], weights=s["weights"])
+    plan, weights = s["plan"], s["weights"]
+    loss, row_loss, stats = plan.aed_distill_forward(s["logits"], s["values"], s["ids"], rest=s["rest"], weights=weights)
     if not s["case"]["training"]:
         return {"loss": loss, "row_loss": row_loss}
-    d_logits = plan.aed_distill_backward(*given, stats, weights=s["weights"])
+    d_logits = plan.aed_distill_backward(s["logits"], s["ids"], stats, weights=weights)
     return {"loss": loss, "row_loss": row_loss, "d_logits": d_logits}
 
 
