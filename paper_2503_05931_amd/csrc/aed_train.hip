@@ -1,69 +1,27 @@
 // Host side of include/aed_train.h: argument checks, workspaces and launches of ragged attention and the preference loss.
 #include "../../include/aed_train.h"
 
-#include <cstdarg>
-#include <cstdio>
-#include <cstring>
-#include <exception>
-#include <new>
-#include <vector>
-
 #include "attn_plan.h"
 #include "attn_ragged.h"
+#include "host_calls.h"
 #include "preference.h"
 
 static_assert(sizeof(aed::PlanItem) == sizeof(aed::RaggedItem) && sizeof(aed::PlanJoin) == sizeof(aed::RaggedJoin), "the lists are copied as they are");
 
+thread_local char aed::train_error[512] = "";
+
 namespace {
 
-thread_local char g_error[512] = "";
-
-aed_status fail(aed_status st, const char* fmt, ...) {
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(g_error, sizeof g_error, fmt, ap);
-    va_end(ap);
-    return st;
-}
-aed_status hip_status(hipError_t e, const char* what) { return e == hipSuccess ? AED_OK : fail(AED_EHIP, "%s: %s", what, hipGetErrorString(e)); }
-// No exception leaves an entry point: what is thrown here is an allocation that failed.
-template <typename F> aed_status guarded(F f) {
-    try {
-        return f();
-    } catch (const std::bad_alloc&) {
-        return fail(AED_ECAPACITY, "out of host memory");
-    } catch (const std::exception& e) {
-        return fail(AED_EINVAL, "%s", e.what());
-    }
-}
+using aed::Arena;
+using aed::fail;
+using aed::finish;
+using aed::guarded;
+using aed::hip_status;
+using aed::start;
 
 constexpr int64_t kMost = 0x7fffffff;
 constexpr int64_t kMostStart = (int64_t)1 << 38;  // times the bytes between rows (kAttnMaxPitch, 2^24 less a few): below 2^62
 constexpr int64_t kMostStride = (int64_t)1 << 38;  // elements; in bytes and times the heads (2^16) below 2^57
-size_t rounded(size_t n) { return (n + 255) & ~(size_t)255; }
-
-// Tables that go to the workspace's beginning in one copy, then scratch
-struct Arena {
-    std::vector<char> tables;
-    size_t total = 0;
-    template <typename T> size_t table(const std::vector<T>& v) {
-        const size_t at = tables.size();
-        tables.resize(rounded(at + v.size() * sizeof(T)));
-        if (!v.empty()) memcpy(tables.data() + at, v.data(), v.size() * sizeof(T));
-        return total = tables.size(), at;
-    }
-    size_t scratch(size_t bytes) {  // after all tables
-        const size_t at = total;
-        total = rounded(total + bytes);
-        return at;
-    }
-};
-aed_status check_workspace(const void* ws, size_t have, size_t need) {
-    if (!ws) return fail(AED_EINVAL, "workspace is NULL");
-    if ((uintptr_t)ws % 256 != 0) return fail(AED_EINVAL, "workspace must be 256-byte aligned");
-    if (have < need) return fail(AED_EINVAL, "workspace has %zu bytes, %zu needed", have, need);
-    return AED_OK;
-}
 
 }  // namespace
 
@@ -285,32 +243,11 @@ aed_status preference_args(const aed_preference* p, const void* logits, int64_t 
     return AED_OK;
 }
 
-// A handle whose tables are on their way to the workspace
-template <typename P> aed_status start(P* p, void* workspace, size_t bytes, void* hip_stream, P** out) {
-    aed_status st = check_workspace(workspace, bytes, p->arena.total);
-    p->ws = static_cast<char*>(workspace);
-    p->stream = static_cast<hipStream_t>(hip_stream);
-    if (st == AED_OK && !p->arena.tables.empty())  // the source lives as long as the handle
-        st = hip_status(hipMemcpyAsync(p->ws, p->arena.tables.data(), p->arena.tables.size(), hipMemcpyHostToDevice, p->stream), "copying the work lists");
-    if (st != AED_OK) {
-        delete p;
-        return st;
-    }
-    *out = p;
-    return AED_OK;
-}
-template <typename P> aed_status finish(P* p) {
-    if (!p) return AED_OK;
-    const hipError_t e = hipStreamSynchronize(p->stream);
-    delete p;
-    return hip_status(e, "hipStreamSynchronize");
-}
-
 }  // namespace
 
 extern "C" {
 
-const char* aed_train_last_error(void) { return g_error; }
+const char* aed_train_last_error(void) { return aed::train_error; }
 
 aed_status aed_attn_workspace_bytes(const aed_attn_config* cfg, const int32_t* q_lens, const int32_t* k_lens, const int64_t* k_starts, int32_t batch,
                                     size_t* bytes) {

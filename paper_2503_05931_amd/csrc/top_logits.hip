@@ -1,0 +1,135 @@
+// A row's largest logits, in order, with their ids, and the log of the sum of exponentials of all others.
+//
+// Bound by memory: a row is read once, into registers.  Its lanes' maxima give a bound that a few more elements than are asked for are not below; those are
+// gathered in LDS and placed by comparing each with each.  Everything below the bound adds to the rest's sum in the same pass, relative to the
+// bound, so nothing is subtracted from a whole row's sum, however little is left of it.
+#include "vocab_rows.h"
+
+namespace aed {
+
+namespace {
+
+template <int W> struct TopLds {
+    RowBounds<W> bounds;
+    List list;
+    Histogram hist;
+    float part[W];
+    float over[kList];
+};
+template <int W> __device__ __forceinline__ float block_sum(float v, float* part) {
+    v = wave_sum(v);
+    if constexpr (W > 1) {
+        __syncthreads();  // part is free
+        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = part[0];
+#pragma unroll
+        for (int i = 1; i < W; ++i) v += part[i];
+    }
+    return v;
+}
+template <int W> __device__ __forceinline__ float block_max(float v, float* part) {
+    v = wave_max(v);
+    if constexpr (W > 1) {
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = part[0];
+#pragma unroll
+        for (int i = 1; i < W; ++i) v = fmaxf(v, part[i]);
+    }
+    return v;
+}
+
+}  // namespace
+
+template <typename T, int W, int S> __global__ __launch_bounds__(64 * W) void top_logits_kernel(TopArgs a) {
+    constexpr int kThreads = 64 * W;
+    __shared__ TopLds<W> lds;
+    List& list = lds.list;
+    const int r = blockIdx.x, tid = threadIdx.x, K = a.top;
+    const Row<T, W, S> row(a.z, r);
+    float* const values = a.values + (int64_t)r * K;
+    int32_t* const ids = a.ids + (int64_t)r * K;
+    float top, bound;
+    bound_row<W>(row, K, lds.bounds, list, top, bound);
+    float sum = 0.f;  // of what is below the bound, relative to it
+    row.each([&](float z, int id) {
+        if (z >= bound && z > -kInf) put_in(list, z, id);
+        sum += z < bound ? __builtin_amdgcn_exp2f((z - bound) * a.scale) : 0.f;
+    });
+    __syncthreads();
+    int n = list.count;
+    Place last{-kInf, INT_MAX};
+    const bool searched = n > kList;
+    if (searched) {  // many equal ones, mostly
+        last = find_last<false>(row.again(), top, K, lds.hist, list, [](float, int) { return true; }, [](float) { return (uint64_t)1; });
+        if (tid == 0) list.count = 0;
+        __syncthreads();
+        row.again().each([&](float z, int id) {
+            if (z > -kInf && up_to(z, id, last)) put_in(list, z, id);
+        });
+        __syncthreads();
+        n = list.count;
+    }
+    for (int i = tid; i < n; i += kThreads) {
+        const float z = list.z[i];
+        const int id = list.id[i];
+        int place = 0;
+        for (int j = 0; j < n; ++j) place += before(list.z[j], list.id[j], z, id);
+        if (place < K) {
+            values[place] = z;
+            ids[place] = id;
+            if (place == K - 1) lds.hist.last = Place{z, id};
+        } else {
+            lds.over[place] = z;
+        }
+    }
+    for (int i = n + tid; i < K; i += kThreads) {
+        values[i] = -kInf;
+        ids[i] = -1;
+    }
+    float rest = -kInf;
+    if (n >= K) {  // there may be others
+        float base = bound;
+        __syncthreads();
+        // listed, but not among the first: in their order, as the list has none
+        for (int i = K + tid; i < n; i += kThreads) sum += __builtin_amdgcn_exp2f((lds.over[i] - bound) * a.scale);
+        sum = searched ? 0.f : block_sum<W>(sum, lds.part);
+        if (!(sum >= 0x1p-60f && sum < 0x1p100f)) {  // nothing, or far from the bound: relative to its own largest
+            last = lds.hist.last;
+            float m = -kInf;
+            row.again().each([&](float z, int id) { m = up_to(z, id, last) ? m : fmaxf(m, z); });
+            base = block_max<W>(m, lds.part);
+            sum = 0.f;
+            if (base > -kInf) row.again().each([&](float z, int id) { sum += z > -kInf && !up_to(z, id, last) ? __builtin_amdgcn_exp2f((z - base) * a.scale) : 0.f; });
+            sum = block_sum<W>(sum, lds.part);
+        }
+        if (base > -kInf) rest = base == kInf ? kInf : base / a.temperature + logf(sum);
+    }
+    if (tid == 0) a.rest[r] = rest;
+}
+
+namespace {
+
+template <typename T, int W, int S> hipError_t launch_top_as(const TopArgs& a, hipStream_t s) {
+    top_logits_kernel<T, W, S><<<dim3(a.z.rows), dim3(64 * W), 0, s>>>(a);
+    return hipGetLastError();
+}
+template <typename T> hipError_t launch_top_of(const TopArgs& a, hipStream_t s) {
+    const int vecs = (a.z.vocab + RowVec<T>::n - 1) / RowVec<T>::n;
+    if (a.top <= 64) {
+        if (vecs <= 64 * 2) return launch_top_as<T, 1, 2>(a, s);
+        if (vecs <= 64 * 8) return launch_top_as<T, 1, 8>(a, s);
+    }
+    if (vecs <= 256 * 4) return launch_top_as<T, 4, 4>(a, s);
+    if (vecs <= 256 * 16) return launch_top_as<T, 4, 16>(a, s);
+    if (vecs <= 1024 * 8) return launch_top_as<T, 16, 8>(a, s);
+    return launch_top_as<T, 16, 0>(a, s);
+}
+
+}  // namespace
+
+hipError_t launch_top(const TopArgs& a, bool bf16, hipStream_t s) { return bf16 ? launch_top_of<bf16_t>(a, s) : launch_top_of<float>(a, s); }
+
+}  // namespace aed

@@ -337,7 +337,7 @@ _functions = None
 
 
 def _autograd():
-    """The two torch.autograd.Function classes (made when they are first needed: torch is not imported before)."""
+    """The two torch.autograd.Function classes and what makes their gradients constants (made when they are first needed: torch is not imported before)."""
     global _functions
     if _functions is None:
         import torch
@@ -352,7 +352,7 @@ def _autograd():
 
             @staticmethod
             def backward(ctx, *_):
-                raise RuntimeError("second derivatives of attention and of the preference loss are not computed")
+                raise RuntimeError("second derivatives of the library's operators are not computed")
 
         def once(gradients, *made_from):
             if not torch.is_grad_enabled():  # on only under create_graph
@@ -390,5 +390,5 @@ def _autograd():
                 gradient = ctx.plan.aed_preference_backward(logits, labels, ratio, lse, d_loss.contiguous())
                 return None, *once((gradient,), d_loss, logits), None, None
 
-        _functions = Attend, Loss
+        _functions = Attend, Loss, once
     return _functions
