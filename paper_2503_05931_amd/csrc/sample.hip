@@ -24,19 +24,40 @@ constexpr int kMostListed = 128;  // top-k above it goes by search
 template <int W, int RUNS> struct SampleLds {
     RowBounds<W> bounds;
     List list;
-    Histogram hist;
-    uint64_t w[kList];
+    Search<W, 11, true> search;
+    uint64_t w[kList];  // by id
+    int by_place[kList], by_id[kList];
+    float z[kList];
     uint64_t run[RUNS];
 };
 
+// 2^y, y <= 0, to some 2^-50: the exponential's series for the fraction, |y| <= 1/2: the term that is left out, (ln 2 / 2)^12 / 12!, is 6e-15.
+__device__ __forceinline__ double pow2(double y) {
+    y = fmax(y, -1100.0);
+    const double n = rint(y), f = y - n;
+    constexpr double l = 0.69314718055994530942;
+    constexpr double c2 = l * l / 2, c3 = c2 * l / 3, c4 = c3 * l / 4, c5 = c4 * l / 5, c6 = c5 * l / 6, c7 = c6 * l / 7, c8 = c7 * l / 8, c9 = c8 * l / 9, c10 = c9 * l / 10,
+                     c11 = c10 * l / 11;
+    double p = fma(f, c11, c10);
+    p = fma(f, p, c9);
+    p = fma(f, p, c8);
+    p = fma(f, p, c7);
+    p = fma(f, p, c6);
+    p = fma(f, p, c5);
+    p = fma(f, p, c4);
+    p = fma(f, p, c3);
+    p = fma(f, p, c2);
+    p = fma(f, p, l);
+    p = fma(f, p, 1.0);
+    return ldexp(p, (int)n);
+}
 struct Weigh {
     double top, c, magic;  // log2 e / t; 2^(52 - bits): a double there has whole multiples of 2^-bits as its last digits
     float top_f;
     __device__ __forceinline__ double exact(float z) const {
 #pragma clang fp contract(off)  // the same weight wherever it is made
-        if (z == top_f) return 1.0;
-        if (!(z > -kInf) || top_f == kInf) return 0.0;
-        return exp2(((double)z - top) * c);
+        const double w = z > -kInf && top_f < kInf ? pow2(((double)z - top) * c) : 0.0;
+        return z == top_f ? 1.0 : w;
     }
     __device__ __forceinline__ uint64_t whole(double w) const {
 #pragma clang fp contract(off)
@@ -80,7 +101,7 @@ template <typename T, int W, int S, int RUNS> __global__ __launch_bounds__(64 * 
     __shared__ SampleLds<W, RUNS> lds;
     List& list = lds.list;
     const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const Row<T, W, S> row(a.z, r);
+    Row<T, W, S> row(a.z, r);
     const float t = a.temperatures ? a.temperatures[r] : a.temperature;
     const bool greedy = !(t > 0.f);
     int k = a.top_ks ? a.top_ks[r] : a.top_k;
@@ -93,6 +114,7 @@ template <typename T, int W, int S, int RUNS> __global__ __launch_bounds__(64 * 
 
     float top, bound;
     bound_row<W>(row, by_k ? (k <= kMostListed ? k : 1) : by_p ? kWanted : 1, lds.bounds, list, top, bound);
+    row.forget();
     if (!(top > -kInf)) {  // nothing to draw from
         if (tid == 0) {
             a.tokens[r] = -1;
@@ -123,68 +145,94 @@ template <typename T, int W, int S, int RUNS> __global__ __launch_bounds__(64 * 
         });
     };
     auto anything = [](float, int) { return true; };
-    auto gather = [&](float z, int id) {
-        if (z >= bound && z > -kInf) put_in(list, z, id);
-    };
     const int runs = ((a.z.vocab + N - 1) / N + 63) / 64;
 
     Place last{-kInf, INT_MAX};  // of A, then of B
     if (by_k || by_p) {
-        bool listed = !by_k || k <= kMostListed;
+        bool few = !by_k || k <= kMostListed;
         uint64_t all = 0;  // A's sum, if A is the whole row
-        if (!by_k) {
+        if (few) {
             uint64_t mine = 0;
-            row.each([&](float z, int id) {
-                gather(z, id);
-                mine += weight(z);
+            gather(row, bound, list, [&](float z, float) {
+                if (!by_k) mine += weight(z);
             });
-            all = block_sum64<W>(mine, lds.run);
-        } else if (listed) {
-            row.each(gather);
+            if (!by_k) all = block_sum64<W>(mine, lds.run);
         }
-        __syncthreads();
-        int n = list.count;
-        listed = listed && n <= kList;
-        if (listed) {
-            // each by its thread: its weight, its place and what lies in front of it
-            float z = -kInf;
-            int id = -1, place = INT_MAX;
-            uint64_t w = 0, front = 0;
-            if (tid < n) {
-                z = list.z[tid];
-                id = list.id[tid];
-                w = weight(z);
-                lds.w[tid] = w;
-            }
+        const int n = few ? (int)list.count : 0;
+        few = few && n <= kList;
+        if (few) {
+            // each by its thread: its place in the order, and among the ids
+            if (tid < n) list.z[tid] = in_order(to_f32(row.p[list.id[tid]]));
             __syncthreads();
             if (tid < n) {
-                place = 0;
+                const float z = list.z[tid];
+                const int id = list.id[tid];
+                int place = 0, by_id = 0;
+#pragma unroll 8
                 for (int j = 0; j < n; ++j) {
-                    const bool b = before(list.z[j], list.id[j], z, id);
-                    place += b;
-                    front += b ? lds.w[j] : 0;
+                    place += before(list.z[j], list.id[j], z, id);
+                    by_id += list.id[j] < id;
                 }
+                lds.z[place] = z;
+                lds.by_place[place] = by_id;
+                lds.by_id[by_id] = id;
             }
-            const uint64_t sum = block_sum64<W>(place < k ? w : 0, lds.run);  // of A, or of the part of it that is listed
-            const uint64_t border = by_p ? part_of<true>(top_p, by_k ? sum : all) : ~(uint64_t)0;
-            if (by_k || sum >= border) {  // all of B is listed
-                const bool kept = place < k && (place == 0 || front < border) && weigh.exact(z) >= least;
-                if (tid < n && !kept) lds.w[tid] = 0;
-                const uint64_t left = block_sum64<W>(kept ? w : 0, lds.run);
+            __syncthreads();
+            // in their order, four a lane, by the first wavefront
+            constexpr int kEach = kList / 64;
+            uint64_t w[kEach], mine = 0, of_a = 0;
+            double x[kEach];
+            if (wave == 0) {
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) {
+                    const int place = kEach * lane + i;
+                    x[i] = place < n ? weigh.exact(lds.z[place]) : 0.0;
+                    w[i] = place < n ? weigh.whole(x[i]) : 0;
+                    mine += w[i];
+                    of_a += place < k ? w[i] : 0;
+                }
+                of_a = wave_sum64(of_a);  // A's sum, or that of its listed part
+            }
+            bool found = by_k;
+            if (!by_k) {
+                if (tid == 0) lds.run[0] = of_a;
+                __syncthreads();
+                of_a = lds.run[0];
+                found = of_a >= part_of<true>(top_p, all);  // all of B is listed
+            }
+            if (found) {
+                if (wave != 0) return;
+                const uint64_t border = by_p ? part_of<true>(top_p, by_k ? of_a : all) : ~(uint64_t)0;
+                uint64_t front = wave_prefix(mine) - mine, left = 0;
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) {
+                    const int place = kEach * lane + i;
+                    const uint64_t kept = place < k && (place == 0 || front < border) && x[i] >= least ? w[i] : 0;
+                    front += w[i];
+                    left += kept;
+                    if (place < n) lds.w[lds.by_place[place]] = kept;
+                }
+                left = wave_sum64(left);
+                other_lanes_wrote();
                 const uint64_t target = min(part_of<false>(u, left), left - 1);
-                if (kept) {
-                    uint64_t at = 0;
-                    for (int j = 0; j < n; ++j) at += list.id[j] < id ? lds.w[j] : 0;
-                    if (at <= target && target < at + w) {
-                        a.tokens[r] = id;
-                        a.logp[r] = (float)log((double)w / (double)left);
+                uint64_t v[kEach];
+                mine = 0;
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) mine += v[i] = kEach * lane + i < n ? lds.w[kEach * lane + i] : 0;
+                uint64_t at = wave_prefix(mine) - mine;
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) {
+                    if (at <= target && target < at + v[i]) {
+                        a.tokens[r] = lds.by_id[kEach * lane + i];
+                        a.logp[r] = (float)log((double)v[i] / (double)left);
                     }
+                    at += v[i];
                 }
                 return;
             }
         }
         __syncthreads();
-        if (by_k) last = find_last<false>(row.again(), top, k, lds.hist, list, anything, weight);
+        if (by_k) last = find_last<false>(row.again(), top, k, lds.search, list, anything, weight);
         if (by_p) {
             if (by_k) {
                 uint64_t mine = 0;
@@ -195,7 +243,7 @@ template <typename T, int W, int S, int RUNS> __global__ __launch_bounds__(64 * 
             }
             const uint64_t border = max(part_of<true>(top_p, all), (uint64_t)1);
             const Place of_a = last;
-            last = find_last<true>(row.again(), top, border, lds.hist, list, [=](float z, int id) { return up_to(z, id, of_a); }, weight);
+            last = find_last<true>(row.again(), top, border, lds.search, list, [=](float z, int id) { return up_to(z, id, of_a); }, weight);
         }
     }
     add_runs([=](float z, int id) { return up_to(z, id, last); });
@@ -208,14 +256,14 @@ template <typename T, int W, int S, int RUNS> __global__ __launch_bounds__(64 * 
     uint64_t at = 0;  // in front of the runs that are looked at
     int found = -1;
     for (int first = 0; found < 0 && first < runs; first += 64) {
-        const uint64_t v = first + lane < runs ? lds.run[first + lane] : 0, through = at + wave_prefix64(v);
+        const uint64_t v = first + lane < runs ? lds.run[first + lane] : 0, through = at + wave_prefix(v);
         const uint64_t hit = __ballot(through > target);
         if (hit) {
             const int l = __builtin_ctzll(hit);
             found = first + l;
-            at = __shfl(through - v, l);
+            at = lane_of(through - v, l);
         } else {
-            at = __shfl(through, 63);
+            at = lane_of(through, 63);
         }
     }
     // the run's ids, N a lane
@@ -229,7 +277,7 @@ template <typename T, int W, int S, int RUNS> __global__ __launch_bounds__(64 * 
         w[e] = x > 0.0 && x >= least ? weigh.whole(x) : 0;
         mine += w[e];
     }
-    at += wave_prefix64(mine) - mine;
+    at += wave_prefix(mine) - mine;
 #pragma unroll
     for (int e = 0; e < N; ++e) {
         if (at <= target && target < at + w[e]) {

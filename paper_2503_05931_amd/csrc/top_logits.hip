@@ -12,7 +12,7 @@ namespace {
 template <int W> struct TopLds {
     RowBounds<W> bounds;
     List list;
-    Histogram hist;
+    Search<W, 8, false> search;
     float part[W];
     float over[kList];
 };
@@ -48,22 +48,23 @@ template <typename T, int W, int S> __global__ __launch_bounds__(64 * W) void to
     __shared__ TopLds<W> lds;
     List& list = lds.list;
     const int r = blockIdx.x, tid = threadIdx.x, K = a.top;
-    const Row<T, W, S> row(a.z, r);
+    Row<T, W, S> row(a.z, r);
     float* const values = a.values + (int64_t)r * K;
     int32_t* const ids = a.ids + (int64_t)r * K;
     float top, bound;
     bound_row<W>(row, K, lds.bounds, list, top, bound);
-    float sum = 0.f;  // of what is below the bound, relative to it
-    row.each([&](float z, int id) {
-        if (z >= bound && z > -kInf) put_in(list, z, id);
-        sum += z < bound ? __builtin_amdgcn_exp2f((z - bound) * a.scale) : 0.f;
+    row.forget();
+    float sum = 0.f;  // of what is below the bound, relative to it; may be NaN, if one is in the row
+    gather(row, bound, list, [&](float, float over) {
+        const uint32_t below = __builtin_bit_cast(int, over) >> 31;
+        sum += bits_f32(__builtin_bit_cast(uint32_t, __builtin_amdgcn_exp2f(over * a.scale)) & below);
     });
-    __syncthreads();
+    asm volatile("" : "+v"(sum));  // it is made here, not where it is used: there the comparisons would have to be kept
     int n = list.count;
     Place last{-kInf, INT_MAX};
     const bool searched = n > kList;
     if (searched) {  // many equal ones, mostly
-        last = find_last<false>(row.again(), top, K, lds.hist, list, [](float, int) { return true; }, [](float) { return (uint64_t)1; });
+        last = find_last<false>(row.again(), top, K, lds.search, list, [](float, int) { return true; }, [](float) { return (uint64_t)1; });
         if (tid == 0) list.count = 0;
         __syncthreads();
         row.again().each([&](float z, int id) {
@@ -72,15 +73,18 @@ template <typename T, int W, int S> __global__ __launch_bounds__(64 * W) void to
         __syncthreads();
         n = list.count;
     }
+    for (int i = tid; i < n; i += kThreads) list.z[i] = in_order(to_f32(row.p[list.id[i]]));
+    __syncthreads();
     for (int i = tid; i < n; i += kThreads) {
         const float z = list.z[i];
         const int id = list.id[i];
         int place = 0;
+#pragma unroll 8
         for (int j = 0; j < n; ++j) place += before(list.z[j], list.id[j], z, id);
         if (place < K) {
             values[place] = z;
-            ids[place] = id;
-            if (place == K - 1) lds.hist.last = Place{z, id};
+            ids[place] = z > -kInf ? id : -1;
+            if (place == K - 1) lds.search.last = Place{z, id};
         } else {
             lds.over[place] = z;
         }
@@ -97,7 +101,7 @@ template <typename T, int W, int S> __global__ __launch_bounds__(64 * W) void to
         for (int i = K + tid; i < n; i += kThreads) sum += __builtin_amdgcn_exp2f((lds.over[i] - bound) * a.scale);
         sum = searched ? 0.f : block_sum<W>(sum, lds.part);
         if (!(sum >= 0x1p-60f && sum < 0x1p100f)) {  // nothing, or far from the bound: relative to its own largest
-            last = lds.hist.last;
+            last = lds.search.last;
             float m = -kInf;
             row.again().each([&](float z, int id) { m = up_to(z, id, last) ? m : fmaxf(m, z); });
             base = block_max<W>(m, lds.part);

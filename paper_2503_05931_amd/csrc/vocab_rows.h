@@ -65,6 +65,18 @@ template <typename T, int W, int S> struct Row {
             for (int s = 0; s < S; ++s) x[s] = read(s);
         }
     }
+    // What has been read is read as if anew: left to itself the compiler keeps each bfloat16 of a row as a float too, from one pass to the next, twice the
+    // registers.
+    __device__ __forceinline__ void forget() {
+        if constexpr (S > 0 && sizeof(T) == 2) {
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                u32x4 u = __builtin_bit_cast(u32x4, x[s]);
+                asm volatile("" : "+v"(u));
+                x[s] = __builtin_bit_cast(V, u);
+            }
+        }
+    }
     // f(s, first id, vector); every thread of a wavefront comes along to the last step
     template <typename F> __device__ __forceinline__ void each_vec(F f) const {
         if constexpr (S > 0) {
@@ -110,23 +122,42 @@ __device__ __forceinline__ uint64_t wave_sum64(uint64_t v) {
     hi = __builtin_amdgcn_permlane32_swap((uint32_t)(v >> 32), (uint32_t)(v >> 32), false, false);
     return ((uint64_t)hi[0] << 32 | lo[0]) + ((uint64_t)hi[1] << 32 | lo[1]);
 }
-// of the lanes up to this one
-__device__ __forceinline__ uint64_t wave_prefix64(uint64_t v) {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int by = 1; by < 64; by *= 2) {
-        const uint64_t o = __shfl_up(v, by);
-        if (lane >= by) v += o;
-    }
+// a shift within rows of 16 lanes (zeros come in), or a row's last lane to the rows of ROWS
+template <int CTRL, int ROWS = 0xF> __device__ __forceinline__ uint32_t dpp_or0(uint32_t v) {
+    return __builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, true);
+}
+template <int CTRL, int ROWS = 0xF> __device__ __forceinline__ uint64_t dpp_or0(uint64_t v) {
+    return (uint64_t)dpp_or0<CTRL, ROWS>((uint32_t)(v >> 32)) << 32 | dpp_or0<CTRL, ROWS>((uint32_t)v);
+}
+// sum of the lanes up to this one
+template <typename U> __device__ __forceinline__ U wave_prefix(U v) {
+    v += dpp_or0<0x111>(v);
+    v += dpp_or0<0x112>(v);
+    v += dpp_or0<0x114>(v);
+    v += dpp_or0<0x118>(v);
+    v += dpp_or0<0x142, 0xA>(v);  // lane 15 to row 1, lane 47 to row 3
+    v += dpp_or0<0x143, 0xC>(v);  // lane 31 to rows 2 and 3
     return v;
 }
+__device__ __forceinline__ uint32_t lane_of(uint32_t v, int l) { return __builtin_amdgcn_readlane((int)v, l); }
+__device__ __forceinline__ uint64_t lane_of(uint64_t v, int l) { return (uint64_t)lane_of((uint32_t)(v >> 32), l) << 32 | lane_of((uint32_t)v, l); }
 
-// The j-th largest of the lanes' values (1 <= j <= 64)
-__device__ __forceinline__ float lanes_jth(float v, int j) {
-    int above = 0;
+// larger floats, larger bits; -0 is 0
+__device__ __forceinline__ uint32_t rising_bits(float z) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, z + 0.f);
+    return (u & 0x80000000u) ? ~u : u | 0x80000000u;
+}
+
+// A bound that j (1 to 64) of the lanes' values at least are not below: the j-th largest with the last 16 bits of its float cleared away, by halving over ballots,
+// whose counts are the scalar unit's work.  (Sixty-four lanes read one by one: 192 vector instructions for 16.)
+__device__ __forceinline__ float lanes_bound(float v, int j) {
+    const uint32_t high = rising_bits(v) >> 16;
+    uint32_t t = 0;
 #pragma unroll
-    for (int l = 0; l < 64; ++l) above += bits_f32(__builtin_amdgcn_readlane(__builtin_bit_cast(int, v), l)) > v;
-    return wave_min(above < j ? v : kInf);
+    for (int bit = 15; bit >= 0; --bit)
+        if (__builtin_popcountll(__ballot(high >= (t | 1u << bit))) >= j) t |= 1u << bit;
+    const uint32_t u = t << 16;
+    return t <= 0x7f ? -kInf : __builtin_bit_cast(float, (u & 0x80000000u) ? u & 0x7fffffffu : ~u);
 }
 
 // An element's place in the order
@@ -139,152 +170,210 @@ __device__ __forceinline__ bool before(float z, int id, float z2, int id2) { ret
 __device__ __forceinline__ bool up_to(float z, int id, const Place& last) { return z > last.z || (z == last.z && id <= last.id); }
 
 // ---- the part of a row that can hold its first elements, gathered in LDS ----
-// At least `want` elements are at or above the bound: each of the wavefronts that the row fills takes the (want / wavefronts)-th largest of its lanes'
-// maxima, and the least of these is the bound (no lane's maximum is counted twice).
+// At least `want` elements are at or above the bound: each of the wavefronts that the row fills takes one that (want / wavefronts) of its lanes'
+// maxima are not below, and the least of these is the bound (no lane's maximum is counted twice).
 constexpr int kList = 256;
+constexpr float kMostFloat = 0x1.fffffep127f;
 struct List {
-    int count;  // may be more than kList: then the list is cut off and of no use
+    uint32_t count;  // may be more than kList: then the list is cut off and of no use
     float z[kList];
     int id[kList];
 };
 template <int W> struct RowBounds {
-    float top[W], jth[W];
+    float top[W], bound[W];
 };
 
-// Every thread has the row's largest logit and the bound.
+// Every thread has the row's largest logit and the bound, a finite number.
 template <int W, typename R> __device__ __forceinline__ void bound_row(const R& row, int want, RowBounds<W>& lds, List& list, float& top, float& bound) {
     float m = -kInf;
     row.each([&](float z, int) { m = fmaxf(m, z); });  // NaN is passed over
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int full = max(1, min(W, row.n / (64 * R::N))), j = (want + full - 1) / full;
-    const float wave_top = wave_max(m), jth = want <= 1 ? wave_top : j > 64 ? -kInf : lanes_jth(m, j);
-    if constexpr (W == 1) {
-        top = wave_top;
-        bound = jth;
-        if (lane == 0) list.count = 0;
-        __syncthreads();
-    } else {
+    top = wave_max(m);
+    bound = want <= 1 ? top : j > 64 ? -kInf : lanes_bound(m, j);
+    if constexpr (W > 1) {
         if (lane == 0) {
-            lds.top[wave] = wave_top;
-            lds.jth[wave] = jth;
+            lds.top[wave] = top;
+            lds.bound[wave] = bound;
         }
         if (threadIdx.x == 0) list.count = 0;
         __syncthreads();
         top = lds.top[0];
-        bound = lds.jth[0];
+        bound = lds.bound[0];
 #pragma unroll
         for (int i = 1; i < W; ++i) {
             top = fmaxf(top, lds.top[i]);
-            bound = i < full ? fminf(bound, lds.jth[i]) : bound;
+            bound = i < full ? fminf(bound, lds.bound[i]) : bound;
         }
+        if (want <= 1) bound = top;
     }
-    if (want <= 1) bound = top;
+    bound = fminf(fmaxf(bound, -kMostFloat), kMostFloat);
+    if (bound == 0.f) bound = -0.f;  // so that -0 less the bound is 0, whose sign says that it is not below
 }
 __device__ __forceinline__ void put_in(List& list, float z, int id) {
-    const int at = atomicAdd(&list.count, 1);
+    const uint32_t at = atomicAdd(&list.count, 1u);
     if (at < kList) {
         list.z[at] = z;
         list.id[at] = id;
     }
 }
+// Ids of the elements at or above the bound, in no order, perhaps of some that are NaN; f(logit, logit - bound): what else the pass does with each.  Logits are
+// read by these ids later.  A lane's elements are marked by the signs of their differences, an instruction each (a comparison's result cannot be
+// used at once), so places are handed out once a wavefront, and what is listed costs a few steps.
+template <typename T, int W, int S, typename F> __device__ __forceinline__ void gather(const Row<T, W, S>& row, float bound, List& list, F f) {
+    constexpr int N = RowVec<T>::n;
+    if constexpr (S > 0) {
+        constexpr int kMarks = (S * N + 31) / 32;
+        uint32_t marks[kMarks] = {};
+        row.each_vec([&](int s, int, const auto& v) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const float z = to_f32((T)v[e]), over = z - bound;
+                uint32_t& m = marks[(s * N + e) / 32];
+                m = __builtin_amdgcn_alignbit(m, __builtin_bit_cast(uint32_t, over), 31);  // the sign from the right
+                f(z, over);
+            }
+        });
+        uint32_t mine = 0;
+#pragma unroll
+        for (int i = 0; i < kMarks; ++i) {
+            marks[i] = ~marks[i] << (S * N < 32 ? 32 - S * N : 0);
+            mine += __builtin_popcount(marks[i]);
+        }
+        const uint32_t through = wave_prefix(mine), all = lane_of(through, 63);
+        uint32_t at = through - mine;
+        if constexpr (W == 1) {
+            list.count = all;
+        } else {
+            uint32_t base = 0;
+            if ((threadIdx.x & 63) == 0) base = atomicAdd(&list.count, all);
+            at += lane_of(base, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < kMarks; ++i)
+            while (marks[i]) {
+                const int first = __builtin_clz(marks[i]), k = 32 * i + first;
+                marks[i] &= ~(0x80000000u >> first);
+                if (at < kList) list.id[at] = vec_begin<N>(((k / N) * 64 * W + (int)threadIdx.x) * N, row.n) + k % N;
+                ++at;
+            }
+    } else {
+        row.each([&](float z, int id) {
+            if (z >= bound) put_in(list, z, id);
+            f(z, z - bound);
+        });
+    }
+    __syncthreads();
+}
+// minus infinity in the place of NaN: neither is in the order
+__device__ __forceinline__ float in_order(float z) { return fmaxf(z, -kInf); }
 
 // ---- exact search for the last of the first elements of the order, whatever the row holds ----
-// Digit by digit over histograms of 256 bins: first of the distance to the largest logit (its floating point bits: 16 bins for each power of two
-// from 2^-10 to 2^6), then of the logit's own bits, then of the id's, until the bin that the border falls into has at most kList elements; those are gathered and
-// compared one by one.  Elements are counted, or (WEIGHTS) their weights are added up: whole numbers, so the order of the atomic additions
-// does not matter.
-struct Histogram {
-    uint64_t sum[256];
-    uint32_t count[256];
-    uint64_t before, target;
-    uint32_t members;
+// Digit by digit over histograms of 2^BITS bins: first of the distance to the largest logit (its floating point bits: 16 powers of two, from 2^-10 to 2^6,
+// have as many bins each), then of the logit's own bits, then of the id's, until the bin that the border falls into has at most kList elements; those
+// are compared one by one.  Elements are counted, or (WEIGHTS) their weights are added up: whole numbers, so the order of the atomic additions does not matter.
+template <int W, int BITS, bool WEIGHTS> struct Search {
+    uint64_t sum[1 << BITS];
+    uint64_t part[W], before;
+    uint64_t w[WEIGHTS ? kList : 1];
     int bin;
     Place last;
 };
-__device__ __forceinline__ uint32_t falling_bits(float z) {  // larger logits, smaller bits; -0 is 0
-    const uint32_t u = __builtin_bit_cast(uint32_t, z + 0.f);
-    return (u & 0x80000000u) ? u : ~(u | 0x80000000u);
-}
-__device__ __forceinline__ int distance_bin(float z, float top) {
-    const uint32_t u = __builtin_bit_cast(uint32_t, z == top ? 0.f : top - z) >> 19;
-    constexpr int first = (127 - 10) << 4;
-    return min(max((int)u - first, 0), 255);
+template <int BITS> __device__ __forceinline__ int distance_bin(float z, float top) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, z == top ? 0.f : top - z) >> (27 - BITS);
+    constexpr int first = (127 - 10) << (BITS - 4);
+    return min(max((int)u - first, 0), (1 << BITS) - 1);
 }
 
 // target: for counts, how many elements the first part has; for weights, the least sum that the part up to its last element reaches; 1 or more, and
 // what is more than there is counts as all.  in(z, id): elements that take part, one at least (with a weight above 0); weight(z): theirs.
-template <bool WEIGHTS, typename T, int W, typename In, typename Weight>
-__device__ __noinline__ Place find_last(Row<T, W, 0> row, float top, uint64_t target, Histogram& h, List& list, In in, Weight weight) {
-    constexpr int kThreads = 64 * W;
-    const int tid = threadIdx.x, lane = tid & 63;
-    int level = 0, bin0 = 0;
+template <bool WEIGHTS, typename T, int W, int BITS, bool HAS_W, typename In, typename Weight>
+__device__ __noinline__ Place find_last(Row<T, W, 0> row, float top, uint64_t target, Search<W, BITS, HAS_W>& h, List& list, In in, Weight weight) {
+    static_assert(HAS_W || !WEIGHTS, "room for the listed elements' weights");
+    constexpr int kThreads = 64 * W, kBins = 1 << BITS, kEach = kBins < kThreads ? 1 : kBins / kThreads, kIdBits = 18;
+    static_assert(kMostVocab <= 1 << kIdBits, "an id's digits");
+    constexpr int kZLevels = (32 + BITS - 1) / BITS, kLevels = 1 + kZLevels + (kIdBits + BITS - 1) / BITS;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int bin0 = 0;
     uint32_t bits = 0, id_bits = 0;  // digits found so far
+    int known = 32, id_known = kIdBits;  // and how many bits are below them
     uint64_t passed = 0;             // in front of the bin
-    auto member = [&](float z, int id) {
-        if (!(z > -kInf) || !in(z, id)) return false;
-        if (level > 0 && distance_bin(z, top) != bin0) return false;
-        if (level > 1 && (falling_bits(z) ^ bits) >> (32 - 8 * min(level - 1, 4)) != 0) return false;
-        return level <= 5 || ((uint32_t)id ^ id_bits) >> (24 - 8 * (level - 5)) == 0;
-    };
-    while (true) {
-        for (int i = tid; i < 256; i += kThreads) {
-            h.sum[i] = 0;
-            h.count[i] = 0;
-        }
+    for (int level = 0;; ++level) {
+        auto member = [&](float z, int id) {
+            if (!(z > -kInf) || !in(z, id)) return false;
+            if (level > 0 && distance_bin<BITS>(z, top) != bin0) return false;
+            return (uint64_t)(~rising_bits(z) ^ bits) >> known == 0 && (((uint32_t)id ^ id_bits) >> id_known) == 0;
+        };
+        const bool by_z = level <= kZLevels;
+        const int have = by_z ? known : id_known, take = min(BITS, have), shift = have - take;
+        for (int i = tid; i < kBins; i += kThreads) h.sum[i] = 0;
         __syncthreads();
         row.each([&](float z, int id) {
             if (!member(z, id)) return;
-            const int digit = level == 0   ? distance_bin(z, top)
-                              : level <= 4 ? falling_bits(z) >> (32 - 8 * level) & 255
-                                           : (uint32_t)id >> (24 - 8 * (level - 4)) & 255;
-            atomicAdd(&h.count[digit], 1u);
-            if constexpr (WEIGHTS) atomicAdd((unsigned long long*)&h.sum[digit], (unsigned long long)weight(z));
+            const int digit = level == 0 ? distance_bin<BITS>(z, top) : ((by_z ? ~rising_bits(z) : (uint32_t)id) >> shift) & ((1u << take) - 1);
+            atomicAdd((unsigned long long*)&h.sum[digit], WEIGHTS ? (unsigned long long)weight(z) : 1ull);
         });
         __syncthreads();
-        if (tid < 64) {  // four bins a lane
-            uint64_t v[4], mine = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) mine += v[i] = WEIGHTS ? h.sum[4 * lane + i] : h.count[4 * lane + i];
-            const uint64_t through = passed + wave_prefix64(mine);
-            if (level == 0) {  // there may be fewer
-                target = min(target, (uint64_t)__shfl(through, 63));
-                if (lane == 0) h.target = target;
-            }
-            uint64_t at = through - mine;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (at < target && target <= at + v[i]) {  // one bin of one lane
-                    h.bin = 4 * lane + i;
-                    h.before = at;
-                    h.members = h.count[4 * lane + i];
-                }
-                at += v[i];
-            }
-        }
+        uint64_t mine = 0;
+        if (tid < kBins)
+            for (int i = 0; i < kEach; ++i) mine += h.sum[kEach * tid + i];
+        const uint64_t through = wave_prefix(mine);
+        if (lane == 63) h.part[wave] = through;
         if (tid == 0) list.count = 0;
         __syncthreads();
-        const int bin = h.bin;
+        uint64_t at = passed + through - mine, all = passed;
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            at += i < wave ? h.part[i] : 0;
+            all += h.part[i];
+        }
+        if (level == 0) target = min(target, all);  // there may be fewer
+        if (at < target && target <= at + mine)
+            for (int i = 0; i < kEach; ++i) {
+                const uint64_t v = h.sum[kEach * tid + i];
+                if (at < target && target <= at + v) {  // one bin of one thread
+                    h.bin = kEach * tid + i;
+                    h.before = at;
+                }
+                at += v;
+            }
+        __syncthreads();
         passed = h.before;
-        target = h.target;
-        if (level == 0) bin0 = bin;
-        else if (level <= 4) bits |= (uint32_t)bin << (32 - 8 * level);
-        else id_bits |= (uint32_t)bin << (24 - 8 * (level - 4));
-        ++level;
-        if (h.members <= kList || level > 7) break;
-        __syncthreads();  // all have read
+        if (level == 0) {
+            bin0 = h.bin;
+        } else if (by_z) {
+            bits |= (uint32_t)h.bin << shift;
+            known = shift;
+        } else {
+            id_bits |= (uint32_t)h.bin << shift;
+            id_known = shift;
+        }
+        const int next = level + 1;
+        row.each([&](float z, int id) {
+            if (!(z > -kInf) || !in(z, id) || distance_bin<BITS>(z, top) != bin0) return;
+            if ((uint64_t)(~rising_bits(z) ^ bits) >> known == 0 && (((uint32_t)id ^ id_bits) >> id_known) == 0) put_in(list, z, id);
+        });
+        __syncthreads();
+        if (list.count <= kList || next == kLevels) break;
+        __syncthreads();  // all have read the count
     }
-    row.each([&](float z, int id) {
-        if (member(z, id)) put_in(list, z, id);
-    });
-    __syncthreads();
-    const int n = min(list.count, kList);
+    const int n = min((int)list.count, kList);
+    if constexpr (WEIGHTS) {
+        for (int i = tid; i < n; i += kThreads) h.w[i] = weight(list.z[i]);
+        __syncthreads();
+    }
     for (int i = tid; i < n; i += kThreads) {
         const float z = list.z[i];
         const int id = list.id[i];
-        uint64_t at = passed;
-        for (int j = 0; j < n; ++j)
-            if (before(list.z[j], list.id[j], z, id)) at += WEIGHTS ? weight(list.z[j]) : 1;
-        if (at < target && target <= at + (WEIGHTS ? weight(z) : 1)) h.last = Place{z, id};
+        uint64_t at = passed, own = 1;
+        if constexpr (WEIGHTS) own = h.w[i];
+#pragma unroll 4
+        for (int j = 0; j < n; ++j) {
+            uint64_t w = 1;
+            if constexpr (WEIGHTS) w = h.w[j];
+            if (before(list.z[j], list.id[j], z, id)) at += w;
+        }
+        if (at < target && target <= at + own) h.last = Place{z, id};
     }
     __syncthreads();
     const Place last = h.last;
