@@ -12,6 +12,8 @@
 //   search  they leave many: the end of the first part is searched for by histograms (find_last)
 //   sums    whatever is left is added up by runs of one wavefront's vector (256 or 512 ids in a row); the run that the random number falls into is
 //           then gone through by one wavefront
+#include <type_traits>
+
 #include "vocab_rows.h"
 
 namespace aed {
@@ -25,43 +27,40 @@ template <int W, int RUNS> struct SampleLds {
     RowBounds<W> bounds;
     List list;
     Search<W, 11, true> search;
-    uint64_t w[kList];  // by id
+    uint64_t w[kList];    // by id
+    uint64_t key[kList];  // by place
     int by_place[kList], by_id[kList];
-    float z[kList];
     uint64_t run[RUNS];
 };
 
-// 2^y, y <= 0, to some 2^-50: the exponential's series for the fraction, |y| <= 1/2: the term that is left out, (ln 2 / 2)^12 / 12!, is 6e-15.
-__device__ __forceinline__ double pow2(double y) {
-    y = fmax(y, -1100.0);
-    const double n = rint(y), f = y - n;
-    constexpr double l = 0.69314718055994530942;
-    constexpr double c2 = l * l / 2, c3 = c2 * l / 3, c4 = c3 * l / 4, c5 = c4 * l / 5, c6 = c5 * l / 6, c7 = c6 * l / 7, c8 = c7 * l / 8, c9 = c8 * l / 9, c10 = c9 * l / 10,
-                     c11 = c10 * l / 11;
-    double p = fma(f, c11, c10);
-    p = fma(f, p, c9);
-    p = fma(f, p, c8);
-    p = fma(f, p, c7);
-    p = fma(f, p, c6);
-    p = fma(f, p, c5);
-    p = fma(f, p, c4);
-    p = fma(f, p, c3);
-    p = fma(f, p, c2);
-    p = fma(f, p, l);
-    p = fma(f, p, 1.0);
-    return ldexp(p, (int)n);
-}
+// Weights of a row's logits.  2^y for y <= 0: y's nearest whole number n, and 1 + f q(f) for what is left, q of degree 8 fitted to (2^f - 1) / f on [-1/2, 1/2]
+// for the least largest error, 1.6e-14 of the result.  Its coefficients are kept in scalar registers, where a product can take them from.
 struct Weigh {
-    double top, c, magic;  // log2 e / t; 2^(52 - bits): a double there has whole multiples of 2^-bits as its last digits
+    double top, c, q[9];  // c: log2 e / t
+    double magic;         // 2^(52 - bits): a double there has whole multiples of 2^-bits as its last digits, and its own last 32 bits are 0
     float top_f;
+    __device__ __forceinline__ Weigh(float top, float t, int bits)
+        : top(top), c(t > 0.f ? kLog2eD / (double)t : 0.0),
+          q{0.6931471805598853, 0.24022650695722841, 0.05550410866841879, 0.009618129181143242, 0.0013333557624782767, 0.0001540344090220312, 1.525299054241159e-05,
+            1.3258330955496492e-06, 1.0148218085577417e-07},
+          magic(__builtin_bit_cast(double, (uint64_t)(1023 + 52 - bits) << 52)), top_f(top) {
+#pragma unroll
+        for (int i = 0; i < 9; ++i) asm volatile("" : "+s"(q[i]));
+    }
+    // exactly 1 for the largest; 0 for minus infinity and NaN, and for all but the largest where that is infinite
     __device__ __forceinline__ double exact(float z) const {
 #pragma clang fp contract(off)  // the same weight wherever it is made
-        const double w = z > -kInf && top_f < kInf ? pow2(((double)z - top) * c) : 0.0;
+        const double y = fmax(((double)z - top) * c, -1100.0), n = rint(y), f = y - n;
+        double p = q[8];
+#pragma unroll
+        for (int i = 7; i >= 0; --i) p = fma(f, p, q[i]);
+        const double w = ldexp(fma(f, p, 1.0), (int)n);
         return z == top_f ? 1.0 : w;
     }
     __device__ __forceinline__ uint64_t whole(double w) const {
 #pragma clang fp contract(off)
-        return __builtin_bit_cast(uint64_t, magic + w) - __builtin_bit_cast(uint64_t, magic);
+        const uint64_t u = __builtin_bit_cast(uint64_t, magic + w);
+        return (uint64_t)((uint32_t)(u >> 32) - (uint32_t)(__builtin_bit_cast(uint64_t, magic) >> 32)) << 32 | (uint32_t)u;
     }
 };
 
@@ -122,92 +121,65 @@ template <typename T, int W, int S, int RUNS> __global__ __launch_bounds__(64 * 
         }
         return;
     }
-    Weigh weigh;
-    weigh.top_f = top;
-    weigh.top = top;
-    weigh.c = greedy ? 0.0 : kLog2eD / (double)t;
-    weigh.magic = __builtin_bit_cast(double, (uint64_t)(1023 + 52 - a.weight_bits) << 52);
+    const Weigh weigh(top, greedy ? 0.f : t, a.weight_bits);
     auto weight = [&](float z) { return weigh.whole(weigh.exact(z)); };
-    // runs' sums of what `in` leaves and min-p does
-    auto add_runs = [&](auto in) {
-        row.each_vec([&](int s, int id, const auto& v) {
-            uint64_t mine = 0;
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const float z = to_f32((T)v[e]);
-                if (in(z, id + e)) {
-                    const double w = weigh.exact(z);
-                    mine += w >= least ? weigh.whole(w) : 0;
-                }
-            }
-            mine = wave_sum64(mine);
-            if (lane == 0) lds.run[s * W + wave] = mine;
-        });
-    };
-    auto anything = [](float, int) { return true; };
-    const int runs = ((a.z.vocab + N - 1) / N + 63) / 64;
+    int token = -1;  // of the lane that finds it
+    uint64_t its = 0, left = 0;
 
     Place last{-kInf, INT_MAX};  // of A, then of B
+    bool done = false;
     if (by_k || by_p) {
         bool few = !by_k || k <= kMostListed;
-        uint64_t all = 0;  // A's sum, if A is the whole row
-        if (few) {
+        uint64_t all = 0;  // A's sum
+        if (!by_k) {
             uint64_t mine = 0;
-            gather(row, bound, list, [&](float z, float) {
-                if (!by_k) mine += weight(z);
+            gather(row, list, [&](float z) {
+                mine += weight(z);
+                return z - bound;
             });
-            if (!by_k) all = block_sum64<W>(mine, lds.run);
+            all = block_sum64<W>(mine, lds.run);
+        } else if (few) {
+            gather(row, list, [&](float z) { return z - bound; });
         }
         const int n = few ? (int)list.count : 0;
         few = few && n <= kList;
         if (few) {
-            // each by its thread: its place in the order, and among the ids
-            if (tid < n) list.z[tid] = in_order(to_f32(row.p[list.id[tid]]));
+            read_keys(row, list, n);
             __syncthreads();
-            if (tid < n) {
-                const float z = list.z[tid];
-                const int id = list.id[tid];
-                int place = 0, by_id = 0;
+            if (tid < n) {  // its place in the order, and among the ids
+                const uint64_t key = list.key[tid];
+                const int place = place_of(list, key, n);
+                int by_id = 0;
 #pragma unroll 8
-                for (int j = 0; j < n; ++j) {
-                    place += before(list.z[j], list.id[j], z, id);
-                    by_id += list.id[j] < id;
-                }
-                lds.z[place] = z;
+                for (int j = 0; j < n; ++j) by_id += (uint32_t)list.key[j] > (uint32_t)key;
+                lds.key[place] = key;
                 lds.by_place[place] = by_id;
-                lds.by_id[by_id] = id;
+                lds.by_id[by_id] = key_id(key);
             }
             __syncthreads();
-            // in their order, four a lane, by the first wavefront
+            // in their order, four a lane, by every wavefront: all have to know whether it is done; the first one answers
             constexpr int kEach = kList / 64;
             uint64_t w[kEach], mine = 0, of_a = 0;
             double x[kEach];
-            if (wave == 0) {
 #pragma unroll
-                for (int i = 0; i < kEach; ++i) {
-                    const int place = kEach * lane + i;
-                    x[i] = place < n ? weigh.exact(lds.z[place]) : 0.0;
-                    w[i] = place < n ? weigh.whole(x[i]) : 0;
-                    mine += w[i];
-                    of_a += place < k ? w[i] : 0;
-                }
-                of_a = wave_sum64(of_a);  // A's sum, or that of its listed part
+            for (int i = 0; i < kEach; ++i) {
+                const int place = kEach * lane + i;
+                x[i] = place < n ? weigh.exact(key_logit(lds.key[place])) : 0.0;
+                w[i] = place < n ? weigh.whole(x[i]) : 0;
+                mine += w[i];
+                of_a += place < k ? w[i] : 0;
             }
-            bool found = by_k;
-            if (!by_k) {
-                if (tid == 0) lds.run[0] = of_a;
-                __syncthreads();
-                of_a = lds.run[0];
-                found = of_a >= part_of<true>(top_p, all);  // all of B is listed
-            }
-            if (found) {
+            of_a = wave_sum64(of_a);  // A's sum, or that of its listed part
+            if (by_k) all = of_a;
+            const uint64_t border = by_p ? part_of<true>(top_p, all) : of_a;
+            done = of_a >= border;  // all of B is listed
+            if (done) {
                 if (wave != 0) return;
-                const uint64_t border = by_p ? part_of<true>(top_p, by_k ? of_a : all) : ~(uint64_t)0;
-                uint64_t front = wave_prefix(mine) - mine, left = 0;
+                uint64_t front = wave_prefix(mine) - mine;
 #pragma unroll
                 for (int i = 0; i < kEach; ++i) {
                     const int place = kEach * lane + i;
-                    const uint64_t kept = place < k && (place == 0 || front < border) && x[i] >= least ? w[i] : 0;
+                    const uint64_t kept = place < k && (place == 0 || !by_p || front < border) && x[i] >= least ? w[i] : 0;
                     front += w[i];
                     left += kept;
                     if (place < n) lds.w[lds.by_place[place]] = kept;
@@ -223,68 +195,94 @@ template <typename T, int W, int S, int RUNS> __global__ __launch_bounds__(64 * 
 #pragma unroll
                 for (int i = 0; i < kEach; ++i) {
                     if (at <= target && target < at + v[i]) {
-                        a.tokens[r] = lds.by_id[kEach * lane + i];
-                        a.logp[r] = (float)log((double)v[i] / (double)left);
+                        token = lds.by_id[kEach * lane + i];
+                        its = v[i];
                     }
                     at += v[i];
                 }
-                return;
             }
         }
-        __syncthreads();
-        if (by_k) last = find_last<false>(row.again(), top, k, lds.search, list, anything, weight);
-        if (by_p) {
-            if (by_k) {
+        // the last of A by number, then that of B by weight
+        for (int step = 0; step < 2 && !done; ++step) {
+            const bool by_weight = step == 1;
+            if (by_weight ? !by_p : !by_k) continue;
+            __syncthreads();
+            if (by_weight && by_k) {
                 uint64_t mine = 0;
-                row.each([&](float z, int id) {
-                    if (up_to(z, id, last)) mine += weight(z);
-                });
+                row.again().each([&](float z, int id) { mine += up_to(z, id, last) ? weight(z) : 0; });
                 all = block_sum64<W>(mine, lds.run);
             }
-            const uint64_t border = max(part_of<true>(top_p, all), (uint64_t)1);
+            const uint64_t target = by_weight ? max(part_of<true>(top_p, all), (uint64_t)1) : (uint64_t)k;
             const Place of_a = last;
-            last = find_last<true>(row.again(), top, border, lds.search, list, [=](float z, int id) { return up_to(z, id, of_a); }, weight);
+            last = find_last<11>(row.again(), top, target, lds.search, list, [=](float z, int id) { return up_to(z, id, of_a); },
+                                 [&](float z) { return by_weight ? weight(z) : 1; });
         }
     }
-    add_runs([=](float z, int id) { return up_to(z, id, last); });
-    __syncthreads();
-    if (wave != 0) return;
-    uint64_t left = 0;
-    for (int i = lane; i < runs; i += 64) left += lds.run[i];
-    left = wave_sum64(left);
-    const uint64_t target = min(part_of<false>(u, left), left - 1);
-    uint64_t at = 0;  // in front of the runs that are looked at
-    int found = -1;
-    for (int first = 0; found < 0 && first < runs; first += 64) {
-        const uint64_t v = first + lane < runs ? lds.run[first + lane] : 0, through = at + wave_prefix(v);
-        const uint64_t hit = __ballot(through > target);
-        if (hit) {
-            const int l = __builtin_ctzll(hit);
-            found = first + l;
-            at = lane_of(through - v, l);
-        } else {
-            at = lane_of(through, 63);
-        }
-    }
-    // the run's ids, N a lane
-    const int id0 = (found * 64 + lane) * N, id = vec_begin<N>(id0, a.z.vocab);
-    const auto v = row_vec(row.p, id0, a.z.vocab);
-    uint64_t w[N], mine = 0;
+    if (!done) {
+        row.forget();
+        // runs' sums of what is left
+        const bool filtered = by_k || by_p || least > 0.0;
+        auto add_runs = [&](auto some) {
+            row.each_vec([&](int s, int id, const auto& v) {
+                uint64_t mine = 0;
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-        const float z = to_f32((T)v[e]);
-        const double x = z > -kInf && up_to(z, id + e, last) ? weigh.exact(z) : 0.0;
-        w[e] = x > 0.0 && x >= least ? weigh.whole(x) : 0;
-        mine += w[e];
-    }
-    at += wave_prefix(mine) - mine;
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-        if (at <= target && target < at + w[e]) {
-            a.tokens[r] = id + e;
-            a.logp[r] = (float)log((double)w[e] / (double)left);
+                for (int e = 0; e < N; ++e) {
+                    const float z = to_f32((T)v[e]);
+                    const double x = weigh.exact(z);
+                    uint64_t w = weigh.whole(x);
+                    if constexpr (decltype(some)::value) w = up_to(z, id + e, last) && x >= least ? w : 0;
+                    mine += w;
+                }
+                mine = wave_sum64(mine);
+                if (lane == 0) lds.run[s * W + wave] = mine;
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        };
+        if (filtered) add_runs(std::true_type());
+        else add_runs(std::false_type());
+        __syncthreads();
+        if (wave != 0) return;
+        const int runs = ((a.z.vocab + N - 1) / N + 63) / 64;
+        for (int i = lane; i < runs; i += 64) left += lds.run[i];
+        left = wave_sum64(left);
+        const uint64_t target = min(part_of<false>(u, left), left - 1);
+        uint64_t at = 0;  // in front of the runs that are looked at
+        int found = -1;
+        for (int first = 0; found < 0 && first < runs; first += 64) {
+            const uint64_t v = first + lane < runs ? lds.run[first + lane] : 0, through = at + wave_prefix(v);
+            const uint64_t hit = __ballot(through > target);
+            if (hit) {
+                const int l = __builtin_ctzll(hit);
+                found = first + l;
+                at = lane_of(through - v, l);
+            } else {
+                at = lane_of(through, 63);
+            }
         }
-        at += w[e];
+        // the run's ids, N a lane
+        const int id0 = (found * 64 + lane) * N, id = vec_begin<N>(id0, a.z.vocab);
+        const auto v = row_vec(row.p, id0, a.z.vocab);
+        uint64_t w[N], mine = 0;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float z = to_f32((T)v[e]);
+            const double x = weigh.exact(z);
+            w[e] = up_to(z, id + e, last) && x >= least ? weigh.whole(x) : 0;
+            mine += w[e];
+        }
+        at += wave_prefix(mine) - mine;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            if (at <= target && target < at + w[e]) {
+                token = id + e;
+                its = w[e];
+            }
+            at += w[e];
+        }
+    }
+    if (token >= 0) {  // one lane
+        a.tokens[r] = token;
+        a.logp[r] = (float)log((double)its / (double)left);
     }
 }
 

@@ -9,6 +9,8 @@ namespace aed {
 
 namespace {
 
+constexpr float kLn2 = 0.69314718055994530942f;
+
 template <int W> struct TopLds {
     RowBounds<W> bounds;
     List list;
@@ -54,37 +56,40 @@ template <typename T, int W, int S> __global__ __launch_bounds__(64 * W) void to
     float top, bound;
     bound_row<W>(row, K, lds.bounds, list, top, bound);
     row.forget();
-    float sum = 0.f;  // of what is below the bound, relative to it; may be NaN, if one is in the row
-    gather(row, bound, list, [&](float, float over) {
-        const uint32_t below = __builtin_bit_cast(int, over) >> 31;
-        sum += bits_f32(__builtin_bit_cast(uint32_t, __builtin_amdgcn_exp2f(over * a.scale)) & below);
+    // Exponents relative to a border that the bound's own product, rounded, is not below.  Where a product could be infinite, the row is searched.
+    const float scaled = bound * a.scale, border = scaled - fabsf(scaled) * 0x1p-22f - 0x1p-126f;
+    const bool fits = fabsf(scaled) < 1e37f;
+    float sum = 0.f;  // of what is below the border, relative to it; may be NaN, if one is in the row
+    gather(row, list, [&](float z) {
+        const float over = fmaf(z, a.scale, -border);
+        const float below = __builtin_amdgcn_fmed3f(over * -0x1p100f, 0.f, 1.f);
+        sum = fmaf(__builtin_amdgcn_exp2f(over), below, sum);
+        return over;
     });
-    asm volatile("" : "+v"(sum));  // it is made here, not where it is used: there the comparisons would have to be kept
+    asm volatile("" : "+v"(sum));  // it is made here, not where it is used: there the row would have to be kept
     int n = list.count;
     Place last{-kInf, INT_MAX};
-    const bool searched = n > kList;
+    const bool searched = n > kList || !fits;
     if (searched) {  // many equal ones, mostly
-        last = find_last<false>(row.again(), top, K, lds.search, list, [](float, int) { return true; }, [](float) { return (uint64_t)1; });
+        if (top > -kInf) last = find_last<8>(row.again(), top, K, lds.search, list, [](float, int) { return true; }, [](float) { return 1; });
         if (tid == 0) list.count = 0;
         __syncthreads();
         row.again().each([&](float z, int id) {
-            if (z > -kInf && up_to(z, id, last)) put_in(list, z, id);
+            if (z > -kInf && up_to(z, id, last)) put_in(list, id);
         });
         __syncthreads();
         n = list.count;
     }
-    for (int i = tid; i < n; i += kThreads) list.z[i] = in_order(to_f32(row.p[list.id[i]]));
+    read_keys(row, list, n);
     __syncthreads();
     for (int i = tid; i < n; i += kThreads) {
-        const float z = list.z[i];
-        const int id = list.id[i];
-        int place = 0;
-#pragma unroll 8
-        for (int j = 0; j < n; ++j) place += before(list.z[j], list.id[j], z, id);
+        const uint64_t key = list.key[i];
+        const int place = place_of(list, key, n);
+        const float z = key_logit(key);
         if (place < K) {
             values[place] = z;
-            ids[place] = z > -kInf ? id : -1;
-            if (place == K - 1) lds.search.last = Place{z, id};
+            ids[place] = z > -kInf ? key_id(key) : -1;
+            if (place == K - 1) lds.search.last = Place{z, key_id(key)};
         } else {
             lds.over[place] = z;
         }
@@ -95,21 +100,22 @@ template <typename T, int W, int S> __global__ __launch_bounds__(64 * W) void to
     }
     float rest = -kInf;
     if (n >= K) {  // there may be others
-        float base = bound;
         __syncthreads();
         // listed, but not among the first: in their order, as the list has none
-        for (int i = K + tid; i < n; i += kThreads) sum += __builtin_amdgcn_exp2f((lds.over[i] - bound) * a.scale);
+        for (int i = K + tid; i < n; i += kThreads) sum += __builtin_amdgcn_exp2f(fmaf(lds.over[i], a.scale, -border));
         sum = searched ? 0.f : block_sum<W>(sum, lds.part);
-        if (!(sum >= 0x1p-60f && sum < 0x1p100f)) {  // nothing, or far from the bound: relative to its own largest
+        if (sum >= 0x1p-60f && sum < 0x1p100f) {
+            rest = kLn2 * (border + __builtin_amdgcn_logf(sum));
+        } else {  // nothing, or far from the border: relative to its own largest
             last = lds.search.last;
             float m = -kInf;
             row.again().each([&](float z, int id) { m = up_to(z, id, last) ? m : fmaxf(m, z); });
-            base = block_max<W>(m, lds.part);
+            const float base = block_max<W>(m, lds.part);
             sum = 0.f;
             if (base > -kInf) row.again().each([&](float z, int id) { sum += z > -kInf && !up_to(z, id, last) ? __builtin_amdgcn_exp2f((z - base) * a.scale) : 0.f; });
             sum = block_sum<W>(sum, lds.part);
+            if (base > -kInf) rest = base == kInf ? kInf : base / a.temperature + logf(sum);
         }
-        if (base > -kInf) rest = base == kInf ? kInf : base / a.temperature + logf(sum);
     }
     if (tid == 0) a.rest[r] = rest;
 }

@@ -65,10 +65,9 @@ template <typename T, int W, int S> struct Row {
             for (int s = 0; s < S; ++s) x[s] = read(s);
         }
     }
-    // What has been read is read as if anew: left to itself the compiler keeps each bfloat16 of a row as a float too, from one pass to the next, twice the
-    // registers.
+    // What has been read counts as new: left to itself the compiler keeps, from one pass to the next, what it has made of each element.
     __device__ __forceinline__ void forget() {
-        if constexpr (S > 0 && sizeof(T) == 2) {
+        if constexpr (S > 0) {
 #pragma unroll
             for (int s = 0; s < S; ++s) {
                 u32x4 u = __builtin_bit_cast(u32x4, x[s]);
@@ -83,7 +82,12 @@ template <typename T, int W, int S> struct Row {
 #pragma unroll
             for (int s = 0; s < S; ++s) f(s, vec_begin<N>(s * kStep + (int)threadIdx.x * N, n), x[s]);
         } else {
-            for (int s = 0; s * kStep < n; ++s) f(s, vec_begin<N>(s * kStep + (int)threadIdx.x * N, n), read(s));
+            V next = read(0);
+            for (int s = 0; s * kStep < n; ++s) {
+                const V v = next;
+                if ((s + 1) * kStep < n) next = read(s + 1);
+                f(s, vec_begin<N>(s * kStep + (int)threadIdx.x * N, n), v);
+            }
         }
     }
     // f(logit, id); an id may come again, or one behind the row's end, with minus infinity
@@ -160,14 +164,21 @@ __device__ __forceinline__ float lanes_bound(float v, int j) {
     return t <= 0x7f ? -kInf : __builtin_bit_cast(float, (u & 0x80000000u) ? u & 0x7fffffffu : ~u);
 }
 
-// An element's place in the order
+// An element's place in the order: of two, the one in front has the larger key
+__device__ __forceinline__ uint64_t order_key(float z, int id) { return (uint64_t)rising_bits(z) << 32 | (uint32_t)~id; }
+__device__ __forceinline__ float key_logit(uint64_t key) {
+    const uint32_t u = key >> 32;
+    return __builtin_bit_cast(float, (u & 0x80000000u) ? u & 0x7fffffffu : ~u);
+}
+__device__ __forceinline__ int key_id(uint64_t key) { return ~(uint32_t)key; }
 struct Place {
     float z;
     int id;
 };
-__device__ __forceinline__ bool before(float z, int id, float z2, int id2) { return z > z2 || (z == z2 && id < id2); }
 // in the order up to `last`
 __device__ __forceinline__ bool up_to(float z, int id, const Place& last) { return z > last.z || (z == last.z && id <= last.id); }
+// minus infinity in the place of NaN: neither is in the order
+__device__ __forceinline__ float in_order(float z) { return fmaxf(z, -kInf); }
 
 // ---- the part of a row that can hold its first elements, gathered in LDS ----
 // At least `want` elements are at or above the bound: each of the wavefronts that the row fills takes one that (want / wavefronts) of its lanes'
@@ -176,8 +187,8 @@ constexpr int kList = 256;
 constexpr float kMostFloat = 0x1.fffffep127f;
 struct List {
     uint32_t count;  // may be more than kList: then the list is cut off and of no use
-    float z[kList];
     int id[kList];
+    uint64_t key[kList];
 };
 template <int W> struct RowBounds {
     float top[W], bound[W];
@@ -210,17 +221,26 @@ template <int W, typename R> __device__ __forceinline__ void bound_row(const R& 
     bound = fminf(fmaxf(bound, -kMostFloat), kMostFloat);
     if (bound == 0.f) bound = -0.f;  // so that -0 less the bound is 0, whose sign says that it is not below
 }
-__device__ __forceinline__ void put_in(List& list, float z, int id) {
+__device__ __forceinline__ void put_in(List& list, int id) {
     const uint32_t at = atomicAdd(&list.count, 1u);
-    if (at < kList) {
-        list.z[at] = z;
-        list.id[at] = id;
-    }
+    if (at < kList) list.id[at] = id;
 }
-// Ids of the elements at or above the bound, in no order, perhaps of some that are NaN; f(logit, logit - bound): what else the pass does with each.  Logits are
-// read by these ids later.  A lane's elements are marked by the signs of their differences, an instruction each (a comparison's result cannot be
+// makes the first n listed elements' keys; a barrier has to follow
+template <typename T, int W, int S> __device__ __forceinline__ void read_keys(const Row<T, W, S>& row, List& list, int n) {
+    for (int i = threadIdx.x; i < n; i += 64 * W) list.key[i] = order_key(in_order(to_f32(row.p[list.id[i]])), list.id[i]);
+}
+// how many of the n keys are larger
+__device__ __forceinline__ int place_of(const List& list, uint64_t key, int n) {
+    int place = 0;
+#pragma unroll 8
+    for (int j = 0; j < n; ++j) place += list.key[j] > key;
+    return place;
+}
+
+// Ids of the elements of which over(logit) is not negative, in no order, perhaps of some that are NaN; over grows with the logit, and is minus infinity for minus
+// infinity.  Logits are read by these ids later.  A lane's elements are marked by over's signs, an instruction each (a comparison's result cannot be
 // used at once), so places are handed out once a wavefront, and what is listed costs a few steps.
-template <typename T, int W, int S, typename F> __device__ __forceinline__ void gather(const Row<T, W, S>& row, float bound, List& list, F f) {
+template <typename T, int W, int S, typename F> __device__ __forceinline__ void gather(const Row<T, W, S>& row, List& list, F over) {
     constexpr int N = RowVec<T>::n;
     if constexpr (S > 0) {
         constexpr int kMarks = (S * N + 31) / 32;
@@ -228,11 +248,10 @@ template <typename T, int W, int S, typename F> __device__ __forceinline__ void 
         row.each_vec([&](int s, int, const auto& v) {
 #pragma unroll
             for (int e = 0; e < N; ++e) {
-                const float z = to_f32((T)v[e]), over = z - bound;
                 uint32_t& m = marks[(s * N + e) / 32];
-                m = __builtin_amdgcn_alignbit(m, __builtin_bit_cast(uint32_t, over), 31);  // the sign from the right
-                f(z, over);
+                m = __builtin_amdgcn_alignbit(m, __builtin_bit_cast(uint32_t, over(to_f32((T)v[e]))), 31);  // the sign from the right
             }
+            __builtin_amdgcn_sched_barrier(0);  // one vector after the other, or all have their registers at once
         });
         uint32_t mine = 0;
 #pragma unroll
@@ -259,23 +278,20 @@ template <typename T, int W, int S, typename F> __device__ __forceinline__ void 
             }
     } else {
         row.each([&](float z, int id) {
-            if (z >= bound) put_in(list, z, id);
-            f(z, z - bound);
+            if (over(z) >= 0.f) put_in(list, id);
         });
     }
     __syncthreads();
 }
-// minus infinity in the place of NaN: neither is in the order
-__device__ __forceinline__ float in_order(float z) { return fmaxf(z, -kInf); }
 
 // ---- exact search for the last of the first elements of the order, whatever the row holds ----
 // Digit by digit over histograms of 2^BITS bins: first of the distance to the largest logit (its floating point bits: 16 powers of two, from 2^-10 to 2^6,
 // have as many bins each), then of the logit's own bits, then of the id's, until the bin that the border falls into has at most kList elements; those
-// are compared one by one.  Elements are counted, or (WEIGHTS) their weights are added up: whole numbers, so the order of the atomic additions does not matter.
-template <int W, int BITS, bool WEIGHTS> struct Search {
+// are compared one by one.  Weights are whole numbers (1, where elements are counted), so the order of the atomic additions does not matter.
+template <int W, int BITS, bool HAS_W> struct Search {
     uint64_t sum[1 << BITS];
     uint64_t part[W], before;
-    uint64_t w[WEIGHTS ? kList : 1];
+    uint64_t w[HAS_W ? kList : 1];
     int bin;
     Place last;
 };
@@ -286,33 +302,34 @@ template <int BITS> __device__ __forceinline__ int distance_bin(float z, float t
 }
 
 // target: for counts, how many elements the first part has; for weights, the least sum that the part up to its last element reaches; 1 or more, and
-// what is more than there is counts as all.  in(z, id): elements that take part, one at least (with a weight above 0); weight(z): theirs.
-template <bool WEIGHTS, typename T, int W, int BITS, bool HAS_W, typename In, typename Weight>
-__device__ __noinline__ Place find_last(Row<T, W, 0> row, float top, uint64_t target, Search<W, BITS, HAS_W>& h, List& list, In in, Weight weight) {
-    static_assert(HAS_W || !WEIGHTS, "room for the listed elements' weights");
+// what is more than there is counts as all.  in(z, id): elements that take part, one at least (with a weight above 0); weight(z): what each counts.
+template <int BITS, typename R, int W, bool HAS_W, typename In, typename Weight>
+__device__ __forceinline__ Place find_last(const R& row, float top, uint64_t target, Search<W, BITS, HAS_W>& h, List& list, In in, Weight weight) {
     constexpr int kThreads = 64 * W, kBins = 1 << BITS, kEach = kBins < kThreads ? 1 : kBins / kThreads, kIdBits = 18;
     static_assert(kMostVocab <= 1 << kIdBits, "an id's digits");
     constexpr int kZLevels = (32 + BITS - 1) / BITS, kLevels = 1 + kZLevels + (kIdBits + BITS - 1) / BITS;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int bin0 = 0;
-    uint32_t bits = 0, id_bits = 0;  // digits found so far
+    uint32_t bits = 0, id_bits = 0;      // digits found so far
     int known = 32, id_known = kIdBits;  // and how many bits are below them
-    uint64_t passed = 0;             // in front of the bin
+    uint64_t passed = 0;                 // in front of the bin
     for (int level = 0;; ++level) {
-        auto member = [&](float z, int id) {
-            if (!(z > -kInf) || !in(z, id)) return false;
-            if (level > 0 && distance_bin<BITS>(z, top) != bin0) return false;
-            return (uint64_t)(~rising_bits(z) ^ bits) >> known == 0 && (((uint32_t)id ^ id_bits) >> id_known) == 0;
-        };
         const bool by_z = level <= kZLevels;
         const int have = by_z ? known : id_known, take = min(BITS, have), shift = have - take;
         for (int i = tid; i < kBins; i += kThreads) h.sum[i] = 0;
         __syncthreads();
-        row.each([&](float z, int id) {
-            if (!member(z, id)) return;
-            const int digit = level == 0 ? distance_bin<BITS>(z, top) : ((by_z ? ~rising_bits(z) : (uint32_t)id) >> shift) & ((1u << take) - 1);
-            atomicAdd((unsigned long long*)&h.sum[digit], WEIGHTS ? (unsigned long long)weight(z) : 1ull);
-        });
+        if (level == 0) {
+            row.each([&](float z, int id) {
+                if (z > -kInf && in(z, id)) atomicAdd((unsigned long long*)&h.sum[distance_bin<BITS>(z, top)], (unsigned long long)weight(z));
+            });
+        } else {
+            row.each([&](float z, int id) {
+                if (!(z > -kInf) || distance_bin<BITS>(z, top) != bin0 || !in(z, id)) return;
+                const uint32_t falling = ~rising_bits(z);
+                if ((uint64_t)(falling ^ bits) >> known != 0 || ((uint32_t)id ^ id_bits) >> id_known != 0) return;
+                atomicAdd((unsigned long long*)&h.sum[((by_z ? falling : (uint32_t)id) >> shift) & ((1u << take) - 1)], (unsigned long long)weight(z));
+            });
+        }
         __syncthreads();
         uint64_t mine = 0;
         if (tid < kBins)
@@ -348,32 +365,31 @@ __device__ __noinline__ Place find_last(Row<T, W, 0> row, float top, uint64_t ta
             id_bits |= (uint32_t)h.bin << shift;
             id_known = shift;
         }
-        const int next = level + 1;
         row.each([&](float z, int id) {
-            if (!(z > -kInf) || !in(z, id) || distance_bin<BITS>(z, top) != bin0) return;
-            if ((uint64_t)(~rising_bits(z) ^ bits) >> known == 0 && (((uint32_t)id ^ id_bits) >> id_known) == 0) put_in(list, z, id);
+            if (!(z > -kInf) || distance_bin<BITS>(z, top) != bin0 || !in(z, id)) return;
+            if ((uint64_t)(~rising_bits(z) ^ bits) >> known == 0 && ((uint32_t)id ^ id_bits) >> id_known == 0) put_in(list, id);
         });
         __syncthreads();
-        if (list.count <= kList || next == kLevels) break;
+        if (list.count <= kList || level + 1 == kLevels) break;
         __syncthreads();  // all have read the count
     }
     const int n = min((int)list.count, kList);
-    if constexpr (WEIGHTS) {
-        for (int i = tid; i < n; i += kThreads) h.w[i] = weight(list.z[i]);
-        __syncthreads();
+    read_keys(row, list, n);
+    if constexpr (HAS_W) {
+        for (int i = tid; i < n; i += kThreads) h.w[i] = weight(in_order(to_f32(row.p[list.id[i]])));
     }
+    __syncthreads();
     for (int i = tid; i < n; i += kThreads) {
-        const float z = list.z[i];
-        const int id = list.id[i];
+        const uint64_t key = list.key[i];
         uint64_t at = passed, own = 1;
-        if constexpr (WEIGHTS) own = h.w[i];
-#pragma unroll 4
-        for (int j = 0; j < n; ++j) {
-            uint64_t w = 1;
-            if constexpr (WEIGHTS) w = h.w[j];
-            if (before(list.z[j], list.id[j], z, id)) at += w;
+        if constexpr (HAS_W) {
+            own = h.w[i];
+#pragma unroll 8
+            for (int j = 0; j < n; ++j) at += list.key[j] > key ? h.w[j] : 0;
+        } else {
+            at += place_of(list, key, n);
         }
-        if (at < target && target <= at + own) h.last = Place{z, id};
+        if (at < target && target <= at + own) h.last = Place{key_logit(key), key_id(key)};
     }
     __syncthreads();
     const Place last = h.last;
