@@ -67,6 +67,16 @@ template <size_t N> aed_status check_words(const char* names, const void* const 
     return AED_OK;
 }
 
+constexpr double kLog2e = 1.4426950408889634074;
+void set_temperature(const aed_distill_config& c, aed::DistillArgs& a) {
+    const double t = c.temperature;
+    a.top = c.top;
+    a.temperature = c.temperature;
+    a.scale_d = kLog2e / t;
+    a.scale = (float)a.scale_d;
+    a.factor = t * t / kLog2e;
+}
+
 }  // namespace
 
 struct aed_sampler : Plan<aed_sampler_config> {};
@@ -132,7 +142,7 @@ aed_status aed_top_logits(aed_top* p, const void* logits, int64_t row_stride, in
     a.rest = rest;
     a.top = p->cfg.top;
     a.temperature = p->cfg.temperature;
-    a.scale = (float)(1.4426950408889634074 / (double)p->cfg.temperature);
+    a.scale = (float)(kLog2e / (double)p->cfg.temperature);
     return hip_status(aed::launch_top(a, p->cfg.dtype == 1, p->stream), "aed_top_logits");
 }
 
@@ -158,8 +168,7 @@ aed_status aed_distill_forward(aed_distill* p, const void* logits, int64_t row_s
     a.loss = loss;
     a.row_loss = row_loss;
     a.stats = stats;
-    a.top = p->cfg.top;
-    a.temperature = p->cfg.temperature;
+    set_temperature(p->cfg, a);
     return hip_status(aed::launch_distill_forward(a, p->cfg.dtype == 1, p->stream), "aed_distill_forward");
 }
 
@@ -178,8 +187,7 @@ aed_status aed_distill_backward(aed_distill* p, const void* logits, int64_t row_
     a.d_loss = d_loss;
     a.d_logits = d_logits;
     a.d_stride = rows > 1 ? d_row_stride : 0;
-    a.top = p->cfg.top;
-    a.temperature = p->cfg.temperature;
+    set_temperature(p->cfg, a);
     return hip_status(aed::launch_distill_backward(a, p->cfg.dtype == 1, p->stream), "aed_distill_backward");
 }
 

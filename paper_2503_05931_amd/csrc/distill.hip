@@ -7,108 +7,134 @@
 // thousands) is made in forward in 64 bits where it is a small difference of large numbers, its gradients too; backward writes p's multiple
 // everywhere and then the list's own.  p_R is the sum over what is not in the list, found by a bit for each id in LDS, and never a difference to 1: of
 // a student that is sure of the list it is 1e-10 and less.  What lies outside is taken relative to its own largest logit, so that p_i / p_R keeps its digits too.
+#include <algorithm>
+
 #include "vocab_rows.h"
 
 namespace aed {
 
 namespace {
 
-// (maximum, sum of exponentials relative to it): of two parts
+// Largest logit and the sum of 2^((z - top) scale)
 struct Partial {
-    float m, l;
+    float top, sum;
 };
 __device__ __forceinline__ Partial joined(Partial a, Partial b, float scale) {
-    const float m = fmaxf(a.m, b.m), base = m == -kInf ? 0.f : m;
-    return Partial{m, a.l * __builtin_amdgcn_exp2f((a.m - base) * scale) + b.l * __builtin_amdgcn_exp2f((b.m - base) * scale)};
+    const float top = fmaxf(a.top, b.top), to = top == -kInf ? 0.f : top;
+    return Partial{top, a.sum * __builtin_amdgcn_exp2f((a.top - to) * scale) + b.sum * __builtin_amdgcn_exp2f((b.top - to) * scale)};
 }
 
-__device__ __forceinline__ double wave_sum_d(double v) {
-#pragma unroll
-    for (int by = 1; by < 64; by *= 2) v += __shfl_xor(v, by);
-    return v;
+// 2^y, minus infinity and NaN as they are
+__device__ __forceinline__ double exactly(const Pow2& pow2, double y) { return y != y ? y : pow2(y); }
+// log2 x of x > 0 that is near to what a float can be: that of the float nearest, and of what 2 to its power lacks
+__device__ __forceinline__ double log2_of(const Pow2& pow2, double x) {
+    const double near = __builtin_amdgcn_logf((float)x), left = x * pow2(-near) - 1;  // some 1e-7
+    return near + left * (1 - 0.5 * left) * kLog2eD;
 }
 
-constexpr int kPer = kMostTop / 64;  // entries of a lane
+constexpr int kMarks = 8192;  // ids of a list that fall on the same of so many bits may be the same
 
 }  // namespace
 
-// W wavefronts a row, S vectors of it a thread at once.  OTHERS: what is not in the list is a class of its own.  LDS: a bit for each id, with OTHERS.
-template <typename T, int W, int S, bool OTHERS> __global__ __launch_bounds__(64 * W) void distill_rows_kernel(DistillArgs a) {
+// W wavefronts a row, S vectors of it a thread at once, E entries of the list a lane.  OTHERS: what is not in the list is a class of its own.  LDS: a bit for
+// each id, or for the last digits of each.
+template <typename T, int W, int S, int E, bool OTHERS> __global__ __launch_bounds__(64 * W) void distill_rows_kernel(DistillArgs a) {
     typedef typename RowVec<T>::type V;
     constexpr int N = RowVec<T>::n, kThreads = 64 * W;
     extern __shared__ uint32_t listed[];
     __shared__ Partial parts[W];
     const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, K = a.top, vocab = a.z.vocab;
     float* const stats = a.stats + (int64_t)r * (K + 2);
+    // the list: entry 64 i + lane
+    float value[E], at[E];
+    int id[E];
+    bool valid[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+        const int k = min(64 * i + lane, K - 1);
+        value[i] = a.values[(int64_t)r * K + k];
+        id[i] = a.ids[(int64_t)r * K + k];
+    }
     if (a.weights && a.weights[r] == 0.f) {
         if (tid == 0) a.row_loss[r] = 0.f;
         return;
     }
     const T* const z = static_cast<const T*>(a.z.data) + r * a.z.stride;
-    const float scale = (float)(kLog2eD / (double)a.temperature);
-
-    // the list: entry 64 i + lane
-    float value[kPer], at[kPer];
-    int id[kPer];
-    bool valid[kPer];
+    const int vecs = (vocab + N - 1) / N, steps = (vecs + kThreads * S - 1) / (kThreads * S);
+    V x[S];
+    auto read = [&](int step) {
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        const int k = 64 * i + lane;
-        value[i] = -kInf;
-        id[i] = -1;
-        at[i] = -kInf;
-        if (k < K) {
-            value[i] = a.values[(int64_t)r * K + k];
-            id[i] = a.ids[(int64_t)r * K + k];
+        for (int i = 0; i < S; ++i) {
+            const int first = ((step * S + i) * kThreads + tid) * N;
+            if (((step * S + i) * kThreads + kThreads) * N <= vocab) x[i] = *reinterpret_cast<const typename RowVec<T>::any*>(z + first);
+            else x[i] = row_vec(z, first, vocab);
         }
-        valid[i] = (unsigned)id[i] < (unsigned)vocab && value[i] != -kInf;
+    };
+    read(0);
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+        valid[i] = 64 * i + lane < K && (unsigned)id[i] < (unsigned)vocab && value[i] != -kInf;
         if (!valid[i]) id[i] = -1;
-        else if (wave == 0) at[i] = to_f32(z[id[i]]);
+        at[i] = -kInf;
+        if (valid[i] && wave == 0) at[i] = to_f32(z[id[i]]);
     }
-    if constexpr (OTHERS) {
-        for (int i = tid; i < (vocab + 31) / 32; i += kThreads) listed[i] = 0;
+    bool twice = false;  // an id may stand twice in the list
+    {
+        const int words = (min(vocab, OTHERS ? kMostVocab : kMarks) + 31) / 32;
+        for (int i = tid; i < words; i += kThreads) listed[i] = 0;
         __syncthreads();
         if (wave == 0) {
 #pragma unroll
-            for (int i = 0; i < kPer; ++i)
-                if (valid[i]) atomicOr(&listed[id[i] >> 5], 1u << (id[i] & 31));
+            for (int i = 0; i < E; ++i) {
+                const int mark = OTHERS ? id[i] : id[i] & (kMarks - 1);
+                if (valid[i]) twice |= atomicOr(&listed[mark >> 5], 1u << (mark & 31)) >> (mark & 31) & 1;
+            }
         }
-        __syncthreads();
+        if (OTHERS) __syncthreads();
     }
 
     // the row: all of it, or what is not in the list
+    const float scale = a.scale;
     Partial mine{-kInf, 0.f};
-    const int vecs = (vocab + N - 1) / N;
-    for (int v0 = tid; v0 < (vecs + kThreads * S - 1) / (kThreads * S) * (kThreads * S); v0 += kThreads * S) {
-        V x[S];
-#pragma unroll
-        for (int i = 0; i < S; ++i) x[i] = row_vec(z, (v0 + kThreads * i) * N, vocab);
-        float y[S][N], top = mine.m;
+    for (int step = 0; step < steps; ++step) {
+        float y[S][N], top = mine.top;
 #pragma unroll
         for (int i = 0; i < S; ++i) {
             uint32_t bits = 0;
             if constexpr (OTHERS) {
-                const int first = (v0 + kThreads * i) * N;
+                const int first = ((step * S + i) * kThreads + tid) * N;
                 if (first < vocab) bits = listed[first >> 5] >> (first & 31) << (first - vec_begin<N>(first, vocab));
             }
 #pragma unroll
             for (int e = 0; e < N; ++e) {
                 y[i][e] = to_f32((T)x[i][e]);
-                if constexpr (OTHERS) y[i][e] = bits >> e & 1 ? -kInf : y[i][e];
+                if constexpr (OTHERS) {  // minus infinity under the bit
+                    const uint32_t mask = (int)(bits << (31 - e)) >> 31;
+                    y[i][e] = bits_f32((__builtin_bit_cast(uint32_t, y[i][e]) & ~mask) | (mask & 0xff800000u));
+                }
                 top = fmaxf(top, y[i][e]);
             }
         }
-        const float base = top == -kInf ? 0.f : top;
-        mine.l *= __builtin_amdgcn_exp2f((mine.m - base) * scale);
-        mine.m = top;
+        if (step + 1 < steps) read(step + 1);
+        const float to = top == -kInf ? 0.f : top, product = to * scale;
+        float sum = 0.f;
+        if (!__any(fabsf(product) > 1e37f)) {  // one operation an exponent; what the product is rounded by is the same for all of them
 #pragma unroll
-        for (int i = 0; i < S; ++i)
+            for (int i = 0; i < S; ++i)
 #pragma unroll
-            for (int e = 0; e < N; ++e) mine.l += __builtin_amdgcn_exp2f((y[i][e] - base) * scale);
+                for (int e = 0; e < N; ++e) sum += __builtin_amdgcn_exp2f(fmaf(y[i][e], scale, -product));
+            sum *= __builtin_amdgcn_exp2f(-fmaf(to, scale, -product));
+        } else {
+#pragma unroll
+            for (int i = 0; i < S; ++i)
+#pragma unroll
+                for (int e = 0; e < N; ++e) sum += __builtin_amdgcn_exp2f((y[i][e] - to) * scale);
+        }
+        mine = Partial{top, fmaf(mine.sum, __builtin_amdgcn_exp2f((mine.top - to) * scale), sum)};
     }
     {
-        const float top = wave_max(mine.m), base = top == -kInf ? 0.f : top;
-        mine = Partial{top, wave_sum(mine.l * __builtin_amdgcn_exp2f((mine.m - base) * scale))};
+        const float top = wave_max(mine.top), to = top == -kInf ? 0.f : top;
+        mine = Partial{top, wave_sum(mine.sum * __builtin_amdgcn_exp2f((mine.top - to) * scale))};
     }
     if constexpr (W > 1) {
         if (lane == 0) parts[wave] = mine;
@@ -117,23 +143,22 @@ template <typename T, int W, int S, bool OTHERS> __global__ __launch_bounds__(64
         for (int i = 1; i < W; ++i) mine = joined(mine, parts[i], scale);
     }
 
-    // the list against the row, by one wavefront
-    const double c = 1.0 / (double)a.temperature;
-    const float rest = OTHERS ? a.rest[r] : -kInf;
+    // the list against the row, by one wavefront, in 64 bits; logarithms to base 2
+    const Pow2 pow2;
+    const double c = a.scale_d;
+    const double rest = OTHERS ? (double)a.rest[r] * kLog2eD : -(double)kInf;
     float value_top = -kInf, at_top = -kInf;
-    bool again[kPer];  // the id stands further in front, too
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
+    for (int i = 0; i < E; ++i) {
         value_top = fmaxf(value_top, valid[i] ? value[i] : -kInf);
         at_top = fmaxf(at_top, at[i]);
-        again[i] = false;
     }
     value_top = wave_max(value_top);
     at_top = wave_max(at_top);
-    const double lead = fmax((double)value_top * c, (double)rest);
+    const double lead = fmax((double)value_top * c, rest);
     if (lead == -(double)kInf) {  // neither an entry nor a rest
 #pragma unroll
-        for (int i = 0; i < kPer; ++i)
+        for (int i = 0; i < E; ++i)
             if (64 * i + lane < K) stats[2 + 64 * i + lane] = kLeftOut;
         if (lane == 0) {
             stats[0] = stats[1] = 0.f;
@@ -141,84 +166,75 @@ template <typename T, int W, int S, bool OTHERS> __global__ __launch_bounds__(64
         }
         return;
     }
-    // the teacher's
-    double log_q[kPer], q[kPer], n = 0;
+    // the teacher's, and the student's relative to its largest
+    const bool some = mine.top > -kInf;  // of what the row gave
+    const float top = OTHERS ? fmaxf(mine.top, at_top) : mine.top;
+    const double to = top == -kInf ? 0.0 : (double)top, row_top = some ? ((double)mine.top - to) * c : 0.0;
+    double log_q[E], q[E], same[E], p[E], n = 0, total = 0;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
+    for (int i = 0; i < E; ++i) {
         log_q[i] = (double)value[i] * c - lead;
-        q[i] = valid[i] ? exp(log_q[i]) : 0.0;
+        q[i] = valid[i] ? exactly(pow2, log_q[i]) : 0.0;
+        p[i] = valid[i] ? exactly(pow2, ((double)at[i] - to) * c) : 0.0;
         n += q[i];
+        total += p[i];
     }
-    n = wave_sum_d(n);
-    if constexpr (OTHERS) n += exp((double)rest - lead);
-    const double log_n = log(n);
-    double same[kPer];  // q's sum over the entries of the id
+    n = wave_sum(n);
+    // lane 0: the rest's part of n, others: what the row's sum is relative to the student's largest
+    const double uniform = exactly(pow2, lane == 0 ? rest - lead : row_top);
+    const double q_others = OTHERS ? lane_of(uniform, 0) : 0.0, shift = lane_of(uniform, 1), others = (double)mine.sum * shift;
+    n += q_others;
+    if (__any(twice)) {  // entries of one id share what they have; the first of them counts for p
+        for (int i = 0; i < E; ++i) same[i] = 0;
+        total = 0;
+        bool again[E];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        log_q[i] -= log_n;
-        q[i] = valid[i] ? q[i] / n : 0.0;
-        same[i] = q[i];
-    }
-    bool any = false;
-    for (int k = 0; k < K; ++k) {
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            if (k >> 6 != j) continue;
-            const int other = __builtin_amdgcn_readlane(id[j], k & 63);
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                again[i] |= other == id[i] && k < 64 * i + lane;
-                any |= other == id[i] && k != 64 * i + lane && valid[i];
-            }
-        }
-    }
-    if (__any(any)) {
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) same[i] = 0;
+        for (int i = 0; i < E; ++i) again[i] = false;
         for (int k = 0; k < K; ++k) {
 #pragma unroll
-            for (int j = 0; j < kPer; ++j) {
+            for (int j = 0; j < E; ++j) {
                 if (k >> 6 != j) continue;
                 const int other = __builtin_amdgcn_readlane(id[j], k & 63);
-                const double more = __shfl(q[j], k & 63);
+                const double more = lane_of(q[j], k & 63);
 #pragma unroll
-                for (int i = 0; i < kPer; ++i) same[i] += other == id[i] ? more : 0.0;
+                for (int i = 0; i < E; ++i) {
+                    same[i] += other == id[i] ? more : 0.0;
+                    again[i] |= other == id[i] && k < 64 * i + lane;
+                }
             }
         }
-    }
-    // the student's
-    const float top = OTHERS ? fmaxf(mine.m, at_top) : mine.m;
-    const double base = top == -kInf ? 0.0 : (double)top;
-    double e[kPer], total = 0;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        e[i] = valid[i] ? exp(((double)at[i] - base) * c) : 0.0;
-        total += again[i] ? 0.0 : e[i];
+        for (int i = 0; i < E; ++i) total += again[i] ? 0.0 : p[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < E; ++i) same[i] = q[i];
     }
-    const double shift = exp((mine.m == -kInf ? 0.0 : (double)mine.m - base) * c), others = (double)mine.l * shift;
-    total = OTHERS ? wave_sum_d(total) + others : others;
-    const double log_total = total == 0 ? 0.0 : log(total);  // no logit at all: every p is 0
+    total = OTHERS ? wave_sum(total) + others : others;
+    // lane 0: of n, 1: of the student's sum, 2: of what the row gave
+    const double of = lane == 0 ? n : lane == 1 ? total : (double)mine.sum;
+    const double inverse = of > 0 ? 1 / of : of == 0 ? 0 : of, log_of = of == 0 ? 0.0 : log2_of(pow2, of);  // NaN stays; without any logit every p is 0
+    const double n_inverse = lane_of(inverse, 0), total_inverse = lane_of(inverse, 1), log_n = lane_of(log_of, 0), log_total = lane_of(log_of, 1);
     double row = 0;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i)
-        if (q[i] != 0) row += q[i] * (log_q[i] - (((double)at[i] - base) * c - log_total));
-    row = wave_sum_d(row);
-    const double inverse = total > 0 ? 1 / total : total == 0 ? 0 : total;  // NaN stays
-    const bool some = mine.m > -kInf;  // outside of the list: p_i = exp((z_i - s0) / T) s1, less what p_R takes
-    double outside = shift * inverse;
+    for (int i = 0; i < E; ++i) {
+        q[i] *= n_inverse;
+        if (q[i] != 0) row += q[i] * (log_q[i] - log_n - (((double)at[i] - to) * c - log_total));
+    }
+    row = wave_sum(row);
+    double outside = shift * total_inverse;  // p_i = 2^((z_i - top) scale) of this, less what p_R takes
     if constexpr (OTHERS) {
-        const double log_rest = (double)rest - lead - log_n, q_rest = exp(log_rest);
-        const double log_others = some ? log((double)mine.l) + ((double)mine.m - base) * c : -(double)kInf;
-        if (q_rest != 0) row += q_rest * (log_rest - (log_others - log_total));
-        outside -= q_rest / (double)mine.l;
+        const double q_rest = q_others * n_inverse;
+        const double log_others = some ? lane_of(log_of, 2) + row_top : -(double)kInf;
+        if (q_rest != 0) row += q_rest * (rest - lead - log_n - (log_others - log_total));
+        outside -= q_rest * lane_of(inverse, 2);
     }
 #pragma unroll
-    for (int i = 0; i < kPer; ++i)
-        if (64 * i + lane < K) stats[2 + 64 * i + lane] = valid[i] ? (float)(e[i] * inverse - same[i]) : kLeftOut;
+    for (int i = 0; i < E; ++i)
+        if (64 * i + lane < K) stats[2 + 64 * i + lane] = valid[i] ? (float)(p[i] * total_inverse - same[i] * n_inverse) : kLeftOut;
     if (lane == 0) {
-        stats[0] = some ? mine.m : 0.f;
+        stats[0] = some ? mine.top : 0.f;
         stats[1] = some ? (float)outside : 0.f;
-        a.row_loss[r] = (float)((double)a.temperature * (double)a.temperature * row);
+        a.row_loss[r] = (float)(a.factor * row);
     }
 }
 
@@ -227,11 +243,18 @@ __global__ __launch_bounds__(1024) void distill_loss_kernel(DistillArgs a) {
     const int tid = threadIdx.x;
     __shared__ double part[16];
     double v = 0;
-    for (int r = tid; r < a.z.rows; r += 1024) {
-        const float w = a.weights ? a.weights[r] : 1.f;
-        v += w == 0.f ? 0.0 : (double)w * (double)a.row_loss[r];
+    for (int first = tid; first < a.z.rows; first += 8192) {
+        float w[8], l[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = min(first + 1024 * i, a.z.rows - 1);
+            w[i] = a.weights ? a.weights[r] : 1.f;
+            l[i] = a.row_loss[r];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v += w[i] == 0.f || first + 1024 * i >= a.z.rows ? 0.0 : (double)w[i] * (double)l[i];
     }
-    v = wave_sum_d(v);
+    v = wave_sum(v);
     if ((tid & 63) == 0) part[tid >> 6] = v;
     __syncthreads();
     if (tid == 0) {
@@ -268,7 +291,7 @@ template <typename T, int W, int S> __global__ __launch_bounds__(64 * W) void di
         for (int v = tid; v < vecs; v += kThreads) put(v, (V)(from_f32<T>(0.f)));
         return;
     }
-    const float scale = (float)(kLog2eD / (double)a.temperature), slope = w * a.temperature * (a.d_loss ? a.d_loss[0] : 1.f);
+    const float scale = a.scale, slope = w * a.temperature * (a.d_loss ? a.d_loss[0] : 1.f);
     const float s0 = stats[0], s1 = slope * stats[1];
     for (int v0 = tid; v0 < vecs; v0 += kThreads * S) {
         V x[S];
@@ -295,16 +318,17 @@ template <typename T, int W, int S> __global__ __launch_bounds__(64 * W) void di
 
 namespace {
 
-template <typename T, int W, int S> hipError_t launch_rows_as(const DistillArgs& a, hipStream_t s) {
-    if (a.rest) distill_rows_kernel<T, W, S, true><<<dim3(a.z.rows), dim3(64 * W), (size_t)(a.z.vocab + 31) / 32 * 4, s>>>(a);
-    else distill_rows_kernel<T, W, S, false><<<dim3(a.z.rows), dim3(64 * W), 0, s>>>(a);
+template <typename T, int W, int S, int E> hipError_t launch_rows_as(const DistillArgs& a, hipStream_t s) {
+    const size_t words = (size_t)(std::min(a.z.vocab, a.rest ? kMostVocab : kMarks) + 31) / 32;
+    if (a.rest) distill_rows_kernel<T, W, S, E, true><<<dim3(a.z.rows), dim3(64 * W), words * 4, s>>>(a);
+    else distill_rows_kernel<T, W, S, E, false><<<dim3(a.z.rows), dim3(64 * W), words * 4, s>>>(a);
     return hipGetLastError();
 }
-template <typename T> hipError_t launch_rows_of(const DistillArgs& a, hipStream_t s) {
+template <typename T, int E> hipError_t launch_rows_of(const DistillArgs& a, hipStream_t s) {
     const int vecs = (a.z.vocab + RowVec<T>::n - 1) / RowVec<T>::n;
-    if (vecs <= 64 * 2) return launch_rows_as<T, 1, 2>(a, s);
-    if (vecs <= 64 * 16) return launch_rows_as<T, 1, 8>(a, s);
-    return launch_rows_as<T, 4, 8>(a, s);
+    if (vecs <= 64 * 2) return launch_rows_as<T, 1, 2, E>(a, s);
+    if (vecs <= 64 * 16) return launch_rows_as<T, 1, 4, E>(a, s);
+    return launch_rows_as<T, 4, 4, E>(a, s);
 }
 template <typename T> hipError_t launch_gradient_of(const DistillArgs& a, hipStream_t s) {
     const int vecs = (a.z.vocab + RowVec<T>::n - 1) / RowVec<T>::n;
@@ -317,7 +341,8 @@ template <typename T> hipError_t launch_gradient_of(const DistillArgs& a, hipStr
 
 hipError_t launch_distill_forward(const DistillArgs& a, bool bf16, hipStream_t s) {
     if (a.z.rows > 0) {
-        const hipError_t e = bf16 ? launch_rows_of<bf16_t>(a, s) : launch_rows_of<float>(a, s);
+        const hipError_t e = a.top <= 64 ? bf16 ? launch_rows_of<bf16_t, 1>(a, s) : launch_rows_of<float, 1>(a, s)
+                                        : bf16 ? launch_rows_of<bf16_t, 2>(a, s) : launch_rows_of<float, 2>(a, s);
         if (e != hipSuccess) return e;
     }
     distill_loss_kernel<<<1, 1024, 0, s>>>(a);

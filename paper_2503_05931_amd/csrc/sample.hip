@@ -33,28 +33,17 @@ template <int W, int RUNS> struct SampleLds {
     uint64_t run[RUNS];
 };
 
-// Weights of a row's logits.  2^y for y <= 0: y's nearest whole number n, and 1 + f q(f) for what is left, q of degree 8 fitted to (2^f - 1) / f on [-1/2, 1/2]
-// for the least largest error, 1.6e-14 of the result.  Its coefficients are kept in scalar registers, where a product can take them from.
+// Weights of a row's logits
 struct Weigh {
-    double top, c, q[9];  // c: log2 e / t
-    double magic;         // 2^(52 - bits): a double there has whole multiples of 2^-bits as its last digits, and its own last 32 bits are 0
+    Pow2 pow2;
+    double top, c;  // c: log2 e / t
+    double magic;   // 2^(52 - bits): a double there has whole multiples of 2^-bits as its last digits, and its own last 32 bits are 0
     float top_f;
     __device__ __forceinline__ Weigh(float top, float t, int bits)
-        : top(top), c(t > 0.f ? kLog2eD / (double)t : 0.0),
-          q{0.6931471805598853, 0.24022650695722841, 0.05550410866841879, 0.009618129181143242, 0.0013333557624782767, 0.0001540344090220312, 1.525299054241159e-05,
-            1.3258330955496492e-06, 1.0148218085577417e-07},
-          magic(__builtin_bit_cast(double, (uint64_t)(1023 + 52 - bits) << 52)), top_f(top) {
-#pragma unroll
-        for (int i = 0; i < 9; ++i) asm volatile("" : "+s"(q[i]));
-    }
+        : top(top), c(t > 0.f ? kLog2eD / (double)t : 0.0), magic(__builtin_bit_cast(double, (uint64_t)(1023 + 52 - bits) << 52)), top_f(top) {}
     // exactly 1 for the largest; 0 for minus infinity and NaN, and for all but the largest where that is infinite
     __device__ __forceinline__ double exact(float z) const {
-#pragma clang fp contract(off)  // the same weight wherever it is made
-        const double y = fmax(((double)z - top) * c, -1100.0), n = rint(y), f = y - n;
-        double p = q[8];
-#pragma unroll
-        for (int i = 7; i >= 0; --i) p = fma(f, p, q[i]);
-        const double w = ldexp(fma(f, p, 1.0), (int)n);
+        const double w = pow2(((double)z - top) * c);
         return z == top_f ? 1.0 : w;
     }
     __device__ __forceinline__ uint64_t whole(double w) const {

@@ -49,7 +49,8 @@ struct DistillArgs {
     void* d_logits;
     int64_t d_stride;
     int top;
-    float temperature;
+    float temperature, scale;  // scale: log2 e / temperature
+    double scale_d, factor;    // factor: temperature^2 ln 2
 };
 
 hipError_t launch_sample(const SampleArgs& a, bool bf16, hipStream_t s);

@@ -126,6 +126,23 @@ __device__ __forceinline__ uint64_t wave_sum64(uint64_t v) {
     hi = __builtin_amdgcn_permlane32_swap((uint32_t)(v >> 32), (uint32_t)(v >> 32), false, false);
     return ((uint64_t)hi[0] << 32 | lo[0]) + ((uint64_t)hi[1] << 32 | lo[1]);
 }
+// sum of doubles over a wavefront, in one order
+__device__ __forceinline__ double wave_sum(double v) {
+    auto as_u = [](double d) { return __builtin_bit_cast(uint64_t, d); };
+    auto as_d = [](uint64_t u) { return __builtin_bit_cast(double, u); };
+    v += as_d(dpp_mov64<0xB1>(as_u(v)));
+    v += as_d(dpp_mov64<0x4E>(as_u(v)));
+    v += as_d(dpp_mov64<0x141>(as_u(v)));
+    v += as_d(dpp_mov64<0x140>(as_u(v)));
+    uint64_t u = as_u(v);
+    auto lo = __builtin_amdgcn_permlane16_swap((uint32_t)u, (uint32_t)u, false, false);
+    auto hi = __builtin_amdgcn_permlane16_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
+    v = as_d((uint64_t)hi[0] << 32 | lo[0]) + as_d((uint64_t)hi[1] << 32 | lo[1]);
+    u = as_u(v);
+    lo = __builtin_amdgcn_permlane32_swap((uint32_t)u, (uint32_t)u, false, false);
+    hi = __builtin_amdgcn_permlane32_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
+    return as_d((uint64_t)hi[0] << 32 | lo[0]) + as_d((uint64_t)hi[1] << 32 | lo[1]);
+}
 // a shift within rows of 16 lanes (zeros come in), or a row's last lane to the rows of ROWS
 template <int CTRL, int ROWS = 0xF> __device__ __forceinline__ uint32_t dpp_or0(uint32_t v) {
     return __builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, true);
@@ -163,6 +180,29 @@ __device__ __forceinline__ float lanes_bound(float v, int j) {
     const uint32_t u = t << 16;
     return t <= 0x7f ? -kInf : __builtin_bit_cast(float, (u & 0x80000000u) ? u & 0x7fffffffu : ~u);
 }
+
+__device__ __forceinline__ double lane_of(double v, int l) { return __builtin_bit_cast(double, lane_of(__builtin_bit_cast(uint64_t, v), l)); }
+
+// 2^y: y's nearest whole number n, and 1 + f q(f) for what is left, q of degree 8 fitted to (2^f - 1) / f on [-1/2, 1/2] for the least largest error, 1.6e-14 of
+// the result.  The coefficients are kept in scalar registers, where a product can take them from.  NaN counts as minus infinity.
+struct Pow2 {
+    double q[9];
+    __device__ __forceinline__ Pow2()
+        : q{0.6931471805598853, 0.24022650695722841, 0.05550410866841879, 0.009618129181143242, 0.0013333557624782767, 0.0001540344090220312, 1.525299054241159e-05,
+            1.3258330955496492e-06, 1.0148218085577417e-07} {
+#pragma unroll
+        for (int i = 0; i < 9; ++i) asm volatile("" : "+s"(q[i]));
+    }
+    __device__ __forceinline__ double operator()(double y) const {
+#pragma clang fp contract(off)  // the same result wherever it is made
+        y = fmax(y, -1100.0);
+        const double n = rint(y), f = y - n;
+        double p = q[8];
+#pragma unroll
+        for (int i = 7; i >= 0; --i) p = fma(f, p, q[i]);
+        return ldexp(fma(f, p, 1.0), (int)n);
+    }
+};
 
 // An element's place in the order: of two, the one in front has the larger key
 __device__ __forceinline__ uint64_t order_key(float z, int id) { return (uint64_t)rising_bits(z) << 32 | (uint32_t)~id; }
