@@ -8,7 +8,7 @@
 // thousands (a flat row of 4096) would be its neighbour.
 //
 // One workgroup a row.  Three ways through it, by what the row's own parameters ask for:
-//   list    the filters leave few: those at or above a bound from the lanes' maxima are gathered in LDS and compared with each other
+//   list    the filters leave few: those at or above a bound (from the lanes' maxima, or min-p's) are gathered in LDS and compared with each other
 //   search  they leave many: the end of the first part is searched for by histograms (find_last)
 //   sums    whatever is left is added up by runs of one wavefront's vector (256 or 512 ids in a row); the run that the random number falls into is
 //           then gone through by one wavefront
@@ -101,7 +101,7 @@ template <typename T, int W, int S, int RUNS> __global__ __launch_bounds__(64 * 
     const float u = u0 > 0.f ? fminf(u0, 1.f) : 0.f;
 
     float top, bound;
-    bound_row<W>(row, by_k ? (k <= kMostListed ? k : 1) : by_p ? kWanted : 1, lds.bounds, list, top, bound);
+    bound_row<W>(row, by_k ? (k <= kMostListed ? k : 0) : by_p ? kWanted : 0, lds.bounds, list, top, bound);
     row.forget();
     if (!(top > -kInf)) {  // nothing to draw from
         if (tid == 0) {
@@ -117,22 +117,33 @@ template <typename T, int W, int S, int RUNS> __global__ __launch_bounds__(64 * 
 
     Place last{-kInf, INT_MAX};  // of A, then of B
     bool done = false;
-    if (by_k || by_p) {
-        bool few = !by_k || k <= kMostListed;
+    if (by_k || by_p || least > 0.0) {
         uint64_t all = 0;  // A's sum
-        if (!by_k) {
-            uint64_t mine = 0;
+        const bool needs_a = by_k && by_p;  // A's sum, from the list
+        if (least > 0.0 && !needs_a) {  // what min-p takes out need not be listed; a little below its end, as that is rounded
+            const float end = t * logf((float)least);
+            bound = fmaxf(bound, top + end - 1e-5f * (fabsf(top) + fabsf(end)));
+        }
+        const bool complete = !needs_a && weigh.exact(bound) < least;  // nothing below the bound is in C
+        bound = gather_bound(bound);
+        bool few = complete || (by_k ? k <= kMostListed : by_p);
+        if (by_p && !by_k) {
+            uint64_t mine = 0, above = 0;
             gather(row, list, [&](float z) {
-                mine += weight(z);
-                return z - bound;
+                const uint64_t w = weight(z);
+                const float over = z - bound;
+                mine += w;
+                above += over < 0.f ? 0 : w;
+                return over;
             });
             all = block_sum64<W>(mine, lds.run);
+            few = complete || block_sum64<W>(above, lds.run) >= part_of<true>(top_p, all);  // all of B is listed
         } else if (few) {
             gather(row, list, [&](float z) { return z - bound; });
         }
         const int n = few ? (int)list.count : 0;
-        few = few && n <= kList;
-        if (few) {
+        done = few && n <= kList;
+        if (done) {
             read_keys(row, list, n);
             __syncthreads();
             if (tid < n) {  // its place in the order, and among the ids
@@ -146,49 +157,48 @@ template <typename T, int W, int S, int RUNS> __global__ __launch_bounds__(64 * 
                 lds.by_id[by_id] = key_id(key);
             }
             __syncthreads();
-            // in their order, four a lane, by every wavefront: all have to know whether it is done; the first one answers
+            if (wave != 0) return;
+            // in their order, by one wavefront
             constexpr int kEach = kList / 64;
-            uint64_t w[kEach], mine = 0, of_a = 0;
+            uint64_t w[kEach], of_a = 0;
             double x[kEach];
 #pragma unroll
             for (int i = 0; i < kEach; ++i) {
-                const int place = kEach * lane + i;
-                x[i] = place < n ? weigh.exact(key_logit(lds.key[place])) : 0.0;
-                w[i] = place < n ? weigh.whole(x[i]) : 0;
-                mine += w[i];
+                const int place = 64 * i + lane;
+                x[i] = 0;
+                w[i] = 0;
+                if (64 * i < n && place < n) {
+                    x[i] = weigh.exact(key_logit(lds.key[place]));
+                    w[i] = weigh.whole(x[i]);
+                }
                 of_a += place < k ? w[i] : 0;
             }
-            of_a = wave_sum64(of_a);  // A's sum, or that of its listed part
-            if (by_k) all = of_a;
-            const uint64_t border = by_p ? part_of<true>(top_p, all) : of_a;
-            done = of_a >= border;  // all of B is listed
-            if (done) {
-                if (wave != 0) return;
-                uint64_t front = wave_prefix(mine) - mine;
+            if (by_k && by_p) all = wave_sum64(of_a);
+            const uint64_t border = by_p ? part_of<true>(top_p, all) : 0;
+            uint64_t front = 0;  // of the places that are looked at
 #pragma unroll
-                for (int i = 0; i < kEach; ++i) {
-                    const int place = kEach * lane + i;
-                    const uint64_t kept = place < k && (place == 0 || !by_p || front < border) && x[i] >= least ? w[i] : 0;
-                    front += w[i];
-                    left += kept;
-                    if (place < n) lds.w[lds.by_place[place]] = kept;
+            for (int i = 0; i < kEach; ++i) {
+                if (64 * i >= n) continue;
+                const int place = 64 * i + lane;
+                const uint64_t through = front + wave_prefix(w[i]);
+                const uint64_t kept = place < k && (place == 0 || !by_p || through - w[i] < border) && x[i] >= least ? w[i] : 0;
+                front = lane_of(through, 63);
+                left += kept;
+                if (place < n) lds.w[lds.by_place[place]] = kept;
+            }
+            left = wave_sum64(left);
+            other_lanes_wrote();
+            const uint64_t target = min(part_of<false>(u, left), left - 1);
+            uint64_t at = 0;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                if (64 * i >= n) continue;
+                const uint64_t v = 64 * i + lane < n ? lds.w[64 * i + lane] : 0, through = at + wave_prefix(v);
+                if (through - v <= target && target < through) {
+                    token = lds.by_id[64 * i + lane];
+                    its = v;
                 }
-                left = wave_sum64(left);
-                other_lanes_wrote();
-                const uint64_t target = min(part_of<false>(u, left), left - 1);
-                uint64_t v[kEach];
-                mine = 0;
-#pragma unroll
-                for (int i = 0; i < kEach; ++i) mine += v[i] = kEach * lane + i < n ? lds.w[kEach * lane + i] : 0;
-                uint64_t at = wave_prefix(mine) - mine;
-#pragma unroll
-                for (int i = 0; i < kEach; ++i) {
-                    if (at <= target && target < at + v[i]) {
-                        token = lds.by_id[kEach * lane + i];
-                        its = v[i];
-                    }
-                    at += v[i];
-                }
+                at = lane_of(through, 63);
             }
         }
         // the last of A by number, then that of B by weight
@@ -283,9 +293,10 @@ template <typename T, int W, int S> hipError_t launch_sample_as(const SampleArgs
     return hipGetLastError();
 }
 template <typename T> hipError_t launch_sample_of(const SampleArgs& a, hipStream_t s) {
-    const int vecs = (a.z.vocab + RowVec<T>::n - 1) / RowVec<T>::n;
-    if (vecs <= 256 * 4) return launch_sample_as<T, 4, 4>(a, s);
-    if (vecs <= 1024 * 8) return launch_sample_as<T, 16, 8>(a, s);
+    constexpr int N = RowVec<T>::n;
+    if (a.z.vocab <= 256 * 16) return launch_sample_as<T, 4, 16 / N>(a, s);
+    if (a.z.vocab <= 1024 * 16) return launch_sample_as<T, 16, 16 / N>(a, s);
+    if (a.z.vocab <= 1024 * 32) return launch_sample_as<T, 16, 32 / N>(a, s);
     return launch_sample_as<T, 16, 0>(a, s);
 }
 

@@ -55,6 +55,7 @@ template <typename T, int W, int S> __global__ __launch_bounds__(64 * W) void to
     int32_t* const ids = a.ids + (int64_t)r * K;
     float top, bound;
     bound_row<W>(row, K, lds.bounds, list, top, bound);
+    bound = gather_bound(bound);
     row.forget();
     // Exponents relative to a border that the bound's own product, rounded, is not below.  Where a product could be infinite, the row is searched.
     const float scaled = bound * a.scale, border = scaled - fabsf(scaled) * 0x1p-22f - 0x1p-126f;

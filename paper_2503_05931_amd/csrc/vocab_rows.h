@@ -234,14 +234,14 @@ template <int W> struct RowBounds {
     float top[W], bound[W];
 };
 
-// Every thread has the row's largest logit and the bound, a finite number.
+// Every thread has the row's largest logit and the bound; want 0: minus infinity.
 template <int W, typename R> __device__ __forceinline__ void bound_row(const R& row, int want, RowBounds<W>& lds, List& list, float& top, float& bound) {
     float m = -kInf;
     row.each([&](float z, int) { m = fmaxf(m, z); });  // NaN is passed over
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int full = max(1, min(W, row.n / (64 * R::N))), j = (want + full - 1) / full;
     top = wave_max(m);
-    bound = want <= 1 ? top : j > 64 ? -kInf : lanes_bound(m, j);
+    bound = want == 1 ? top : want == 0 || j > 64 ? -kInf : lanes_bound(m, j);
     if constexpr (W > 1) {
         if (lane == 0) {
             lds.top[wave] = top;
@@ -256,10 +256,13 @@ template <int W, typename R> __device__ __forceinline__ void bound_row(const R& 
             top = fmaxf(top, lds.top[i]);
             bound = i < full ? fminf(bound, lds.bound[i]) : bound;
         }
-        if (want <= 1) bound = top;
+        if (want == 1) bound = top;
     }
+}
+// a bound as gather's differences need it: finite, and -0 for 0, so that -0 less the bound is 0, whose sign says that it is not below
+__device__ __forceinline__ float gather_bound(float bound) {
     bound = fminf(fmaxf(bound, -kMostFloat), kMostFloat);
-    if (bound == 0.f) bound = -0.f;  // so that -0 less the bound is 0, whose sign says that it is not below
+    return bound == 0.f ? -0.f : bound;
 }
 __device__ __forceinline__ void put_in(List& list, int id) {
     const uint32_t at = atomicAdd(&list.count, 1u);
