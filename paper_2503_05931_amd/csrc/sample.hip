@@ -12,21 +12,21 @@
 //   search  they leave many: the end of the first part is searched for by histograms (find_last)
 //   sums    whatever is left is added up by runs of one wavefront's vector (256 or 512 ids in a row); the run that the random number falls into is
 //           then gone through by one wavefront
-#include <type_traits>
-
 #include "vocab_rows.h"
 
 namespace aed {
 
 namespace {
 
-constexpr int kWanted = 64;      // gathered without top-k: a nucleus of a trained model's row is seldom larger
+constexpr int kWanted = 64;      // gathered for top-p: a nucleus of a trained model's row is seldom larger
+constexpr int kFewRows = 512;     // two a compute unit: eight wavefronts each
 constexpr int kMostListed = 128;  // top-k above it goes by search
 
 template <int W, int RUNS> struct SampleLds {
+    static constexpr int kBits = W > 4 ? 11 : 10;
     RowBounds<W> bounds;
     List list;
-    Search<W, 11, true> search;
+    Search<W, kBits> search;
     uint64_t w[kList];    // by id
     uint64_t key[kList];  // by place
     int by_place[kList], by_id[kList];
@@ -42,9 +42,30 @@ struct Weigh {
     __device__ __forceinline__ Weigh(float top, float t, int bits)
         : top(top), c(t > 0.f ? kLog2eD / (double)t : 0.0), magic(__builtin_bit_cast(double, (uint64_t)(1023 + 52 - bits) << 52)), top_f(top) {}
     // exactly 1 for the largest; 0 for minus infinity and NaN, and for all but the largest where that is infinite
+    template <int N> __device__ __forceinline__ void exact(const float (&z)[N], double (&x)[N]) const {
+#pragma clang fp contract(off)  // the same weight wherever it is made
+        constexpr int M = N < 4 ? N : 4;  // as many at once as the registers are for
+#pragma unroll
+        for (int first = 0; first < N; first += M) {
+            double y[M];
+#pragma unroll
+            for (int e = 0; e < M; ++e) y[e] = ((double)z[first + e] - top) * c;
+            pow2(y);
+#pragma unroll
+            for (int e = 0; e < M; ++e) x[first + e] = z[first + e] == top_f ? 1.0 : y[e];
+        }
+    }
     __device__ __forceinline__ double exact(float z) const {
-        const double w = pow2(((double)z - top) * c);
-        return z == top_f ? 1.0 : w;
+        const float one[1] = {z};
+        double x[1];
+        exact(one, x);
+        return x[0];
+    }
+    template <int N> __device__ __forceinline__ void wholes(const float (&z)[N], uint64_t (&w)[N]) const {
+        double x[N];
+        exact(z, x);
+#pragma unroll
+        for (int e = 0; e < N; ++e) w[e] = whole(x[e]);
     }
     __device__ __forceinline__ uint64_t whole(double w) const {
 #pragma clang fp contract(off)
@@ -81,12 +102,73 @@ template <int W> __device__ __forceinline__ uint64_t block_sum64(uint64_t v, uin
     return v;
 }
 
+// A row and what its elements weigh: held in registers, where these suffice, else made anew for each pass from the row in memory by weights(first id, logits,
+// weights)
+template <typename T, int W, int S> struct Held {
+    static constexpr int N = RowVec<T>::n;
+    const Row<T, W, S>& row;
+    uint64_t (&w)[S][N];
+    template <typename F> __device__ __forceinline__ void logits(F f) const {
+        row.each_floats([&](int, int, float (&z)[N]) {
+            anew(z);
+            f(z);
+        });
+    }
+    template <typename F> __device__ __forceinline__ void each(F f) const {
+        row.each_floats([&](int s, int id, float (&z)[N]) {
+            anew(z);
+            uint64_t v[N];
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                v[e] = w[s][e];
+                asm volatile("" : "+v"(v[e]));
+            }
+            f(id, z, v);
+        });
+    }
+    template <typename Of, typename F> __device__ __forceinline__ void each_if(Of of, F f) const {
+        each([&](int id, const float (&z)[N], const uint64_t (&v)[N]) {
+            if (__any(of(id, z))) f(id, z, v);
+        });
+    }
+    // or what a pass makes of the logits is kept for the next one, and there are no registers for it
+    static __device__ __forceinline__ void anew(float (&z)[N]) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) asm volatile("" : "+v"(z[e]));
+    }
+};
+template <typename T, int W, typename Weights> struct Made {
+    static constexpr int N = RowVec<T>::n;
+    RowLoop<T, W> loop;
+    Weights weights;
+    template <typename F> __device__ __forceinline__ void logits(F f) const {
+        loop.each_floats([&](int, int, float (&z)[N]) { f(z); });
+    }
+    template <typename F> __device__ __forceinline__ void each(F f) const {
+        loop.each_floats([&](int, int id, float (&z)[N]) {
+            uint64_t w[N];
+            weights(id, z, w);
+            f(id, z, w);
+        });
+    }
+    template <typename Of, typename F> __device__ __forceinline__ void each_if(Of of, F f) const {
+        loop.each_floats([&](int, int id, float (&z)[N]) {
+            if (!__any(of(id, z))) return;
+            uint64_t w[N];
+            weights(id, z, w);
+            f(id, z, w);
+        });
+    }
+};
+
 }  // namespace
 
-template <typename T, int W, int S, int RUNS> __global__ __launch_bounds__(64 * W) void sample_kernel(SampleArgs a) {
+template <typename T, int W, int S, int RUNS> __global__ __launch_bounds__(64 * W, 4) void sample_kernel(SampleArgs a) {
     constexpr int N = RowVec<T>::n;
-    static_assert(64 * W >= kList && RUNS >= W, "a thread for each that is listed, sums of wavefronts in the runs' place");
-    __shared__ SampleLds<W, RUNS> lds;
+    constexpr bool kHeld = S > 0 && S * N <= 8;  // a thread's weights have room in registers
+    static_assert(64 * W >= kList && RUNS >= 2 * W, "a thread for each that is listed, sums of wavefronts in the runs' place");
+    typedef SampleLds<W, RUNS> Lds;
+    __shared__ Lds lds;
     List& list = lds.list;
     const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     Row<T, W, S> row(a.z, r);
@@ -96,7 +178,9 @@ template <typename T, int W, int S, int RUNS> __global__ __launch_bounds__(64 * 
     k = greedy ? 1 : k <= 0 || k > a.z.vocab ? a.z.vocab : k;
     const float given_p = greedy ? 1.f : a.top_ps ? a.top_ps[r] : a.top_p, top_p = fmaxf(given_p, 0.f), min_p = a.min_ps ? a.min_ps[r] : a.min_p;
     const bool by_k = k < a.z.vocab, by_p = given_p < 1.f;  // not by NaN
-    const double least = greedy || !(min_p > 0.f) ? 0.0 : (double)fminf(min_p, 1.f);
+    const float least = greedy || !(min_p > 0.f) ? 0.f : fminf(min_p, 1.f);
+    // the least weight that min-p leaves
+    const uint64_t least_w = (uint64_t)ceil((double)least * __builtin_bit_cast(double, (uint64_t)(1023 + a.weight_bits) << 52));
     const float u0 = a.uniforms[r];
     const float u = u0 > 0.f ? fminf(u0, 1.f) : 0.f;
 
@@ -111,47 +195,61 @@ template <typename T, int W, int S, int RUNS> __global__ __launch_bounds__(64 * 
         return;
     }
     const Weigh weigh(top, greedy ? 0.f : t, a.weight_bits);
-    auto weight = [&](float z) { return weigh.whole(weigh.exact(z)); };
+    const RowLoop<T, W> loop{row.p, row.n};
+    uint64_t held[kHeld ? S : 1][N];
     int token = -1;  // of the lane that finds it
     uint64_t its = 0, left = 0;
 
     Place last{-kInf, INT_MAX};  // of A, then of B
-    bool done = false;
-    if (by_k || by_p || least > 0.0) {
+    const bool by_least = least > 0.f, needs_a = by_k && by_p;  // A's sum, from the list
+    if (by_k || by_p || by_least) {
         uint64_t all = 0;  // A's sum
-        const bool needs_a = by_k && by_p;  // A's sum, from the list
-        if (least > 0.0 && !needs_a) {  // what min-p takes out need not be listed; a little below its end, as that is rounded
-            const float end = t * logf((float)least);
-            bound = fmaxf(bound, top + end - 1e-5f * (fabsf(top) + fabsf(end)));
+        float least_bound = -kInf;
+        if (by_least && !needs_a) {  // what min-p takes out need not be listed; a little below its end, as that is rounded
+            const float end = t * logf(least);
+            least_bound = fmaxf(top + end - 1e-5f * (fabsf(top) + fabsf(end)), -kInf);
         }
-        const bool complete = !needs_a && weigh.exact(bound) < least;  // nothing below the bound is in C
-        bound = gather_bound(bound);
+        const bool complete = least_bound >= bound && weigh.whole(weigh.exact(least_bound)) < least_w;  // nothing below min-p's end is in C
+        bound = gather_bound(fmaxf(bound, least_bound));
         bool few = complete || (by_k ? k <= kMostListed : by_p);
         if (by_p && !by_k) {
             uint64_t mine = 0, above = 0;
-            gather(row, list, [&](float z) {
-                const uint64_t w = weight(z);
-                const float over = z - bound;
-                mine += w;
-                above += over < 0.f ? 0 : w;
-                return over;
+            row.each_floats([&](int s, int, float (&z)[N]) {
+                uint64_t w[N];
+                weigh.wholes(z, w);
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    mine += w[e];
+                    above += z[e] - bound >= 0.f ? w[e] : 0;
+                    if constexpr (kHeld) held[s][e] = w[e];
+                }
+                __builtin_amdgcn_sched_barrier(0);
             });
             all = block_sum64<W>(mine, lds.run);
-            few = complete || block_sum64<W>(above, lds.run) >= part_of<true>(top_p, all);  // all of B is listed
-        } else if (few) {
-            gather(row, list, [&](float z) { return z - bound; });
+            few = complete || block_sum64<W>(above, lds.run + W) >= part_of<true>(top_p, all);  // all of B is listed
+            row.forget();
         }
+        if (!few && least_bound > -kInf && weigh.whole(weigh.exact(least_bound)) < least_w) {  // perhaps min-p leaves few
+            bound = gather_bound(least_bound);
+            few = true;
+        }
+        if (few)
+            gather(row, list, [&](float (&z)[N]) {
+#pragma unroll
+                for (int e = 0; e < N; ++e) z[e] -= bound;
+            });
         const int n = few ? (int)list.count : 0;
-        done = few && n <= kList;
-        if (done) {
-            read_keys(row, list, n);
+        if (few && n <= kList) {
+            read_keys<W>(row.p, list, n);
             __syncthreads();
             if (tid < n) {  // its place in the order, and among the ids
                 const uint64_t key = list.key[tid];
-                const int place = place_of(list, key, n);
-                int by_id = 0;
+                int place = 0, by_id = 0;
 #pragma unroll 8
-                for (int j = 0; j < n; ++j) by_id += (uint32_t)list.key[j] > (uint32_t)key;
+                for (int j = 0; j < n; ++j) {
+                    place += list.key[j] > key;
+                    by_id += (uint32_t)list.key[j] > (uint32_t)key;
+                }
                 lds.key[place] = key;
                 lds.by_place[place] = by_id;
                 lds.by_id[by_id] = key_id(key);
@@ -161,19 +259,14 @@ template <typename T, int W, int S, int RUNS> __global__ __launch_bounds__(64 * 
             // in their order, by one wavefront
             constexpr int kEach = kList / 64;
             uint64_t w[kEach], of_a = 0;
-            double x[kEach];
 #pragma unroll
             for (int i = 0; i < kEach; ++i) {
                 const int place = 64 * i + lane;
-                x[i] = 0;
                 w[i] = 0;
-                if (64 * i < n && place < n) {
-                    x[i] = weigh.exact(key_logit(lds.key[place]));
-                    w[i] = weigh.whole(x[i]);
-                }
+                if (64 * i < n) w[i] = weigh.whole(weigh.exact(place < n ? key_logit(lds.key[place]) : -kInf));
                 of_a += place < k ? w[i] : 0;
             }
-            if (by_k && by_p) all = wave_sum64(of_a);
+            if (needs_a) all = wave_sum64(of_a);
             const uint64_t border = by_p ? part_of<true>(top_p, all) : 0;
             uint64_t front = 0;  // of the places that are looked at
 #pragma unroll
@@ -181,7 +274,7 @@ template <typename T, int W, int S, int RUNS> __global__ __launch_bounds__(64 * 
                 if (64 * i >= n) continue;
                 const int place = 64 * i + lane;
                 const uint64_t through = front + wave_prefix(w[i]);
-                const uint64_t kept = place < k && (place == 0 || !by_p || through - w[i] < border) && x[i] >= least ? w[i] : 0;
+                const uint64_t kept = place < k && (place == 0 || !by_p || through - w[i] < border) && w[i] >= least_w ? w[i] : 0;
                 front = lane_of(through, 63);
                 left += kept;
                 if (place < n) lds.w[lds.by_place[place]] = kept;
@@ -200,84 +293,130 @@ template <typename T, int W, int S, int RUNS> __global__ __launch_bounds__(64 * 
                 }
                 at = lane_of(through, 63);
             }
+            if (token >= 0) {  // one lane
+                a.tokens[r] = token;
+                a.logp[r] = (float)log((double)its / (double)left);
+            }
+            return;
         }
         // the last of A by number, then that of B by weight
-        for (int step = 0; step < 2 && !done; ++step) {
+        __syncthreads();
+        const Place everything{-kInf, INT_MAX};
+        auto search = [&](const Place& among, bool by_weight, uint64_t target) {
+            const float span = by_weight ? t * 45.f : kInf;  // a weight of e^-45 is nothing in units of 2^-50
+            if constexpr (kHeld) return find_last<T>(Held<T, W, S>{row, held}, top, span, target, lds.search, list);
+            auto weights = [&](int id, const float (&z)[N], uint64_t (&w)[N]) {
+                if (by_weight) weigh.wholes(z, w);
+#pragma unroll
+                for (int e = 0; e < N; ++e) w[e] = z[e] > -kInf && up_to(z[e], id + e, among) ? by_weight ? w[e] : 1 : 0;
+            };
+            return find_last<T>(Made<T, W, decltype(weights)>{loop, weights}, top, span, target, lds.search, list);
+        };
+        for (int step = 0; step < 2; ++step) {
             const bool by_weight = step == 1;
             if (by_weight ? !by_p : !by_k) continue;
-            __syncthreads();
+            if constexpr (kHeld) {
+                if (by_k)  // 1 each, or those of A
+                    row.each_floats([&](int s, int id, float (&z)[N]) {
+                        uint64_t w[N];
+                        if (by_weight) weigh.wholes(z, w);
+#pragma unroll
+                        for (int e = 0; e < N; ++e) held[s][e] = z[e] > -kInf && up_to(z[e], id + e, last) ? by_weight ? w[e] : 1 : 0;
+                        __builtin_amdgcn_sched_barrier(0);
+                    });
+            }
             if (by_weight && by_k) {
                 uint64_t mine = 0;
-                row.again().each([&](float z, int id) { mine += up_to(z, id, last) ? weight(z) : 0; });
+                if constexpr (kHeld) {
+#pragma unroll
+                    for (int s = 0; s < S; ++s)
+#pragma unroll
+                        for (int e = 0; e < N; ++e) mine += held[s][e];
+                } else {
+                    loop.each_floats([&](int, int id, float (&z)[N]) {
+                        uint64_t w[N];
+                        weigh.wholes(z, w);
+#pragma unroll
+                        for (int e = 0; e < N; ++e) mine += up_to(z[e], id + e, last) ? w[e] : 0;
+                    });
+                }
                 all = block_sum64<W>(mine, lds.run);
             }
-            const uint64_t target = by_weight ? max(part_of<true>(top_p, all), (uint64_t)1) : (uint64_t)k;
-            const Place of_a = last;
-            last = find_last<11>(row.again(), top, target, lds.search, list, [=](float z, int id) { return up_to(z, id, of_a); },
-                                 [&](float z) { return by_weight ? weight(z) : 1; });
+            last = search(last, by_weight, by_weight ? max(part_of<true>(top_p, all), (uint64_t)1) : (uint64_t)k);
         }
     }
-    if (!done) {
-        row.forget();
-        // runs' sums of what is left
-        const bool filtered = by_k || by_p || least > 0.0;
-        auto add_runs = [&](auto some) {
-            row.each_vec([&](int s, int id, const auto& v) {
-                uint64_t mine = 0;
+    // runs' sums of what is left
+    const bool filtered = by_k || by_p || by_least;
+    auto add_run = [&](int s, uint64_t mine) {
+        mine = wave_sum64(mine);
+        if (lane == 0) lds.run[s * W + wave] = mine;
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    if (filtered) {
+        auto left_of = [&](int id, const float (&z)[N], const uint64_t (&w)[N]) {
+            uint64_t mine = 0;
 #pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const float z = to_f32((T)v[e]);
-                    const double x = weigh.exact(z);
-                    uint64_t w = weigh.whole(x);
-                    if constexpr (decltype(some)::value) w = up_to(z, id + e, last) && x >= least ? w : 0;
-                    mine += w;
-                }
-                mine = wave_sum64(mine);
-                if (lane == 0) lds.run[s * W + wave] = mine;
-                __builtin_amdgcn_sched_barrier(0);
-            });
+            for (int e = 0; e < N; ++e) mine += up_to(z[e], id + e, last) && w[e] >= least_w ? w[e] : 0;
+            return mine;
         };
-        if (filtered) add_runs(std::true_type());
-        else add_runs(std::false_type());
-        __syncthreads();
-        if (wave != 0) return;
-        const int runs = ((a.z.vocab + N - 1) / N + 63) / 64;
-        for (int i = lane; i < runs; i += 64) left += lds.run[i];
-        left = wave_sum64(left);
-        const uint64_t target = min(part_of<false>(u, left), left - 1);
-        uint64_t at = 0;  // in front of the runs that are looked at
-        int found = -1;
-        for (int first = 0; found < 0 && first < runs; first += 64) {
-            const uint64_t v = first + lane < runs ? lds.run[first + lane] : 0, through = at + wave_prefix(v);
-            const uint64_t hit = __ballot(through > target);
-            if (hit) {
-                const int l = __builtin_ctzll(hit);
-                found = first + l;
-                at = lane_of(through - v, l);
-            } else {
-                at = lane_of(through, 63);
-            }
+        if (kHeld && by_p) {  // they are there
+            if constexpr (kHeld) row.each_floats([&](int s, int id, float (&z)[N]) { add_run(s, left_of(id, z, held[s])); });
+        } else {
+            loop.each_floats([&](int s, int id, float (&z)[N]) {
+                uint64_t w[N];
+                weigh.wholes(z, w);
+                add_run(s, left_of(id, z, w));
+            });
         }
-        // the run's ids, N a lane
-        const int id0 = (found * 64 + lane) * N, id = vec_begin<N>(id0, a.z.vocab);
-        const auto v = row_vec(row.p, id0, a.z.vocab);
-        uint64_t w[N], mine = 0;
+    } else {
+        row.each_floats([&](int s, int, float (&z)[N]) {
+            uint64_t w[N], mine = 0;
+            weigh.wholes(z, w);
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const float z = to_f32((T)v[e]);
-            const double x = weigh.exact(z);
-            w[e] = up_to(z, id + e, last) && x >= least ? weigh.whole(x) : 0;
-            mine += w[e];
+            for (int e = 0; e < N; ++e) mine += w[e];
+            add_run(s, mine);
+        });
+    }
+    __syncthreads();
+    if (wave != 0) return;
+    const int runs = ((a.z.vocab + N - 1) / N + 63) / 64;
+    for (int i = lane; i < runs; i += 64) left += lds.run[i];
+    left = wave_sum64(left);
+    const uint64_t target = min(part_of<false>(u, left), left - 1);
+    uint64_t at = 0;  // in front of the runs that are looked at
+    int found = -1;
+    for (int first = 0; found < 0 && first < runs; first += 64) {
+        const uint64_t v = first + lane < runs ? lds.run[first + lane] : 0, through = at + wave_prefix(v);
+        const uint64_t hit = __ballot(through > target);
+        if (hit) {
+            const int l = __builtin_ctzll(hit);
+            found = first + l;
+            at = lane_of(through - v, l);
+        } else {
+            at = lane_of(through, 63);
         }
-        at += wave_prefix(mine) - mine;
+    }
+    // the run's ids, N a lane
+    const int id0 = (found * 64 + lane) * N, id = vec_begin<N>(id0, a.z.vocab);
+    const auto v = row_vec(row.p, id0, a.z.vocab);
+    float z[N];
+    uint64_t w[N], mine = 0;
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            if (at <= target && target < at + w[e]) {
-                token = id + e;
-                its = w[e];
-            }
-            at += w[e];
+    for (int e = 0; e < N; ++e) z[e] = to_f32((T)v[e]);
+    weigh.wholes(z, w);
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        w[e] = up_to(z[e], id + e, last) && w[e] >= least_w ? w[e] : 0;
+        mine += w[e];
+    }
+    at += wave_prefix(mine) - mine;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        if (at <= target && target < at + w[e]) {
+            token = id + e;
+            its = w[e];
         }
+        at += w[e];
     }
     if (token >= 0) {  // one lane
         a.tokens[r] = token;
@@ -289,12 +428,12 @@ namespace {
 
 template <typename T, int W, int S> hipError_t launch_sample_as(const SampleArgs& a, hipStream_t s) {
     constexpr int runs = S > 0 ? S * W : kMostVocab / (64 * RowVec<T>::n);
-    sample_kernel<T, W, S, runs><<<dim3(a.z.rows), dim3(64 * W), 0, s>>>(a);
+    sample_kernel<T, W, S, (runs < 2 * W ? 2 * W : runs)><<<dim3(a.z.rows), dim3(64 * W), 0, s>>>(a);
     return hipGetLastError();
 }
 template <typename T> hipError_t launch_sample_of(const SampleArgs& a, hipStream_t s) {
     constexpr int N = RowVec<T>::n;
-    if (a.z.vocab <= 256 * 16) return launch_sample_as<T, 4, 16 / N>(a, s);
+    if (a.z.vocab <= 4096) return a.z.rows <= kFewRows ? launch_sample_as<T, 8, 8 / N>(a, s) : launch_sample_as<T, 4, 16 / N>(a, s);
     if (a.z.vocab <= 1024 * 16) return launch_sample_as<T, 16, 16 / N>(a, s);
     if (a.z.vocab <= 1024 * 32) return launch_sample_as<T, 16, 32 / N>(a, s);
     return launch_sample_as<T, 16, 0>(a, s);

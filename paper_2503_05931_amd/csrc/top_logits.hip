@@ -14,9 +14,30 @@ constexpr float kLn2 = 0.69314718055994530942f;
 template <int W> struct TopLds {
     RowBounds<W> bounds;
     List list;
-    Search<W, 8, false> search;
+    Search<W, 8, uint8_t> search;
     float part[W];
     float over[kList];
+};
+// every element of the order counts 1
+template <typename T, int W> struct Counted {
+    static constexpr int N = RowVec<T>::n;
+    RowLoop<T, W> loop;
+    template <typename F> __device__ __forceinline__ void logits(F f) const {
+        loop.each_floats([&](int, int, float (&z)[N]) { f(z); });
+    }
+    template <typename F> __device__ __forceinline__ void each(F f) const {
+        loop.each_floats([&](int, int id, float (&z)[N]) {
+            uint64_t w[N];
+#pragma unroll
+            for (int e = 0; e < N; ++e) w[e] = z[e] > -kInf;
+            f(id, z, w);
+        });
+    }
+    template <typename Of, typename F> __device__ __forceinline__ void each_if(Of of, F f) const {
+        each([&](int id, const float (&z)[N], const uint64_t (&w)[N]) {
+            if (__any(of(id, z))) f(id, z, w);
+        });
+    }
 };
 template <int W> __device__ __forceinline__ float block_sum(float v, float* part) {
     v = wave_sum(v);
@@ -57,31 +78,34 @@ template <typename T, int W, int S> __global__ __launch_bounds__(64 * W) void to
     bound_row<W>(row, K, lds.bounds, list, top, bound);
     bound = gather_bound(bound);
     row.forget();
+    const RowLoop<T, W> loop{row.p, row.n};
     // Exponents relative to a border that the bound's own product, rounded, is not below.  Where a product could be infinite, the row is searched.
     const float scaled = bound * a.scale, border = scaled - fabsf(scaled) * 0x1p-22f - 0x1p-126f;
     const bool fits = fabsf(scaled) < 1e37f;
     float sum = 0.f;  // of what is below the border, relative to it; may be NaN, if one is in the row
-    gather(row, list, [&](float z) {
-        const float over = fmaf(z, a.scale, -border);
-        const float below = __builtin_amdgcn_fmed3f(over * -0x1p100f, 0.f, 1.f);
-        sum = fmaf(__builtin_amdgcn_exp2f(over), below, sum);
-        return over;
+    gather(row, list, [&](float (&z)[RowVec<T>::n]) {
+#pragma unroll
+        for (int e = 0; e < RowVec<T>::n; ++e) {
+            z[e] = fmaf(z[e], a.scale, -border);
+            const float below = __builtin_amdgcn_fmed3f(z[e] * -0x1p100f, 0.f, 1.f);
+            sum = fmaf(__builtin_amdgcn_exp2f(z[e]), below, sum);
+        }
     });
     asm volatile("" : "+v"(sum));  // it is made here, not where it is used: there the row would have to be kept
     int n = list.count;
     Place last{-kInf, INT_MAX};
     const bool searched = n > kList || !fits;
     if (searched) {  // many equal ones, mostly
-        if (top > -kInf) last = find_last<8>(row.again(), top, K, lds.search, list, [](float, int) { return true; }, [](float) { return 1; });
+        if (top > -kInf) last = find_last<T>(Counted<T, W>{loop}, top, kInf, K, lds.search, list);
         if (tid == 0) list.count = 0;
         __syncthreads();
-        row.again().each([&](float z, int id) {
+        loop.each([&](float z, int id) {
             if (z > -kInf && up_to(z, id, last)) put_in(list, id);
         });
         __syncthreads();
         n = list.count;
     }
-    read_keys(row, list, n);
+    read_keys<W>(row.p, list, n);
     __syncthreads();
     for (int i = tid; i < n; i += kThreads) {
         const uint64_t key = list.key[i];
@@ -110,10 +134,10 @@ template <typename T, int W, int S> __global__ __launch_bounds__(64 * W) void to
         } else {  // nothing, or far from the border: relative to its own largest
             last = lds.search.last;
             float m = -kInf;
-            row.again().each([&](float z, int id) { m = up_to(z, id, last) ? m : fmaxf(m, z); });
+            loop.each([&](float z, int id) { m = up_to(z, id, last) ? m : fmaxf(m, z); });
             const float base = block_max<W>(m, lds.part);
             sum = 0.f;
-            if (base > -kInf) row.again().each([&](float z, int id) { sum += z > -kInf && !up_to(z, id, last) ? __builtin_amdgcn_exp2f((z - base) * a.scale) : 0.f; });
+            if (base > -kInf) loop.each([&](float z, int id) { sum += z > -kInf && !up_to(z, id, last) ? __builtin_amdgcn_exp2f((z - base) * a.scale) : 0.f; });
             sum = block_sum<W>(sum, lds.part);
             if (base > -kInf) rest = base == kInf ? kInf : base / a.temperature + logf(sum);
         }

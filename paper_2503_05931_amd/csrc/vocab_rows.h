@@ -57,8 +57,6 @@ template <typename T, int W, int S> struct Row {
         return row_vec(p, id, n);
     }
     __device__ __forceinline__ Row(const T* p, int n) : p(p), n(n) {}
-    // the same row from memory: for what is seldom done, and would keep the registers
-    __device__ __forceinline__ Row<T, W, 0> again() const { return Row<T, W, 0>(p, n); }
     __device__ __forceinline__ Row(const LogitRows& z, int row) : p(static_cast<const T*>(z.data) + row * z.stride), n(z.vocab) {
         if constexpr (S > 0) {
 #pragma unroll
@@ -83,12 +81,22 @@ template <typename T, int W, int S> struct Row {
             for (int s = 0; s < S; ++s) f(s, vec_begin<N>(s * kStep + (int)threadIdx.x * N, n), x[s]);
         } else {
             V next = read(0);
+#pragma unroll 1
             for (int s = 0; s * kStep < n; ++s) {
                 const V v = next;
                 if ((s + 1) * kStep < n) next = read(s + 1);
                 f(s, vec_begin<N>(s * kStep + (int)threadIdx.x * N, n), v);
             }
         }
+    }
+    // f(s, first id, logits)
+    template <typename F> __device__ __forceinline__ void each_floats(F f) const {
+        each_vec([&](int s, int id, const V& v) {
+            float z[N];
+#pragma unroll
+            for (int e = 0; e < N; ++e) z[e] = to_f32((T)v[e]);
+            f(s, id, z);
+        });
     }
     // f(logit, id); an id may come again, or one behind the row's end, with minus infinity
     template <typename F> __device__ __forceinline__ void each(F f) const {
@@ -97,6 +105,17 @@ template <typename T, int W, int S> struct Row {
             for (int e = 0; e < N; ++e) f(to_f32((T)v[e]), id + e);
         });
     }
+};
+
+// A row that is read from memory anew for each pass, in a loop of short code, the next vector asked for ahead.
+template <typename T, int W> struct RowLoop {
+    static constexpr int N = RowVec<T>::n, kThreads = 64 * W;
+    const T* p;
+    int n;
+    // f(s, first id, logits)
+    template <typename F> __device__ __forceinline__ void each_floats(F f) const { Row<T, W, 0>(p, n).each_floats(f); }
+    // f(logit, id)
+    template <typename F> __device__ __forceinline__ void each(F f) const { Row<T, W, 0>(p, n).each(f); }
 };
 
 __device__ __forceinline__ float wave_max(float v) {
@@ -202,6 +221,27 @@ struct Pow2 {
         for (int i = 7; i >= 0; --i) p = fma(f, p, q[i]);
         return ldexp(fma(f, p, 1.0), (int)n);
     }
+    // of several at once, step by step: an exponential is a chain of operations that each wait for the one before.  They are all made here, and not one by
+    // one where they are used.
+    template <int N> __device__ __forceinline__ void operator()(double (&y)[N]) const {
+#pragma clang fp contract(off)
+        double n[N], p[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            y[e] = fmax(y[e], -1100.0);
+            n[e] = rint(y[e]);
+            y[e] -= n[e];
+            p[e] = q[8];
+        }
+#pragma unroll
+        for (int i = 7; i >= 0; --i)
+#pragma unroll
+            for (int e = 0; e < N; ++e) p[e] = fma(y[e], p[e], q[i]);
+#pragma unroll
+        for (int e = 0; e < N; ++e) y[e] = ldexp(fma(y[e], p[e], 1.0), (int)n[e]);
+#pragma unroll
+        for (int e = 0; e < N; ++e) asm volatile("" : "+v"(y[e]));
+    }
 };
 
 // An element's place in the order: of two, the one in front has the larger key
@@ -269,8 +309,8 @@ __device__ __forceinline__ void put_in(List& list, int id) {
     if (at < kList) list.id[at] = id;
 }
 // makes the first n listed elements' keys; a barrier has to follow
-template <typename T, int W, int S> __device__ __forceinline__ void read_keys(const Row<T, W, S>& row, List& list, int n) {
-    for (int i = threadIdx.x; i < n; i += 64 * W) list.key[i] = order_key(in_order(to_f32(row.p[list.id[i]])), list.id[i]);
+template <int W, typename T> __device__ __forceinline__ void read_keys(const T* p, List& list, int n) {
+    for (int i = threadIdx.x; i < n; i += 64 * W) list.key[i] = order_key(in_order(to_f32(p[list.id[i]])), list.id[i]);
 }
 // how many of the n keys are larger
 __device__ __forceinline__ int place_of(const List& list, uint64_t key, int n) {
@@ -280,19 +320,20 @@ __device__ __forceinline__ int place_of(const List& list, uint64_t key, int n) {
     return place;
 }
 
-// Ids of the elements of which over(logit) is not negative, in no order, perhaps of some that are NaN; over grows with the logit, and is minus infinity for minus
-// infinity.  Logits are read by these ids later.  A lane's elements are marked by over's signs, an instruction each (a comparison's result cannot be
+// Ids of the elements of which over is not negative, in no order, perhaps of some that are NaN.  over(a vector's logits) puts in the place of each a number that grows with
+// it and is minus infinity for minus infinity.  Logits are read by these ids later.  A lane's elements are marked by over's signs, an instruction each (a comparison's result cannot be
 // used at once), so places are handed out once a wavefront, and what is listed costs a few steps.
 template <typename T, int W, int S, typename F> __device__ __forceinline__ void gather(const Row<T, W, S>& row, List& list, F over) {
     constexpr int N = RowVec<T>::n;
     if constexpr (S > 0) {
         constexpr int kMarks = (S * N + 31) / 32;
         uint32_t marks[kMarks] = {};
-        row.each_vec([&](int s, int, const auto& v) {
+        row.each_floats([&](int s, int, float (&z)[N]) {
+            over(z);
 #pragma unroll
             for (int e = 0; e < N; ++e) {
                 uint32_t& m = marks[(s * N + e) / 32];
-                m = __builtin_amdgcn_alignbit(m, __builtin_bit_cast(uint32_t, over(to_f32((T)v[e]))), 31);  // the sign from the right
+                m = __builtin_amdgcn_alignbit(m, __builtin_bit_cast(uint32_t, z[e]), 31);  // the sign from the right
             }
             __builtin_amdgcn_sched_barrier(0);  // one vector after the other, or all have their registers at once
         });
@@ -320,35 +361,36 @@ template <typename T, int W, int S, typename F> __device__ __forceinline__ void 
                 ++at;
             }
     } else {
-        row.each([&](float z, int id) {
-            if (over(z) >= 0.f) put_in(list, id);
+        row.each_floats([&](int, int id, float (&z)[N]) {
+            over(z);
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if (z[e] >= 0.f) put_in(list, id + e);
         });
     }
     __syncthreads();
 }
 
 // ---- exact search for the last of the first elements of the order, whatever the row holds ----
-// Digit by digit over histograms of 2^BITS bins: first of the distance to the largest logit (its floating point bits: 16 powers of two, from 2^-10 to 2^6,
-// have as many bins each), then of the logit's own bits, then of the id's, until the bin that the border falls into has at most kList elements; those
-// are compared one by one.  Weights are whole numbers (1, where elements are counted), so the order of the atomic additions does not matter.
-template <int W, int BITS, bool HAS_W> struct Search {
+// Digit by digit over histograms of 2^BITS bins: first of the distance to the largest logit in equal steps, then of the logit's own bits, then of the id's,
+// until the bin that the border falls into has at most kList elements; those are compared one by one.  Weights are whole numbers (1, where elements are
+// counted), so the order of the atomic additions does not matter.  What costs is additions of a wavefront to the same bin, some 50 cycles each: hence equal
+// steps, as many as there is room for, and one addition where all lanes' logits are the same.
+template <int W, int BITS, typename Weight = uint64_t> struct Search {
     uint64_t sum[1 << BITS];
     uint64_t part[W], before;
-    uint64_t w[HAS_W ? kList : 1];
+    Weight w[kList];
+    float low[W];
     int bin;
     Place last;
 };
-template <int BITS> __device__ __forceinline__ int distance_bin(float z, float top) {
-    const uint32_t u = __builtin_bit_cast(uint32_t, z == top ? 0.f : top - z) >> (27 - BITS);
-    constexpr int first = (127 - 10) << (BITS - 4);
-    return min(max((int)u - first, 0), (1 << BITS) - 1);
-}
 
-// target: for counts, how many elements the first part has; for weights, the least sum that the part up to its last element reaches; 1 or more, and
-// what is more than there is counts as all.  in(z, id): elements that take part, one at least (with a weight above 0); weight(z): what each counts.
-template <int BITS, typename R, int W, bool HAS_W, typename In, typename Weight>
-__device__ __forceinline__ Place find_last(const R& row, float top, uint64_t target, Search<W, BITS, HAS_W>& h, List& list, In in, Weight weight) {
-    constexpr int kThreads = 64 * W, kBins = 1 << BITS, kEach = kBins < kThreads ? 1 : kBins / kThreads, kIdBits = 18;
+// source.each(f): f(first id, logits, weights) for every vector of the row; what weighs 0 takes no part (minus infinity and NaN among it, and something has to
+// take part); source.each_if(of, f): only where of(first id, logits) is true for a lane; source.logits(f): f(logits).  target: the least sum of weights that the part up to its last element reaches, 1 or more; what is more than there is
+// counts as all.  span: what is further than that from the largest weighs 0, or nothing is known about it (infinity).
+template <typename T, int BITS, int W, typename Weight, typename Source>
+__device__ __forceinline__ Place find_last(const Source& source, float top, float span, uint64_t target, Search<W, BITS, Weight>& h, List& list) {
+    constexpr int N = RowVec<T>::n, kThreads = 64 * W, kBins = 1 << BITS, kEach = kBins < kThreads ? 1 : kBins / kThreads, kIdBits = 18;
     static_assert(kMostVocab <= 1 << kIdBits, "an id's digits");
     constexpr int kZLevels = (32 + BITS - 1) / BITS, kLevels = 1 + kZLevels + (kIdBits + BITS - 1) / BITS;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -356,21 +398,58 @@ __device__ __forceinline__ Place find_last(const R& row, float top, uint64_t tar
     uint32_t bits = 0, id_bits = 0;      // digits found so far
     int known = 32, id_known = kIdBits;  // and how many bits are below them
     uint64_t passed = 0;                 // in front of the bin
+    float rate;
+    {
+        float low = kInf;  // of those in the order
+        source.logits([&](const float (&z)[N]) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) low = fminf(low, z[e] > -kInf ? z[e] : kInf);
+        });
+        low = wave_min(low);
+        if (lane == 0) h.low[wave] = low;
+        for (int i = tid; i < kBins; i += kThreads) h.sum[i] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < W; ++i) low = fminf(low, h.low[i]);
+        rate = (float)kBins / fminf(fmaxf(top - low, 0x1p-100f), span);
+    }
+    auto bin_of = [&](float z) { return (int)fminf((top - z) * rate, (float)(kBins - 1)); };
+    auto in_bin = [&](float z, int id) {
+        return bin_of(z) == bin0 && (uint64_t)(~rising_bits(z) ^ bits) >> known == 0 && ((uint32_t)id ^ id_bits) >> id_known == 0;
+    };
     for (int level = 0;; ++level) {
         const bool by_z = level <= kZLevels;
         const int have = by_z ? known : id_known, take = min(BITS, have), shift = have - take;
-        for (int i = tid; i < kBins; i += kThreads) h.sum[i] = 0;
-        __syncthreads();
         if (level == 0) {
-            row.each([&](float z, int id) {
-                if (z > -kInf && in(z, id)) atomicAdd((unsigned long long*)&h.sum[distance_bin<BITS>(z, top)], (unsigned long long)weight(z));
+            source.each([&](int, const float (&z)[N], const uint64_t (&w)[N]) {
+                const float one = bits_f32(__builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, z[0])));
+                bool alike = true;  // the whole wavefront's logits are one
+#pragma unroll
+                for (int e = 0; e < N; ++e) alike = alike && w[e] != 0 && z[e] == one;
+                if (__all(alike)) {
+                    if (lane == 0) atomicAdd((unsigned long long*)&h.sum[bin_of(one)], (unsigned long long)(w[0] * (64 * N)));
+                    return;
+                }
+#pragma unroll
+                for (int e = 0; e < N; ++e)
+                    if (w[e] != 0) atomicAdd((unsigned long long*)&h.sum[bin_of(z[e])], (unsigned long long)w[e]);
             });
         } else {
-            row.each([&](float z, int id) {
-                if (!(z > -kInf) || distance_bin<BITS>(z, top) != bin0 || !in(z, id)) return;
-                const uint32_t falling = ~rising_bits(z);
-                if ((uint64_t)(falling ^ bits) >> known != 0 || ((uint32_t)id ^ id_bits) >> id_known != 0) return;
-                atomicAdd((unsigned long long*)&h.sum[((by_z ? falling : (uint32_t)id) >> shift) & ((1u << take) - 1)], (unsigned long long)weight(z));
+            source.each([&](int first, const float (&z)[N], const uint64_t (&w)[N]) {
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const int id = first + e;
+                    const bool counts = w[e] != 0 && in_bin(z[e], id);
+                    const int digit = ((by_z ? ~rising_bits(z[e]) : (uint32_t)id) >> shift) & ((1u << take) - 1);
+                    const uint64_t lanes = __ballot(counts);
+                    if (lanes == 0) continue;
+                    const int one = __builtin_ctzll(lanes);
+                    if (by_z && __ballot(counts && z[e] == bits_f32(lane_of(__builtin_bit_cast(uint32_t, z[e]), one))) == lanes) {
+                        if (lane == one) atomicAdd((unsigned long long*)&h.sum[digit], (unsigned long long)(w[e] * __builtin_popcountll(lanes)));
+                    } else if (counts) {
+                        atomicAdd((unsigned long long*)&h.sum[digit], (unsigned long long)w[e]);
+                    }
+                }
             });
         }
         __syncthreads();
@@ -408,30 +487,35 @@ __device__ __forceinline__ Place find_last(const R& row, float top, uint64_t tar
             id_bits |= (uint32_t)h.bin << shift;
             id_known = shift;
         }
-        row.each([&](float z, int id) {
-            if (!(z > -kInf) || distance_bin<BITS>(z, top) != bin0 || !in(z, id)) return;
-            if ((uint64_t)(~rising_bits(z) ^ bits) >> known == 0 && ((uint32_t)id ^ id_bits) >> id_known == 0) put_in(list, id);
-        });
+        source.each_if(
+            [&](int first, const float (&z)[N]) {
+                bool any = false;
+#pragma unroll
+                for (int e = 0; e < N; ++e) any |= in_bin(z[e], first + e);
+                return any;
+            },
+            [&](int first, const float (&z)[N], const uint64_t (&w)[N]) {
+#pragma unroll
+                for (int e = 0; e < N; ++e)
+                    if (w[e] != 0 && in_bin(z[e], first + e)) {
+                        const uint32_t to = atomicAdd(&list.count, 1u);
+                        if (to < kList) {
+                            list.key[to] = order_key(z[e], first + e);
+                            h.w[to] = (Weight)w[e];
+                        }
+                    }
+            });
         __syncthreads();
         if (list.count <= kList || level + 1 == kLevels) break;
-        __syncthreads();  // all have read the count
+        for (int i = tid; i < kBins; i += kThreads) h.sum[i] = 0;
+        __syncthreads();  // and all have read the count
     }
     const int n = min((int)list.count, kList);
-    read_keys(row, list, n);
-    if constexpr (HAS_W) {
-        for (int i = tid; i < n; i += kThreads) h.w[i] = weight(in_order(to_f32(row.p[list.id[i]])));
-    }
-    __syncthreads();
     for (int i = tid; i < n; i += kThreads) {
-        const uint64_t key = list.key[i];
-        uint64_t at = passed, own = 1;
-        if constexpr (HAS_W) {
-            own = h.w[i];
+        const uint64_t key = list.key[i], own = h.w[i];
+        uint64_t at = passed;
 #pragma unroll 8
-            for (int j = 0; j < n; ++j) at += list.key[j] > key ? h.w[j] : 0;
-        } else {
-            at += place_of(list, key, n);
-        }
+        for (int j = 0; j < n; ++j) at += list.key[j] > key ? (uint64_t)h.w[j] : 0;
         if (at < target && target <= at + own) h.last = Place{key_logit(key), key_id(key)};
     }
     __syncthreads();
