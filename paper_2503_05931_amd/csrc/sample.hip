@@ -102,12 +102,13 @@ template <int W> __device__ __forceinline__ uint64_t block_sum64(uint64_t v, uin
     return v;
 }
 
-// A row and what its elements weigh: held in registers, where these suffice, else made anew for each pass from the row in memory by weights(first id, logits,
-// weights)
+// What find_last goes through: the elements up to `among`, that count 1 each or their weights.  Held: their weights (or 1, or 0) are in registers.
 template <typename T, int W, int S> struct Held {
     static constexpr int N = RowVec<T>::n;
     const Row<T, W, S>& row;
-    uint64_t (&w)[S][N];
+    const uint64_t (&w)[S][N];
+    const Weigh& weigh;
+    bool by_weight;
     template <typename F> __device__ __forceinline__ void logits(F f) const {
         row.each_floats([&](int, int, float (&z)[N]) {
             anew(z);
@@ -126,39 +127,43 @@ template <typename T, int W, int S> struct Held {
             f(id, z, v);
         });
     }
-    template <typename Of, typename F> __device__ __forceinline__ void each_if(Of of, F f) const {
-        each([&](int id, const float (&z)[N], const uint64_t (&v)[N]) {
-            if (__any(of(id, z))) f(id, z, v);
+    template <typename F> __device__ __forceinline__ void members(F f) const {
+        row.each_floats([&](int s, int id, float (&z)[N]) {
+            anew(z);
+            f(id, z, [&](int e) { return w[s][e] != 0; });
         });
     }
+    __device__ __forceinline__ uint64_t weight(float z) const { return by_weight ? weigh.whole(weigh.exact(z)) : 1; }
     // or what a pass makes of the logits is kept for the next one, and there are no registers for it
     static __device__ __forceinline__ void anew(float (&z)[N]) {
 #pragma unroll
         for (int e = 0; e < N; ++e) asm volatile("" : "+v"(z[e]));
     }
 };
-template <typename T, int W, typename Weights> struct Made {
+// Made: weights are made anew in each pass, from the row in memory.
+template <typename T, int W> struct Made {
     static constexpr int N = RowVec<T>::n;
     RowLoop<T, W> loop;
-    Weights weights;
+    const Weigh& weigh;
+    Place among;
+    bool by_weight;
     template <typename F> __device__ __forceinline__ void logits(F f) const {
         loop.each_floats([&](int, int, float (&z)[N]) { f(z); });
     }
     template <typename F> __device__ __forceinline__ void each(F f) const {
         loop.each_floats([&](int, int id, float (&z)[N]) {
             uint64_t w[N];
-            weights(id, z, w);
+            if (by_weight) weigh.wholes(z, w);
+#pragma unroll
+            for (int e = 0; e < N; ++e) w[e] = takes_part(z[e], id + e) ? by_weight ? w[e] : 1 : 0;
             f(id, z, w);
         });
     }
-    template <typename Of, typename F> __device__ __forceinline__ void each_if(Of of, F f) const {
-        loop.each_floats([&](int, int id, float (&z)[N]) {
-            if (!__any(of(id, z))) return;
-            uint64_t w[N];
-            weights(id, z, w);
-            f(id, z, w);
-        });
+    template <typename F> __device__ __forceinline__ void members(F f) const {
+        loop.each_floats([&](int, int id, float (&z)[N]) { f(id, z, [&](int e) { return takes_part(z[e], id + e); }); });
     }
+    __device__ __forceinline__ uint64_t weight(float z) const { return by_weight ? weigh.whole(weigh.exact(z)) : 1; }
+    __device__ __forceinline__ bool takes_part(float z, int id) const { return z > -kInf && up_to(z, id, among); }
 };
 
 }  // namespace
@@ -301,16 +306,10 @@ template <typename T, int W, int S, int RUNS> __global__ __launch_bounds__(64 * 
         }
         // the last of A by number, then that of B by weight
         __syncthreads();
-        const Place everything{-kInf, INT_MAX};
         auto search = [&](const Place& among, bool by_weight, uint64_t target) {
             const float span = by_weight ? t * 45.f : kInf;  // a weight of e^-45 is nothing in units of 2^-50
-            if constexpr (kHeld) return find_last<T>(Held<T, W, S>{row, held}, top, span, target, lds.search, list);
-            auto weights = [&](int id, const float (&z)[N], uint64_t (&w)[N]) {
-                if (by_weight) weigh.wholes(z, w);
-#pragma unroll
-                for (int e = 0; e < N; ++e) w[e] = z[e] > -kInf && up_to(z[e], id + e, among) ? by_weight ? w[e] : 1 : 0;
-            };
-            return find_last<T>(Made<T, W, decltype(weights)>{loop, weights}, top, span, target, lds.search, list);
+            if constexpr (kHeld) return find_last<T>(Held<T, W, S>{row, held, weigh, by_weight}, top, span, target, lds.search, list);
+            else return find_last<T>(Made<T, W>{loop, weigh, among, by_weight}, top, span, target, lds.search, list);
         };
         for (int step = 0; step < 2; ++step) {
             const bool by_weight = step == 1;

@@ -33,11 +33,10 @@ template <typename T, int W> struct Counted {
             f(id, z, w);
         });
     }
-    template <typename Of, typename F> __device__ __forceinline__ void each_if(Of of, F f) const {
-        each([&](int id, const float (&z)[N], const uint64_t (&w)[N]) {
-            if (__any(of(id, z))) f(id, z, w);
-        });
+    template <typename F> __device__ __forceinline__ void members(F f) const {
+        loop.each_floats([&](int, int id, float (&z)[N]) { f(id, z, [&](int e) { return z[e] > -kInf; }); });
     }
+    __device__ __forceinline__ uint64_t weight(float) const { return 1; }
 };
 template <int W> __device__ __forceinline__ float block_sum(float v, float* part) {
     v = wave_sum(v);

@@ -386,7 +386,8 @@ template <int W, int BITS, typename Weight = uint64_t> struct Search {
 };
 
 // source.each(f): f(first id, logits, weights) for every vector of the row; what weighs 0 takes no part (minus infinity and NaN among it, and something has to
-// take part); source.each_if(of, f): only where of(first id, logits) is true for a lane; source.logits(f): f(logits).  target: the least sum of weights that the part up to its last element reaches, 1 or more; what is more than there is
+// take part); source.members(f): f(first id, logits, which): which(e) tells whether element e takes part; source.weight(logit): of one that does;
+// source.logits(f): f(logits).  target: the least sum of weights that the part up to its last element reaches, 1 or more; what is more than there is
 // counts as all.  span: what is further than that from the largest weighs 0, or nothing is known about it (infinity).
 template <typename T, int BITS, int W, typename Weight, typename Source>
 __device__ __forceinline__ Place find_last(const Source& source, float top, float span, uint64_t target, Search<W, BITS, Weight>& h, List& list) {
@@ -415,6 +416,7 @@ __device__ __forceinline__ Place find_last(const Source& source, float top, floa
     }
     auto bin_of = [&](float z) { return (int)fminf((top - z) * rate, (float)(kBins - 1)); };
     auto in_bin = [&](float z, int id) {
+        if (known == 32) return bin_of(z) == bin0;
         return bin_of(z) == bin0 && (uint64_t)(~rising_bits(z) ^ bits) >> known == 0 && ((uint32_t)id ^ id_bits) >> id_known == 0;
     };
     for (int level = 0;; ++level) {
@@ -423,9 +425,11 @@ __device__ __forceinline__ Place find_last(const Source& source, float top, floa
         if (level == 0) {
             source.each([&](int, const float (&z)[N], const uint64_t (&w)[N]) {
                 const float one = bits_f32(__builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, z[0])));
-                bool alike = true;  // the whole wavefront's logits are one
+                bool alike = z[0] == one;  // the whole wavefront's logits are one
+                if (__all(alike)) {
 #pragma unroll
-                for (int e = 0; e < N; ++e) alike = alike && w[e] != 0 && z[e] == one;
+                    for (int e = 0; e < N; ++e) alike = alike && w[e] != 0 && z[e] == one;
+                }
                 if (__all(alike)) {
                     if (lane == 0) atomicAdd((unsigned long long*)&h.sum[bin_of(one)], (unsigned long long)(w[0] * (64 * N)));
                     return;
@@ -487,30 +491,29 @@ __device__ __forceinline__ Place find_last(const Source& source, float top, floa
             id_bits |= (uint32_t)h.bin << shift;
             id_known = shift;
         }
-        source.each_if(
-            [&](int first, const float (&z)[N]) {
-                bool any = false;
+        source.members([&](int first, const float (&z)[N], auto takes_part) {
+            bool here[N], any = false;
 #pragma unroll
-                for (int e = 0; e < N; ++e) any |= in_bin(z[e], first + e);
-                return any;
-            },
-            [&](int first, const float (&z)[N], const uint64_t (&w)[N]) {
+            for (int e = 0; e < N; ++e) {
+                here[e] = in_bin(z[e], first + e);
+                any |= here[e];
+            }
+            if (!__any(any)) return;
 #pragma unroll
-                for (int e = 0; e < N; ++e)
-                    if (w[e] != 0 && in_bin(z[e], first + e)) {
-                        const uint32_t to = atomicAdd(&list.count, 1u);
-                        if (to < kList) {
-                            list.key[to] = order_key(z[e], first + e);
-                            h.w[to] = (Weight)w[e];
-                        }
-                    }
-            });
+            for (int e = 0; e < N; ++e)
+                if (here[e] && takes_part(e)) {
+                    const uint32_t to = atomicAdd(&list.count, 1u);
+                    if (to < kList) list.key[to] = order_key(z[e], first + e);
+                }
+        });
         __syncthreads();
         if (list.count <= kList || level + 1 == kLevels) break;
         for (int i = tid; i < kBins; i += kThreads) h.sum[i] = 0;
         __syncthreads();  // and all have read the count
     }
     const int n = min((int)list.count, kList);
+    for (int i = tid; i < n; i += kThreads) h.w[i] = (Weight)source.weight(key_logit(list.key[i]));
+    __syncthreads();
     for (int i = tid; i < n; i += kThreads) {
         const uint64_t key = list.key[i], own = h.w[i];
         uint64_t at = passed;
