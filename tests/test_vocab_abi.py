@@ -200,6 +200,7 @@ def plan_of(kind, cfg, monkeypatch, status=0, device=-1, stream=7):
     p.handle, p._destroy = C.c_void_p(1), lambda _: 0
     p.stream, p.raw, p.index = Stream(rec, 5), 5, -1
     p._f32, p._i32, p._how = torch.empty(0), torch.empty(0, dtype=torch.int32), sampling()
+    p._given_how = None
     p._raw_stream = lambda index: rec.stream
     p._get_device, p._only = lambda: rec.device, False
     monkeypatch.setattr(T, "_lib", lambda: types.SimpleNamespace(aed_train_last_error=lambda: b"a launch failed"))
