@@ -1,6 +1,7 @@
 // Host side of include/aed_vocab.h: argument checks and launches of the operators on rows of logits.
 #include "../../include/aed_vocab.h"
 
+#include <algorithm>
 #include <cmath>
 
 #include "host_calls.h"
@@ -74,6 +75,8 @@ void set_temperature(const aed_distill_config& c, aed::DistillArgs& a) {
     a.temperature = c.temperature;
     a.scale_d = kLog2e / t;
     a.scale = (float)a.scale_d;
+    if ((double)a.scale >= a.scale_d) a.scale = std::nextafter(a.scale, 0.f);
+    a.scale_low = std::max((float)(a.scale_d - (double)a.scale), 1e-37f);
     a.factor = t * t / kLog2e;
 }
 

@@ -17,12 +17,9 @@ namespace {
 
 // Largest logit and the sum of 2^((z - top) scale)
 struct Partial {
-    float top, sum;
+    float top;
+    double sum;
 };
-__device__ __forceinline__ Partial joined(Partial a, Partial b, float scale) {
-    const float top = fmaxf(a.top, b.top), to = top == -kInf ? 0.f : top;
-    return Partial{top, a.sum * __builtin_amdgcn_exp2f((a.top - to) * scale) + b.sum * __builtin_amdgcn_exp2f((b.top - to) * scale)};
-}
 
 // 2^y, minus infinity and NaN as they are
 __device__ __forceinline__ double exactly(const Pow2& pow2, double y) { return y != y ? y : pow2(y); }
@@ -93,11 +90,16 @@ template <typename T, int W, int S, int E, bool OTHERS> __global__ __launch_boun
         if (OTHERS) __syncthreads();
     }
 
-    // the row: all of it, or what is not in the list
-    const float scale = a.scale;
-    Partial mine{-kInf, 0.f};
+    // The row: all of it, or what is not in the list.  A divergence is a small difference of logarithms, so its sum has to be better than its terms: the
+    // scale has two parts (the second above 0, so that minus infinity stays), and where lanes come together there are 64 bits.  One part alone made rows' losses
+    // at T = 4 wrong by 3e-5 of themselves.
+    const Pow2 pow2;
+    const double c = a.scale_d;
+    const float scale = a.scale, scale_low = a.scale_low;
+    float lane_top = -kInf, lane_sum = 0.f;  // the sum is relative to 2^lane_base
+    double lane_base = -(double)kInf;
     for (int step = 0; step < steps; ++step) {
-        float y[S][N], top = mine.top;
+        float y[S][N], top = lane_top;
 #pragma unroll
         for (int i = 0; i < S; ++i) {
             uint32_t bits = 0;
@@ -117,35 +119,41 @@ template <typename T, int W, int S, int E, bool OTHERS> __global__ __launch_boun
         }
         if (step + 1 < steps) read(step + 1);
         const float to = top == -kInf ? 0.f : top, product = to * scale;
+        const bool wide = __any(fabsf(product) > 0x1p24f);  // the product's own rounding may be some powers of two
+        const double base = wide ? (double)to * c : (double)product;
         float sum = 0.f;
-        if (!__any(fabsf(product) > 1e37f)) {  // one operation an exponent; what the product is rounded by is the same for all of them
+        if (!wide) {
 #pragma unroll
             for (int i = 0; i < S; ++i)
 #pragma unroll
-                for (int e = 0; e < N; ++e) sum += __builtin_amdgcn_exp2f(fmaf(y[i][e], scale, -product));
-            sum *= __builtin_amdgcn_exp2f(-fmaf(to, scale, -product));
+                for (int e = 0; e < N; ++e) sum += __builtin_amdgcn_exp2f(fmaf(y[i][e], scale_low, fmaf(y[i][e], scale, -product)));
         } else {
 #pragma unroll
             for (int i = 0; i < S; ++i)
 #pragma unroll
-                for (int e = 0; e < N; ++e) sum += __builtin_amdgcn_exp2f((y[i][e] - to) * scale);
+                for (int e = 0; e < N; ++e) sum += __builtin_amdgcn_exp2f(fmaf(y[i][e] - to, scale_low, (y[i][e] - to) * scale));
         }
-        mine = Partial{top, fmaf(mine.sum, __builtin_amdgcn_exp2f((mine.top - to) * scale), sum)};
+        lane_sum = fmaf(lane_sum, __builtin_amdgcn_exp2f((float)(lane_base - base)), sum);
+        lane_top = top;
+        lane_base = top == -kInf ? -(double)kInf : base;
     }
-    {
-        const float top = wave_max(mine.top), to = top == -kInf ? 0.f : top;
-        mine = Partial{top, wave_sum(mine.sum * __builtin_amdgcn_exp2f((mine.top - to) * scale))};
-    }
+    Partial mine;
+    mine.top = wave_max(lane_top);
+    mine.sum = wave_sum((double)lane_sum * pow2(lane_base - (mine.top == -kInf ? 0.0 : (double)mine.top * c)));
     if constexpr (W > 1) {
         if (lane == 0) parts[wave] = mine;
         __syncthreads();
         if (wave != 0) return;
-        for (int i = 1; i < W; ++i) mine = joined(mine, parts[i], scale);
+        for (int i = 1; i < W; ++i) {
+            const Partial other = parts[i];
+            const float top = fmaxf(mine.top, other.top);
+            const double to = top == -kInf ? 0.0 : (double)top;
+            mine.sum = mine.sum * pow2(((double)mine.top - to) * c) + other.sum * pow2(((double)other.top - to) * c);
+            mine.top = top;
+        }
     }
 
     // the list against the row, by one wavefront, in 64 bits; logarithms to base 2
-    const Pow2 pow2;
-    const double c = a.scale_d;
     const double rest = OTHERS ? (double)a.rest[r] * kLog2eD : -(double)kInf;
     float value_top = -kInf, at_top = -kInf;
 #pragma unroll
@@ -182,7 +190,7 @@ template <typename T, int W, int S, int E, bool OTHERS> __global__ __launch_boun
     n = wave_sum(n);
     // lane 0: the rest's part of n, others: what the row's sum is relative to the student's largest
     const double uniform = exactly(pow2, lane == 0 ? rest - lead : row_top);
-    const double q_others = OTHERS ? lane_of(uniform, 0) : 0.0, shift = lane_of(uniform, 1), others = (double)mine.sum * shift;
+    const double q_others = OTHERS ? lane_of(uniform, 0) : 0.0, shift = lane_of(uniform, 1), others = mine.sum * shift;
     n += q_others;
     if (__any(twice)) {  // entries of one id share what they have; the first of them counts for p
         for (int i = 0; i < E; ++i) same[i] = 0;
@@ -211,7 +219,7 @@ template <typename T, int W, int S, int E, bool OTHERS> __global__ __launch_boun
     }
     total = OTHERS ? wave_sum(total) + others : others;
     // lane 0: of n, 1: of the student's sum, 2: of what the row gave
-    const double of = lane == 0 ? n : lane == 1 ? total : (double)mine.sum;
+    const double of = lane == 0 ? n : lane == 1 ? total : mine.sum;
     const double inverse = of > 0 ? 1 / of : of == 0 ? 0 : of, log_of = of == 0 ? 0.0 : log2_of(pow2, of);  // NaN stays; without any logit every p is 0
     const double n_inverse = lane_of(inverse, 0), total_inverse = lane_of(inverse, 1), log_n = lane_of(log_of, 0), log_total = lane_of(log_of, 1);
     double row = 0;
@@ -293,7 +301,7 @@ template <typename T, int W, int S, bool STREAM> __global__ __launch_bounds__(64
         for (int v = tid; v < vecs; v += kThreads) put(v, (V)(from_f32<T>(0.f)));
         return;
     }
-    const float scale = a.scale, slope = w * a.temperature * (a.d_loss ? a.d_loss[0] : 1.f);
+    const float scale = (float)a.scale_d, slope = w * a.temperature * (a.d_loss ? a.d_loss[0] : 1.f);
     const float s0 = stats[0], s1 = slope * stats[1];
     for (int v0 = tid; v0 < vecs; v0 += kThreads * S) {
         V x[S];

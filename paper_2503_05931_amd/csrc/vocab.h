@@ -49,8 +49,8 @@ struct DistillArgs {
     void* d_logits;
     int64_t d_stride;
     int top;
-    float temperature, scale;  // scale: log2 e / temperature
-    double scale_d, factor;    // factor: temperature^2 ln 2
+    float temperature, scale, scale_low;  // scale_d's float below, and what it lacks, above 0
+    double scale_d, factor;               // log2 e / temperature; temperature^2 ln 2
 };
 
 hipError_t launch_sample(const SampleArgs& a, bool bf16, hipStream_t s);

@@ -152,6 +152,38 @@ def test_sure_students(t):
     check(c, "fp32", t=t)
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("vocab,t", [(700, 3.0), (4096, 5.5), (33001, 7.0), (33001, 3.3)])
+def test_small_divergences(vocab, t, dtype):
+    """At a high temperature a row's loss is T^2 times a small difference of logarithms.  What all terms of a sum may have in common is the exponential's own
+    error, one step of float32, 2^-23, and as much for the additions of a thread; an exponent's roundings have either sign and average out.  So 2.5e-7 T^2, ten
+    times less than what is allowed elsewhere; an inverse temperature that were a float alone would add 2^-24 of the mean exponent, some 1e-6 T^2."""
+    from paper_2503_05931_amd import vocabulary as L
+    g = torch.Generator().manual_seed(vocab)
+    c = make(40, vocab, 32, dtype, t=t, seed=vocab, unscored=0)
+    c["z"] = (3 * (c["z"].float() - 8)).to(TYPE[dtype])
+    c["values"], c["ids"], c["rest"] = (torch.tensor(x) for x in zip(*(R.top_logits(row.numpy(), 32, t) for row in
+                                        c["z"].float() + 0.02 * torch.randn(c["z"].shape, generator=g))))
+    c["values"], c["ids"], c["rest"] = c["values"].float(), c["ids"].int(), c["rest"].float()
+    for name in ("others", "list alone"):
+        rest = c["rest"] if name == "others" else None
+        _, got, _ = L.Distillation(vocab, 32, TYPE[dtype], temperature=t).aed_distill_forward(
+            c["z"].cuda(), c["values"].cuda(), c["ids"].cuda(), rest=None if rest is None else rest.cuda(), weights=None)
+        want = R.distill(c["z"].double(), c["values"], c["ids"], rest, None, float(torch.tensor(t)))[1]
+        assert (got.double().cpu() - want).abs().max() <= 2.5e-7 * t * t + 2 ** -22 * float(want.abs().max()), name
+
+
+@pytest.mark.parametrize("fill", [-3e4, -1e9, -7e19, -3e37])
+def test_others_at_one_low_value(fill):
+    """Masks of many sizes: what is outside of the list is all alike, and its mass that of so many ids at the value."""
+    c = make(4, 300, 6, "fp32", seed=9, unscored=0)
+    keep = torch.gather(c["z"], 1, c["ids"].long())
+    c["z"][:] = fill
+    check(c, "fp32")
+    c["z"].scatter_(1, c["ids"].long(), keep)
+    check(c, "fp32")
+
+
 def test_temperatures_and_large_logits():
     for t in (0.01, 50.0, 1000.0):
         check(make(4, 500, 10, "fp32", t=t, seed=7, unscored=0), "fp32", t=t)

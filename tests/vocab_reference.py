@@ -91,7 +91,8 @@ def distill_row(z, values, ids, rest, t):
     if top == -math.inf:
         log_p = torch.full_like(z, -math.inf)
     else:
-        log_p = z / t - torch.logsumexp(z / t, 0)
+        z = (z - top.detach()) / t  # first of all: logits of 1e20 have no place for a sum's log, not in 64 bits either
+        log_p = z - torch.logsumexp(z, 0)
     total = torch.zeros((), dtype=torch.float64)
     for i, v in entries:
         log_q = v / t - log_n
@@ -133,7 +134,8 @@ def distill_gradient(z, values, ids, rest, weights, t):
         if lead == -math.inf:
             continue
         log_n = lead + math.log(math.fsum(math.exp(x - lead) for x in logs))
-        x = z[r].double() / t
+        x = z[r].double()
+        x = (x - (0 if x.max() == -math.inf else x.max())) / t
         log_p = torch.full_like(x, -math.inf) if x.max() == -math.inf else x - torch.logsumexp(x, 0)
         out = torch.ones(vocab, dtype=torch.bool)
         out[[i for i, _ in entries]] = False
