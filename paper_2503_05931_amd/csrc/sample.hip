@@ -31,6 +31,7 @@ template <int W, int RUNS> struct SampleLds {
     uint64_t key[kList];  // by place
     int by_place[kList], by_id[kList];
     uint64_t run[RUNS];
+    float2 estimate[W];
 };
 
 // Weights of a row's logits
@@ -91,15 +92,34 @@ template <bool UP> __device__ __forceinline__ uint64_t part_of(float f, uint64_t
     return whole + (UP && left != 0);
 }
 
-template <int W> __device__ __forceinline__ uint64_t block_sum64(uint64_t v, uint64_t* part) {
-    v = wave_sum64(v);
+// the workgroup's sums of two; part: 2 W
+template <int W> __device__ __forceinline__ void block_sum64(uint64_t& a, uint64_t& b, uint64_t* part) {
+    a = wave_sum64(a);
+    b = wave_sum64(b);
+    if ((threadIdx.x & 63) == 0) {
+        part[threadIdx.x >> 6] = a;
+        part[W + (threadIdx.x >> 6)] = b;
+    }
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = part[0];
+    a = part[0];
+    b = part[W];
 #pragma unroll
-    for (int i = 1; i < W; ++i) v += part[i];
-    return v;
+    for (int i = 1; i < W; ++i) {
+        a += part[i];
+        b += part[W + i];
+    }
+}
+template <int W> __device__ __forceinline__ void block_sum32(float& a, float& b, float2* part) {
+    a = (float)wave_sum((double)a);
+    b = (float)wave_sum((double)b);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = make_float2(a, b);
+    __syncthreads();
+    a = b = 0;
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        a += part[i].x;
+        b += part[i].y;
+    }
 }
 
 // What find_last goes through: the elements up to `among`, that count 1 each or their weights.  Held: their weights (or 1, or 0) are in registers.
@@ -108,11 +128,12 @@ template <typename T, int W, int S> struct Held {
     const Row<T, W, S>& row;
     const uint64_t (&w)[S][N];
     const Weigh& weigh;
+    Place among;
     bool by_weight;
     template <typename F> __device__ __forceinline__ void logits(F f) const {
-        row.each_floats([&](int, int, float (&z)[N]) {
+        row.each_floats([&](int, int id, float (&z)[N]) {
             anew(z);
-            f(z);
+            f(id, z);
         });
     }
     template <typename F> __device__ __forceinline__ void each(F f) const {
@@ -127,13 +148,10 @@ template <typename T, int W, int S> struct Held {
             f(id, z, v);
         });
     }
-    template <typename F> __device__ __forceinline__ void members(F f) const {
-        row.each_floats([&](int s, int id, float (&z)[N]) {
-            anew(z);
-            f(id, z, [&](int e) { return w[s][e] != 0; });
-        });
+    __device__ __forceinline__ float logit(int id) const { return to_f32(row.p[id]); }
+    __device__ __forceinline__ uint64_t weight(float z, int id) const {
+        return z > -kInf && up_to(z, id, among) ? by_weight ? weigh.whole(weigh.exact(z)) : 1 : 0;
     }
-    __device__ __forceinline__ uint64_t weight(float z) const { return by_weight ? weigh.whole(weigh.exact(z)) : 1; }
     // or what a pass makes of the logits is kept for the next one, and there are no registers for it
     static __device__ __forceinline__ void anew(float (&z)[N]) {
 #pragma unroll
@@ -148,7 +166,7 @@ template <typename T, int W> struct Made {
     Place among;
     bool by_weight;
     template <typename F> __device__ __forceinline__ void logits(F f) const {
-        loop.each_floats([&](int, int, float (&z)[N]) { f(z); });
+        loop.each_floats([&](int, int id, float (&z)[N]) { f(id, z); });
     }
     template <typename F> __device__ __forceinline__ void each(F f) const {
         loop.each_floats([&](int, int id, float (&z)[N]) {
@@ -159,10 +177,8 @@ template <typename T, int W> struct Made {
             f(id, z, w);
         });
     }
-    template <typename F> __device__ __forceinline__ void members(F f) const {
-        loop.each_floats([&](int, int id, float (&z)[N]) { f(id, z, [&](int e) { return takes_part(z[e], id + e); }); });
-    }
-    __device__ __forceinline__ uint64_t weight(float z) const { return by_weight ? weigh.whole(weigh.exact(z)) : 1; }
+    __device__ __forceinline__ float logit(int id) const { return to_f32(loop.p[id]); }
+    __device__ __forceinline__ uint64_t weight(float z, int id) const { return takes_part(z, id) ? by_weight ? weigh.whole(weigh.exact(z)) : 1 : 0; }
     __device__ __forceinline__ bool takes_part(float z, int id) const { return z > -kInf && up_to(z, id, among); }
 };
 
@@ -217,7 +233,8 @@ template <typename T, int W, int S, int RUNS> __global__ __launch_bounds__(64 * 
         const bool complete = least_bound >= bound && weigh.whole(weigh.exact(least_bound)) < least_w;  // nothing below min-p's end is in C
         bound = gather_bound(fmaxf(bound, least_bound));
         bool few = complete || (by_k ? k <= kMostListed : by_p);
-        if (by_p && !by_k) {
+        // the whole row's sum, and whether all of B is at or above the bound
+        auto whole_row = [&] {
             uint64_t mine = 0, above = 0;
             row.each_floats([&](int s, int, float (&z)[N]) {
                 uint64_t w[N];
@@ -230,34 +247,71 @@ template <typename T, int W, int S, int RUNS> __global__ __launch_bounds__(64 * 
                 }
                 __builtin_amdgcn_sched_barrier(0);
             });
-            all = block_sum64<W>(mine, lds.run);
-            few = complete || block_sum64<W>(above, lds.run + W) >= part_of<true>(top_p, all);  // all of B is listed
+            block_sum64<W>(mine, above, lds.run);
+            all = mine;
+            const bool within = above >= part_of<true>(top_p, all);
             row.forget();
+            return within;
+        };
+        const bool of_row = by_p && !by_k;
+        if (of_row) {
+            if constexpr (kHeld) {
+                few = whole_row() || complete;
+            } else if (!complete) {  // by float32 whether it may be; a search needs no sum beforehand
+                const float c = kLog2eD / t;
+                float mine = 0.f, above = 0.f;
+                row.each_floats([&](int, int, float (&z)[N]) {
+#pragma unroll
+                    for (int e = 0; e < N; ++e) {
+                        const float x = fmaxf(__builtin_amdgcn_exp2f((z[e] - top) * c), 0.f);
+                        mine += x;
+                        above += z[e] - bound >= 0.f ? x : 0.f;
+                    }
+                });
+                block_sum32<W>(mine, above, lds.estimate);
+                few = !(above < 0.999f * top_p * mine);
+                row.forget();
+            }
         }
+        bool known = !of_row || kHeld || complete;  // that what is needed is listed
         if (!few && least_bound > -kInf && weigh.whole(weigh.exact(least_bound)) < least_w) {  // perhaps min-p leaves few
             bound = gather_bound(least_bound);
-            few = true;
+            few = known = true;
         }
         if (few)
             gather(row, list, [&](float (&z)[N]) {
 #pragma unroll
                 for (int e = 0; e < N; ++e) z[e] -= bound;
             });
+        if constexpr (!kHeld)
+            if (of_row && few && list.count <= kList) few = whole_row() || known;
         const int n = few ? (int)list.count : 0;
         if (few && n <= kList) {
             read_keys<W>(row.p, list, n);
             __syncthreads();
-            if (tid < n) {  // its place in the order, and among the ids
-                const uint64_t key = list.key[tid];
-                int place = 0, by_id = 0;
+            {  // each one's place in the order, and among the ids, by neighbours that share the comparisons
+                constexpr int kShare = 64 * W / kList;
+                static_assert(kShare <= 4, "within a quad");
+                const int i = tid / kShare;
+                if (i < n) {
+                    const uint64_t key = list.key[i];
+                    uint32_t place = 0, by_id = 0;
 #pragma unroll 8
-                for (int j = 0; j < n; ++j) {
-                    place += list.key[j] > key;
-                    by_id += (uint32_t)list.key[j] > (uint32_t)key;
+                    for (int j = tid % kShare; j < n; j += kShare) {
+                        place += list.key[j] > key;
+                        by_id += (uint32_t)list.key[j] > (uint32_t)key;
+                    }
+                    uint64_t both = (uint64_t)by_id << 32 | place;
+                    if constexpr (kShare > 1) both += dpp_mov64<0xB1>(both);
+                    if constexpr (kShare > 2) both += dpp_mov64<0x4E>(both);
+                    place = (uint32_t)both;
+                    by_id = both >> 32;
+                    if (tid % kShare == 0) {
+                        lds.key[place] = key;
+                        lds.by_place[place] = by_id;
+                        lds.by_id[by_id] = key_id(key);
+                    }
                 }
-                lds.key[place] = key;
-                lds.by_place[place] = by_id;
-                lds.by_id[by_id] = key_id(key);
             }
             __syncthreads();
             if (wave != 0) return;
@@ -306,9 +360,10 @@ template <typename T, int W, int S, int RUNS> __global__ __launch_bounds__(64 * 
         }
         // the last of A by number, then that of B by weight
         __syncthreads();
-        auto search = [&](const Place& among, bool by_weight, uint64_t target) {
+        auto search = [&](const Place& among, bool by_weight) {
+            auto target = [&](uint64_t all) { return by_weight ? part_of<true>(top_p, all) : (uint64_t)k; };
             const float span = by_weight ? t * 45.f : kInf;  // a weight of e^-45 is nothing in units of 2^-50
-            if constexpr (kHeld) return find_last<T>(Held<T, W, S>{row, held, weigh, by_weight}, top, span, target, lds.search, list);
+            if constexpr (kHeld) return find_last<T>(Held<T, W, S>{row, held, weigh, among, by_weight}, top, span, target, lds.search, list);
             else return find_last<T>(Made<T, W>{loop, weigh, among, by_weight}, top, span, target, lds.search, list);
         };
         for (int step = 0; step < 2; ++step) {
@@ -324,24 +379,7 @@ template <typename T, int W, int S, int RUNS> __global__ __launch_bounds__(64 * 
                         __builtin_amdgcn_sched_barrier(0);
                     });
             }
-            if (by_weight && by_k) {
-                uint64_t mine = 0;
-                if constexpr (kHeld) {
-#pragma unroll
-                    for (int s = 0; s < S; ++s)
-#pragma unroll
-                        for (int e = 0; e < N; ++e) mine += held[s][e];
-                } else {
-                    loop.each_floats([&](int, int id, float (&z)[N]) {
-                        uint64_t w[N];
-                        weigh.wholes(z, w);
-#pragma unroll
-                        for (int e = 0; e < N; ++e) mine += up_to(z[e], id + e, last) ? w[e] : 0;
-                    });
-                }
-                all = block_sum64<W>(mine, lds.run);
-            }
-            last = search(last, by_weight, by_weight ? max(part_of<true>(top_p, all), (uint64_t)1) : (uint64_t)k);
+            last = search(last, by_weight);
         }
     }
     // runs' sums of what is left

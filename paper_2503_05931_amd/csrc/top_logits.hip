@@ -23,7 +23,7 @@ template <typename T, int W> struct Counted {
     static constexpr int N = RowVec<T>::n;
     RowLoop<T, W> loop;
     template <typename F> __device__ __forceinline__ void logits(F f) const {
-        loop.each_floats([&](int, int, float (&z)[N]) { f(z); });
+        loop.each_floats([&](int, int id, float (&z)[N]) { f(id, z); });
     }
     template <typename F> __device__ __forceinline__ void each(F f) const {
         loop.each_floats([&](int, int id, float (&z)[N]) {
@@ -33,10 +33,8 @@ template <typename T, int W> struct Counted {
             f(id, z, w);
         });
     }
-    template <typename F> __device__ __forceinline__ void members(F f) const {
-        loop.each_floats([&](int, int id, float (&z)[N]) { f(id, z, [&](int e) { return z[e] > -kInf; }); });
-    }
-    __device__ __forceinline__ uint64_t weight(float) const { return 1; }
+    __device__ __forceinline__ float logit(int id) const { return to_f32(loop.p[id]); }
+    __device__ __forceinline__ uint64_t weight(float z, int) const { return z > -kInf; }
 };
 template <int W> __device__ __forceinline__ float block_sum(float v, float* part) {
     v = wave_sum(v);
@@ -95,11 +93,13 @@ template <typename T, int W, int S> __global__ __launch_bounds__(64 * W) void to
     Place last{-kInf, INT_MAX};
     const bool searched = n > kList || !fits;
     if (searched) {  // many equal ones, mostly
-        if (top > -kInf) last = find_last<T>(Counted<T, W>{loop}, top, kInf, K, lds.search, list);
+        if (top > -kInf) last = find_last<T>(Counted<T, W>{loop}, top, kInf, [&](uint64_t) { return (uint64_t)K; }, lds.search, list);
         if (tid == 0) list.count = 0;
         __syncthreads();
-        loop.each([&](float z, int id) {
-            if (z > -kInf && up_to(z, id, last)) put_in(list, id);
+        loop.each_floats([&](int, int id, float (&z)[RowVec<T>::n]) {
+#pragma unroll
+            for (int e = 0; e < RowVec<T>::n; ++e) z[e] = z[e] > -kInf && up_to(z[e], id + e, last) ? 0.f : -1.f;
+            put_in(list, id, z);
         });
         __syncthreads();
         n = list.count;

@@ -304,9 +304,23 @@ __device__ __forceinline__ float gather_bound(float bound) {
     bound = fminf(fmaxf(bound, -kMostFloat), kMostFloat);
     return bound == 0.f ? -0.f : bound;
 }
-__device__ __forceinline__ void put_in(List& list, int id) {
-    const uint32_t at = atomicAdd(&list.count, 1u);
-    if (at < kList) list.id[at] = id;
+// puts in those of each lane's vector whose sign is not set; all lanes come along
+template <int N> __device__ __forceinline__ void put_in(List& list, int id, const float (&over)[N]) {
+    uint32_t marks = 0;
+#pragma unroll
+    for (int e = 0; e < N; ++e) marks = __builtin_amdgcn_alignbit(marks, __builtin_bit_cast(uint32_t, over[e]), 31);
+    marks = ~marks << (32 - N);
+    if (!__any(marks != 0)) return;
+    const uint32_t mine = __builtin_popcount(marks), through = wave_prefix(mine);
+    uint32_t base = 0;
+    if ((threadIdx.x & 63) == 63) base = atomicAdd(&list.count, through);
+    uint32_t at = lane_of(base, 63) + through - mine;
+    while (marks) {
+        const int e = __builtin_clz(marks);
+        marks &= ~(0x80000000u >> e);
+        if (at < kList) list.id[at] = id + e;
+        ++at;
+    }
 }
 // makes the first n listed elements' keys; a barrier has to follow
 template <int W, typename T> __device__ __forceinline__ void read_keys(const T* p, List& list, int n) {
@@ -363,9 +377,7 @@ template <typename T, int W, int S, typename F> __device__ __forceinline__ void 
     } else {
         row.each_floats([&](int, int id, float (&z)[N]) {
             over(z);
-#pragma unroll
-            for (int e = 0; e < N; ++e)
-                if (z[e] >= 0.f) put_in(list, id + e);
+            put_in(list, id, z);
         });
     }
     __syncthreads();
@@ -385,12 +397,12 @@ template <int W, int BITS, typename Weight = uint64_t> struct Search {
     Place last;
 };
 
-// source.each(f): f(first id, logits, weights) for every vector of the row; what weighs 0 takes no part (minus infinity and NaN among it, and something has to
-// take part); source.members(f): f(first id, logits, which): which(e) tells whether element e takes part; source.weight(logit): of one that does;
-// source.logits(f): f(logits).  target: the least sum of weights that the part up to its last element reaches, 1 or more; what is more than there is
-// counts as all.  span: what is further than that from the largest weighs 0, or nothing is known about it (infinity).
-template <typename T, int BITS, int W, typename Weight, typename Source>
-__device__ __forceinline__ Place find_last(const Source& source, float top, float span, uint64_t target, Search<W, BITS, Weight>& h, List& list) {
+// source.each(f): f(first id, logits, weights) for every vector of the row; what weighs 0 takes no part (minus infinity and NaN among it, and something has
+// to take part); source.logits(f): f(first id, logits) for every vector; source.logit(id), source.weight(logit, id): of one element.  target_of(all): the least
+// sum of weights that the part up to its last element reaches, of the sum of all; 0 is as good as 1, and what is more than there is counts as all.  span: what
+// is further than that from the largest weighs 0, or nothing is known about it (infinity).
+template <typename T, int BITS, int W, typename Weight, typename Source, typename F>
+__device__ __forceinline__ Place find_last(const Source& source, float top, float span, F target_of, Search<W, BITS, Weight>& h, List& list) {
     constexpr int N = RowVec<T>::n, kThreads = 64 * W, kBins = 1 << BITS, kEach = kBins < kThreads ? 1 : kBins / kThreads, kIdBits = 18;
     static_assert(kMostVocab <= 1 << kIdBits, "an id's digits");
     constexpr int kZLevels = (32 + BITS - 1) / BITS, kLevels = 1 + kZLevels + (kIdBits + BITS - 1) / BITS;
@@ -398,11 +410,11 @@ __device__ __forceinline__ Place find_last(const Source& source, float top, floa
     int bin0 = 0;
     uint32_t bits = 0, id_bits = 0;      // digits found so far
     int known = 32, id_known = kIdBits;  // and how many bits are below them
-    uint64_t passed = 0;                 // in front of the bin
+    uint64_t passed = 0, target = 0;     // passed: in front of the bin
     float rate;
     {
         float low = kInf;  // of those in the order
-        source.logits([&](const float (&z)[N]) {
+        source.logits([&](int, float (&z)[N]) {
 #pragma unroll
             for (int e = 0; e < N; ++e) low = fminf(low, z[e] > -kInf ? z[e] : kInf);
         });
@@ -470,7 +482,7 @@ __device__ __forceinline__ Place find_last(const Source& source, float top, floa
             at += i < wave ? h.part[i] : 0;
             all += h.part[i];
         }
-        if (level == 0) target = min(target, all);  // there may be fewer
+        if (level == 0) target = max(min(target_of(all), all), (uint64_t)1);  // there may be fewer
         if (at < target && target <= at + mine)
             for (int i = 0; i < kEach; ++i) {
                 const uint64_t v = h.sum[kEach * tid + i];
@@ -491,35 +503,58 @@ __device__ __forceinline__ Place find_last(const Source& source, float top, floa
             id_bits |= (uint32_t)h.bin << shift;
             id_known = shift;
         }
-        source.members([&](int first, const float (&z)[N], auto takes_part) {
-            bool here[N], any = false;
+        if (known == 32 && bin0 < kBins - 1) {  // of the distance in steps less the bin: 0 to 1 by its bits, so NaN and infinity are not in it
+            const float bin = (float)bin0;
+            source.logits([&](int id, float (&z)[N]) {
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                here[e] = in_bin(z[e], first + e);
-                any |= here[e];
-            }
-            if (!__any(any)) return;
-#pragma unroll
-            for (int e = 0; e < N; ++e)
-                if (here[e] && takes_part(e)) {
-                    const uint32_t to = atomicAdd(&list.count, 1u);
-                    if (to < kList) list.key[to] = order_key(z[e], first + e);
+                for (int e = 0; e < N; ++e) {
+                    const uint32_t u = __builtin_bit_cast(uint32_t, (top - z[e]) * rate - bin);
+                    z[e] = bits_f32(u | ~(u - 0x3f800000u));
                 }
-        });
+                put_in(list, id, z);
+            });
+        } else {
+            source.logits([&](int id, float (&z)[N]) {
+#pragma unroll
+                for (int e = 0; e < N; ++e) z[e] = z[e] > -kInf && in_bin(z[e], id + e) ? 0.f : -1.f;
+                put_in(list, id, z);
+            });
+        }
         __syncthreads();
         if (list.count <= kList || level + 1 == kLevels) break;
         for (int i = tid; i < kBins; i += kThreads) h.sum[i] = 0;
         __syncthreads();  // and all have read the count
     }
     const int n = min((int)list.count, kList);
-    for (int i = tid; i < n; i += kThreads) h.w[i] = (Weight)source.weight(key_logit(list.key[i]));
-    __syncthreads();
     for (int i = tid; i < n; i += kThreads) {
-        const uint64_t key = list.key[i], own = h.w[i];
-        uint64_t at = passed;
+        const int id = list.id[i];
+        const float z = source.logit(id);
+        list.key[i] = order_key(z, id);
+        h.w[i] = (Weight)source.weight(z, id);
+    }
+    __syncthreads();
+    if constexpr (kThreads > kList) {  // several neighbours for each element
+        constexpr int kShare = kThreads / kList;
+        static_assert(kShare <= 4, "within a quad");
+        const int i = tid / kShare;
+        if (i < n) {
+            const uint64_t key = list.key[i], own = h.w[i];
+            uint64_t at = 0;
 #pragma unroll 8
-        for (int j = 0; j < n; ++j) at += list.key[j] > key ? (uint64_t)h.w[j] : 0;
-        if (at < target && target <= at + own) h.last = Place{key_logit(key), key_id(key)};
+            for (int j = tid % kShare; j < n; j += kShare) at += list.key[j] > key ? (uint64_t)h.w[j] : 0;
+            at += dpp_mov64<0xB1>(at);
+            if constexpr (kShare == 4) at += dpp_mov64<0x4E>(at);
+            at += passed;
+            if (at < target && target <= at + own) h.last = Place{key_logit(key), key_id(key)};
+        }
+    } else {
+        for (int i = tid; i < n; i += kThreads) {
+            const uint64_t key = list.key[i], own = h.w[i];
+            uint64_t at = passed;
+#pragma unroll 8
+            for (int j = 0; j < n; ++j) at += list.key[j] > key ? (uint64_t)h.w[j] : 0;
+            if (at < target && target <= at + own) h.last = Place{key_logit(key), key_id(key)};
+        }
     }
     __syncthreads();
     const Place last = h.last;
