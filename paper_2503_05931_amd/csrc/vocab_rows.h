@@ -506,6 +506,7 @@ __device__ __forceinline__ Place find_last(const Source& source, float top, floa
         if (known == 32 && bin0 < kBins - 1) {  // of the distance in steps less the bin: 0 to 1 by its bits, so NaN and infinity are not in it
             const float bin = (float)bin0;
             source.logits([&](int id, float (&z)[N]) {
+#pragma clang fp contract(off)  // the same product as bin_of's
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
                     const uint32_t u = __builtin_bit_cast(uint32_t, (top - z[e]) * rate - bin);

@@ -79,10 +79,8 @@ def test_equal_logits(vocab, dtype):
             check(z, u, dtype, **how)
 
 
-@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
-def test_rows_that_lack_logits(dtype):
-    """Minus infinity, NaN and the type's lowest value in masked places; infinite logits; rows that have nothing left."""
-    z, u = rows(12, 700, seed=3)
+def lacking(vocab, dtype):
+    z, u = rows(12, vocab, seed=3)
     z = z.to(TYPE[dtype])
     g = torch.Generator().manual_seed(4)
     out = torch.rand(z.shape, generator=g) < 0.9
@@ -93,12 +91,44 @@ def test_rows_that_lack_logits(dtype):
     z[6] = -math.inf
     z[7] = math.nan
     z[8] = -math.inf
-    z[8, 699] = -3.0
+    z[8, vocab - 1] = -3.0
     z[9] = torch.finfo(TYPE[dtype]).min
     z[10, 17] = math.inf
     z[11, 17:40] = math.inf
+    return z, u
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_rows_that_lack_logits(dtype):
+    """Minus infinity, NaN and the type's lowest value in masked places; infinite logits; rows that have nothing left."""
+    z, u = lacking(700, dtype)
     for how in FILTERS:
         check(z, u, dtype, **how)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("vocab", [6000, 20000, 40003])
+def test_wide_rows_that_lack_logits(vocab, dtype):
+    z, u = lacking(vocab, dtype)
+    for how in (dict(), dict(top_k=5), dict(top_p=0.9), dict(min_p=0.01), dict(top_k=700, top_p=0.99, min_p=0.001, t=1.5), dict(top_p=0.8, min_p=0.02)):
+        check(z, u, dtype, **how)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("vocab", [255, 4096])
+def test_many_rows(vocab, dtype):
+    """More rows than have many wavefronts each: every filter, and the same bits as with a few rows at a time."""
+    z, u = rows(601, vocab, seed=5)
+    z = z.to(TYPE[dtype])
+    z[:12] = lacking(vocab, dtype)[0]
+    z[12:16], z[16] = 0.05 * z[12:16], 1.5
+    z[17] = (torch.arange(vocab) % 3).to(z.dtype)
+    z[18, vocab // 2:] = -math.inf
+    for how in FILTERS:
+        tokens, logp = draw(z, u, dtype, **how)
+        few = check(z[:24], u[:24], dtype, **how)
+        parts = few, draw(z[24:300], u[24:300], dtype, **how), draw(z[300:], u[300:], dtype, **how)
+        assert all(torch.equal(whole, torch.cat(part)) for whole, part in zip((tokens, logp), zip(*parts)))
 
 
 def test_uniforms():
