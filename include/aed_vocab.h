@@ -79,10 +79,10 @@ typedef struct aed_top_config {
     uint32_t struct_size;  /* = sizeof(aed_top_config) */
     int32_t vocab, dtype;
     int32_t top;           /* 1 to 128, at most vocab */
-    float temperature;     /* > 0, finite */
+    float temperature;     /* 1e-20 to 1e20 */
 } aed_top_config;
 
-/* Errors: AED_EINVAL (NULL, struct_size, vocab, dtype, top, temperature), AED_EUNSUPPORTED (vocab; top above 128). */
+/* Errors: AED_EINVAL (NULL, struct_size, vocab, dtype, top, temperature not above 0 or not finite), AED_EUNSUPPORTED (vocab; top above 128; other temperatures). */
 aed_status aed_top_create(const aed_top_config *cfg, void *hip_stream, aed_top **out);
 aed_status aed_top_destroy(aed_top *plan);
 /* values: DEVICE float32[rows, top]; ids: DEVICE int32[rows, top]; rest: DEVICE float32[rows]. */
@@ -102,14 +102,15 @@ aed_status aed_top_logits(aed_top *plan, const void *logits, int64_t row_stride,
  * An id may stand in a list more than once.  A row of weight 0 has L_r 0 and
  * gradient 0, whatever its logits and list hold, and so has one with neither
  * an entry nor (finite) rest.  Student's logits of minus infinity have p = 0 (L_r is
- * infinite where q is not 0 there); NaN and plus infinity give NaN. */
+ * infinite where q is not 0 there); NaN and plus infinity give NaN.  p's
+ * sums are float32: L_r is good to some 2^-22 T^2. */
 typedef struct aed_distill aed_distill; /* opaque */
 
 typedef struct aed_distill_config {
     uint32_t struct_size;  /* = sizeof(aed_distill_config) */
     int32_t vocab, dtype;
     int32_t top;           /* entries of a list, 1 to 128; may be more than vocab */
-    float temperature;     /* > 0, finite */
+    float temperature;     /* 1e-20 to 1e20 */
 } aed_distill_config;
 
 aed_status aed_distill_create(const aed_distill_config *cfg, void *hip_stream, aed_distill **out);

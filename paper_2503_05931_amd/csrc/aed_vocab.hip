@@ -1,7 +1,6 @@
 // Host side of include/aed_vocab.h: argument checks and launches of the operators on rows of logits.
 #include "../../include/aed_vocab.h"
 
-#include <algorithm>
 #include <cmath>
 
 #include "host_calls.h"
@@ -27,6 +26,7 @@ template <typename C> aed_status check_config(const C* c, const void* out) {
 template <typename C> aed_status check_list(const C* c) {
     if (c->top < 1) return fail(AED_EINVAL, "top must be >= 1");
     if (!(c->temperature > 0.f) || !std::isfinite(c->temperature)) return fail(AED_EINVAL, "temperature must be a finite number > 0");
+    if (c->temperature < 1e-20f || c->temperature > 1e20f) return fail(AED_EUNSUPPORTED, "temperature %g is not in 1e-20 to 1e20", (double)c->temperature);
     if (c->top > aed::kMostTop) return fail(AED_EUNSUPPORTED, "top %d is above %d", c->top, aed::kMostTop);
     return AED_OK;
 }
@@ -76,7 +76,7 @@ void set_temperature(const aed_distill_config& c, aed::DistillArgs& a) {
     a.scale_d = kLog2e / t;
     a.scale = (float)a.scale_d;
     if ((double)a.scale >= a.scale_d) a.scale = std::nextafter(a.scale, 0.f);
-    a.scale_low = std::max((float)(a.scale_d - (double)a.scale), 1e-37f);
+    a.scale_low = (float)(a.scale_d - (double)a.scale);  // above 2^-100, as the temperature is limited
     a.factor = t * t / kLog2e;
 }
 

@@ -322,7 +322,8 @@ template <typename T, int W, int S, bool STREAM> __global__ __launch_bounds__(64
     if constexpr (W > 1) __syncthreads();
     for (int k = tid; k < K; k += kThreads) {
         const float g = stats[2 + k];
-        if (g != kLeftOut) d[a.ids[(int64_t)r * K + k]] = from_f32<T>(slope * g);
+        const int id = a.ids[(int64_t)r * K + k];
+        if (g != kLeftOut && (unsigned)id < (unsigned)vocab) d[id] = from_f32<T>(slope * g);
     }
 }
 

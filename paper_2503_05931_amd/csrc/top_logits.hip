@@ -76,9 +76,10 @@ template <typename T, int W, int S> __global__ __launch_bounds__(64 * W) void to
     bound = gather_bound(bound);
     row.forget();
     const RowLoop<T, W> loop{row.p, row.n};
-    // Exponents relative to a border that the bound's own product, rounded, is not below.  Where a product could be infinite, the row is searched.
+    // Exponents relative to a border that the bound's own product, rounded, is not below.  Above 2^28 the border lies so far below the product that what is
+    // between may be infinite; such a row is searched.
     const float scaled = bound * a.scale, border = scaled - fabsf(scaled) * 0x1p-22f - 0x1p-126f;
-    const bool fits = fabsf(scaled) < 1e37f;
+    const bool fits = fabsf(scaled) < 0x1p28f;
     float sum = 0.f;  // of what is below the border, relative to it; may be NaN, if one is in the row
     gather(row, list, [&](float (&z)[RowVec<T>::n]) {
 #pragma unroll

@@ -53,6 +53,13 @@ def _lib():
     return lib
 
 
+def _i32(value, name):
+    """An int32's number: ctypes takes others modulo 2^32."""
+    if not -(1 << 31) <= value < 1 << 31:
+        _t._refuse(f"{name} {value} is not an int32")
+    return value
+
+
 def _rows(logits):
     return logits.shape[0] if logits.dim() == 2 else None  # None: refused for its shape
 
@@ -65,7 +72,7 @@ class _RowsPlan(_t._Plan):
         lib = self.lib = _lib()
         self.vocab = vocab
         self.cfg = cfg
-        cfg.struct_size, cfg.vocab, cfg.dtype = C.sizeof(type(cfg)), vocab, int(dtype == self.torch.bfloat16)
+        cfg.struct_size, cfg.vocab, cfg.dtype = C.sizeof(type(cfg)), _i32(vocab, "vocab"), int(dtype == self.torch.bfloat16)
         self._start(0, lambda _, st, h: getattr(lib, f"aed_{name}_create")(C.byref(cfg), st, h), getattr(lib, f"aed_{name}_destroy"))
 
     def _logits(self, t, name, rows=None):
@@ -100,7 +107,7 @@ class Sampler(_RowsPlan):
                 setattr(how, name + "s", self._flat(value, name, dtype, (rows,)))
                 numbers = False
             else:
-                setattr(how, name, value)
+                setattr(how, name, _i32(value, name) if name == "top_k" else value)
                 setattr(how, name + "s", None)
                 numbers = numbers and type(value) in (int, float)
         self._given_how = (temperature, top_k, top_p, min_p) if numbers else None
@@ -129,7 +136,7 @@ class TopLogits(_RowsPlan):
     """A teacher's largest logits of every row, for Distillation."""
 
     def __init__(self, vocab: int, top: int, dtype, temperature: float = 1.0, device="cuda", stream=None):
-        super().__init__(vocab, dtype, device, stream, "top", AedTopConfig(top=top, temperature=temperature))
+        super().__init__(vocab, dtype, device, stream, "top", AedTopConfig(top=_i32(top, "top"), temperature=temperature))
         self.top = top
         self._i32 = self.torch.empty(0, dtype=self.torch.int32, device=self.device)
 
@@ -153,7 +160,7 @@ class Distillation(_RowsPlan):
     """The loss of a student's rows of logits against a teacher's largest logits."""
 
     def __init__(self, vocab: int, top: int, dtype, temperature: float = 1.0, device="cuda", stream=None):
-        super().__init__(vocab, dtype, device, stream, "distill", AedDistillConfig(top=top, temperature=temperature))
+        super().__init__(vocab, dtype, device, stream, "distill", AedDistillConfig(top=_i32(top, "top"), temperature=temperature))
         self.top = top
 
     def aed_distill_forward(self, logits, values, ids, rest=None, weights=None):

@@ -228,6 +228,19 @@ def test_row_strides_and_gradients_in_place(vocab, pitch, skip, rest, dtype):
     assert (flat == 100).all()
 
 
+def test_gradients_by_other_ids_stay_in_their_rows():
+    """ids are looked at again: those that do not belong to the stats reach no other row."""
+    from paper_2503_05931_amd import vocabulary as L
+    c = make(5, 90, 7, "fp32", seed=14, unscored=0)
+    plan = L.Distillation(90, 7, torch.float32)
+    z, ids = c["z"].cuda(), c["ids"].cuda()
+    stats = plan.aed_distill_forward(z, c["values"].cuda(), ids, rest=c["rest"].cuda())[2]
+    ids[0, 1], ids[2, 3], ids[4, 6] = 91, -1, 2 ** 31 - 1
+    place = torch.full((5, 100), 7.0, device="cuda")
+    plan.aed_distill_backward(z, ids, stats, d_logits=place[:, :90])
+    assert (place[:, 90:] == 7).all()
+
+
 def test_offsets_past_32_bits():
     c = make(3, 900, 9, "bf16", seed=11, unscored=0)
     far = torch.empty(3 * (1 << 30), dtype=torch.bfloat16, device="cuda").as_strided((3, 900), (1 << 30, 1))

@@ -94,6 +94,19 @@ def test_temperatures(t):
         check(z, top, "fp32", t=t)
 
 
+@pytest.mark.parametrize("fill", [-3e4, -1e9, -7e19, -3e37, 2e9])
+def test_others_at_one_large_value(fill):
+    """Masks of many sizes, few enough of them to be listed, where a list reaches into them and where it does not."""
+    z = rows(6, 190, seed=12)
+    out = torch.rand((6, 190), generator=torch.Generator().manual_seed(3)) < 0.9
+    z[:4][out[:4]] = fill
+    z[4] = fill
+    z[5] = fill * (1 + torch.arange(190) / 64)
+    for top in (4, 40):
+        check(z, top, "fp32", t=1.0)
+        check(z, top, "fp32", t=0.3)
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("pitch,skip", [(1024, 0), (1003, 1), (1005, 2), (2000, 3)])
 def test_row_strides(pitch, skip, dtype):

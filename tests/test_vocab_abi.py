@@ -130,6 +130,21 @@ def test_distill_refuses_before_a_launch(lib):
     assert forward(rows=0, loss=None) == E
 
 
+@pytest.mark.parametrize("name", ["top", "distill"])
+def test_temperatures_are_limited(lib, name):
+    for t, status in ((1e-20, OK), (1e20, OK), (1e-21, U), (2e20, U), (1e-45, U), (0.0, E), (-1.0, E), (float("nan"), E), (float("inf"), E)):
+        assert make(lib, name, config(name, temperature=t))[0] == status, t
+
+
+def test_numbers_that_are_no_int32():
+    import torch
+    for call in (lambda: L._i32(1 << 31, "top_k"), lambda: L._i32(-(1 << 31) - 1, "vocab"), lambda: L.TopLogits(100, (1 << 32) + 5, torch.float32),
+                 lambda: L.Distillation(100, (1 << 32) + 5, torch.float32)):
+        with pytest.raises(binding.AedError, match="is not an int32"):
+            call()
+    assert L._i32((1 << 31) - 1, "top_k") == (1 << 31) - 1
+
+
 # ---------------------------------------------------------------- the binding, with torch's streams and the library played by recorders
 class HostDistillation(L.Distillation):
     """Calls of a plan, by torch on the host; no library"""
