@@ -283,6 +283,13 @@ template <typename T, int W, int S, int RUNS> __global__ __launch_bounds__(64 * 
 #pragma unroll
                 for (int e = 0; e < N; ++e) z[e] -= bound;
             });
+        if (few && by_k && k <= kMostListed && list.count > kList) {
+            bound = gather_bound(listed_bound<W>(row.p, list, k));
+            gather(Row<T, W, 0>(row.p, row.n), list, [&](float (&z)[N]) {
+#pragma unroll
+                for (int e = 0; e < N; ++e) z[e] -= bound;
+            });
+        }
         if constexpr (!kHeld)
             if (of_row && few && list.count <= kList) few = whole_row() || known;
         const int n = few ? (int)list.count : 0;
@@ -471,7 +478,8 @@ template <typename T, int W, int S> hipError_t launch_sample_as(const SampleArgs
 template <typename T> hipError_t launch_sample_of(const SampleArgs& a, hipStream_t s) {
     constexpr int N = RowVec<T>::n;
     if (a.z.vocab <= 4096) return a.z.rows <= kFewRows ? launch_sample_as<T, 8, 8 / N>(a, s) : launch_sample_as<T, 4, 16 / N>(a, s);
-    if (a.z.vocab <= 1024 * 16) return launch_sample_as<T, 16, 16 / N>(a, s);
+    if (a.z.vocab <= 512 * 16) return launch_sample_as<T, 8, 16 / N>(a, s);
+    if (a.z.vocab <= 512 * 32) return launch_sample_as<T, 8, 32 / N>(a, s);
     if (a.z.vocab <= 1024 * 32) return launch_sample_as<T, 16, 32 / N>(a, s);
     return launch_sample_as<T, 16, 0>(a, s);
 }

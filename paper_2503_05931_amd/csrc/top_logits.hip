@@ -17,7 +17,35 @@ template <int W> struct TopLds {
     Search<W, 8, uint8_t> search;
     float part[W];
     float over[kList];
+    uint32_t place[W > 1 ? kList : 1];
 };
+// Each one's place: put(key, how many of the n keys are larger).  A lane has M of them, so that a key that is read from LDS, where all lanes take the same, is
+// compared M times: reading costs more than comparing.  Wavefronts share the keys to compare with.  64 of 4096 in bfloat16, 8448 rows: 25.9 us, and 28.2 with one key
+// a lane at a time.
+template <int W, int M, typename F> __device__ __forceinline__ void place_all(TopLds<W>& lds, int n, F put) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint64_t key[M];
+    uint32_t place[M] = {};
+#pragma unroll
+    for (int i = 0; i < M; ++i) key[i] = lds.list.key[min(64 * i + lane, n - 1)];
+#pragma unroll 8
+    for (int j = wave; j < n; j += W) {
+        const uint64_t other = lds.list.key[j];
+#pragma unroll
+        for (int i = 0; i < M; ++i) place[i] += other > key[i];
+    }
+    if constexpr (W == 1) {
+#pragma unroll
+        for (int i = 0; i < M; ++i)
+            if (64 * i + lane < n) put(key[i], place[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < M; ++i)
+            if (64 * i + lane < n) atomicAdd(&lds.place[64 * i + lane], place[i]);
+        __syncthreads();
+        for (int i = threadIdx.x; i < n; i += 64 * W) put(lds.list.key[i], lds.place[i]);
+    }
+}
 // every element of the order counts 1
 template <typename T, int W> struct Counted {
     static constexpr int N = RowVec<T>::n;
@@ -73,23 +101,33 @@ template <typename T, int W, int S> __global__ __launch_bounds__(64 * W) void to
     int32_t* const ids = a.ids + (int64_t)r * K;
     float top, bound;
     bound_row<W>(row, K, lds.bounds, list, top, bound);
-    bound = gather_bound(bound);
     row.forget();
     const RowLoop<T, W> loop{row.p, row.n};
-    // Exponents relative to a border that the bound's own product, rounded, is not below.  Above 2^28 the border lies so far below the product that what is
-    // between may be infinite; such a row is searched.
-    const float scaled = bound * a.scale, border = scaled - fabsf(scaled) * 0x1p-22f - 0x1p-126f;
-    const bool fits = fabsf(scaled) < 0x1p28f;
-    float sum = 0.f;  // of what is below the border, relative to it; may be NaN, if one is in the row
-    gather(row, list, [&](float (&z)[RowVec<T>::n]) {
+    float border, sum;  // sum: of what is below the border, relative to it; may be NaN, if one is in the row
+    bool fits;
+    auto take = [&](const auto& from) {
+        // Exponents relative to a border that the bound's own product, rounded, is not below.  Where a product could be infinite, the row is searched; where the
+        // sum is (what is listed may lie far above the border, if that is large), it is made again below.
+        bound = gather_bound(bound);
+        const float scaled = bound * a.scale;
+        border = scaled - fabsf(scaled) * 0x1p-22f - 0x1p-126f;
+        fits = fabsf(scaled) < 1e37f;
+        sum = 0.f;
+        gather(from, list, [&](float (&z)[RowVec<T>::n]) {
 #pragma unroll
-        for (int e = 0; e < RowVec<T>::n; ++e) {
-            z[e] = fmaf(z[e], a.scale, -border);
-            const float below = __builtin_amdgcn_fmed3f(z[e] * -0x1p100f, 0.f, 1.f);
-            sum = fmaf(__builtin_amdgcn_exp2f(z[e]), below, sum);
-        }
-    });
-    asm volatile("" : "+v"(sum));  // it is made here, not where it is used: there the row would have to be kept
+            for (int e = 0; e < RowVec<T>::n; ++e) {
+                z[e] = fmaf(z[e], a.scale, -border);
+                const float below = __builtin_amdgcn_fmed3f(z[e] * -0x1p100f, 0.f, 1.f);
+                sum = fmaf(__builtin_amdgcn_exp2f(z[e]), below, sum);
+            }
+        });
+        asm volatile("" : "+v"(sum));  // it is made here, not where it is used: there the row would have to be kept
+    };
+    take(row);
+    if (list.count > kList) {
+        bound = listed_bound<W>(row.p, list, K);
+        take(Row<T, W, 0>(row.p, row.n));
+    }
     int n = list.count;
     Place last{-kInf, INT_MAX};
     const bool searched = n > kList || !fits;
@@ -106,10 +144,10 @@ template <typename T, int W, int S> __global__ __launch_bounds__(64 * W) void to
         n = list.count;
     }
     read_keys<W>(row.p, list, n);
+    if constexpr (W > 1)
+        for (int i = tid; i < kList; i += kThreads) lds.place[i] = 0;
     __syncthreads();
-    for (int i = tid; i < n; i += kThreads) {
-        const uint64_t key = list.key[i];
-        const int place = place_of(list, key, n);
+    auto put = [&](uint64_t key, int place) {
         const float z = key_logit(key);
         if (place < K) {
             values[place] = z;
@@ -118,7 +156,10 @@ template <typename T, int W, int S> __global__ __launch_bounds__(64 * W) void to
         } else {
             lds.over[place] = z;
         }
-    }
+    };
+    if (n <= 64) place_all<W, 1>(lds, n, put);
+    else if (n <= 128) place_all<W, 2>(lds, n, put);
+    else place_all<W, 4>(lds, n, put);
     for (int i = n + tid; i < K; i += kThreads) {
         values[i] = -kInf;
         ids[i] = -1;
@@ -151,16 +192,19 @@ template <typename T, int W, int S> hipError_t launch_top_as(const TopArgs& a, h
     top_logits_kernel<T, W, S><<<dim3(a.z.rows), dim3(64 * W), 0, s>>>(a);
     return hipGetLastError();
 }
+// One wavefront has no barriers to wait at and lists the fewest elements; more are for what one has no registers for.  8448 rows of 4096 in bfloat16, 32 of them:
+// one 18.2 us, four 31.2, 128 of them 44.8 and 54.2; 2048 of 32768, 64 of them: four 35.4, sixteen 92; 2048 of 65536: eight 84, sixteen 120.  Rows that no registers hold, 256 of 262144 in
+// float32: eight wavefronts 96, sixteen 212; 4 of 131072: 31 and 22.
+constexpr int kManyRows = 256;
+
 template <typename T> hipError_t launch_top_of(const TopArgs& a, hipStream_t s) {
     const int vecs = (a.z.vocab + RowVec<T>::n - 1) / RowVec<T>::n;
-    if (a.top <= 64) {
-        if (vecs <= 64 * 2) return launch_top_as<T, 1, 2>(a, s);
-        if (vecs <= 64 * 8) return launch_top_as<T, 1, 8>(a, s);
-    }
+    if (vecs <= 64 * 2) return launch_top_as<T, 1, 2>(a, s);
+    if (vecs <= 64 * 8) return launch_top_as<T, 1, 8>(a, s);
     if (vecs <= 256 * 4) return launch_top_as<T, 4, 4>(a, s);
     if (vecs <= 256 * 16) return launch_top_as<T, 4, 16>(a, s);
-    if (vecs <= 1024 * 8) return launch_top_as<T, 16, 8>(a, s);
-    return launch_top_as<T, 16, 0>(a, s);
+    if (vecs <= 512 * 16) return launch_top_as<T, 8, 16>(a, s);
+    return a.z.rows >= kManyRows ? launch_top_as<T, 8, 0>(a, s) : launch_top_as<T, 16, 0>(a, s);
 }
 
 }  // namespace
