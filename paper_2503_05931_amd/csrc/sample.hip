@@ -12,15 +12,22 @@
 //   search  they leave many: the end of the first part is searched for by histograms (find_last)
 //   sums    whatever is left is added up by runs of one wavefront's vector (256 or 512 ids in a row); the run that the random number falls into is
 //           then gone through by one wavefront
+//
+// Bound by latency in small calls (1 row of 4096: 4.6 us without filters, 6.4 by top-k 50, 11 by top-p 0.9 of a flat row, of which 4 are a launch and its first
+// access: some fifteen barriers, each with a trip to LDS) and by vector instructions in large ones: some 22 a weight, made once without filters (1024 rows
+// of 4096 in float32: 9.2 us), twice in a search, whose histogram's additions cost as much as a weight (128 of 32768 in bfloat16 by top-p: 40 us, of which the weights
+// are 12, the histogram's additions 6, the row's bound 2, gathering and comparing the border's bin 5; half of the compute units have no row).
 #include "vocab_rows.h"
 
 namespace aed {
 
 namespace {
 
-constexpr int kWanted = 64;      // gathered for top-p: a nucleus of a trained model's row is seldom larger
-constexpr int kFewRows = 512;     // two a compute unit: eight wavefronts each
-constexpr int kMostListed = 128;  // top-k above it goes by search
+constexpr int kWanted = 64;  // gathered for top-p: a nucleus of a trained model's row is seldom larger
+// Rows of up to 4096, two a compute unit, have eight wavefronts each, whose threads hold their weights in registers.  Of 4096 in float32, by top-p: 256 rows with
+// eight 12.0 us, with four 16.5; 512 rows 15.9 and 19.2; 1024 rows 28.9 and 25.9, by top-k 15.4 and 9.7, without filters 11.4 and 9.2.
+constexpr int kFewRows = 512;
+constexpr int kMostListed = 128;  // top-k above it goes by search: half a list, as the bound lets more in than are asked for
 
 template <int W, int RUNS> struct SampleLds {
     static constexpr int kBits = W > 4 ? 11 : 10;
@@ -475,6 +482,8 @@ template <typename T, int W, int S> hipError_t launch_sample_as(const SampleArgs
     sample_kernel<T, W, S, (runs < 2 * W ? 2 * W : runs)><<<dim3(a.z.rows), dim3(64 * W), 0, s>>>(a);
     return hipGetLastError();
 }
+// Of 512 rows of 8000 in bfloat16 by top-p, eight wavefronts take 27 us, sixteen 44; of 256 of 14000 by top-k 50 8.5 and 21: sixteen fill a compute unit, and one row
+// that is late leaves it idle.  Above 16384 sixteen have the registers: 128 of 32768 by top-p 40 us, eight 44.
 template <typename T> hipError_t launch_sample_of(const SampleArgs& a, hipStream_t s) {
     constexpr int N = RowVec<T>::n;
     if (a.z.vocab <= 4096) return a.z.rows <= kFewRows ? launch_sample_as<T, 8, 8 / N>(a, s) : launch_sample_as<T, 4, 16 / N>(a, s);
