@@ -25,12 +25,6 @@ struct Partial {
 
 // 2^y, minus infinity and NaN as they are
 __device__ __forceinline__ double exactly(const Pow2& pow2, double y) { return y != y ? y : pow2(y); }
-// log2 x of x > 0 that is near to what a float can be: that of the float nearest, and of what 2 to its power lacks
-__device__ __forceinline__ double log2_of(const Pow2& pow2, double x) {
-    const double near = __builtin_amdgcn_logf((float)x), left = x * pow2(-near) - 1;  // some 1e-7
-    return near + left * (1 - 0.5 * left) * kLog2eD;
-}
-
 constexpr int kMarks = 8192;  // ids of a list that fall on the same of so many bits may be the same
 
 }  // namespace

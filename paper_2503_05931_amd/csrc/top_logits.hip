@@ -133,7 +133,12 @@ template <typename T, int W, int S> __global__ __launch_bounds__(64 * W) void to
     Place last{-kInf, INT_MAX};
     const bool searched = n > kList || !fits;
     if (searched) {  // many equal ones, mostly
-        if (top > -kInf) last = find_last<T>(Counted<T, W>{loop}, top, kInf, [&](uint64_t) { return (uint64_t)K; }, lds.search, list);
+        if (top > -kInf) {
+            const Counted<T, W> source{loop};
+            begin_search<T>(source, lds.search);
+            __syncthreads();
+            last = find_last<T>(source, top, kInf, [&](uint64_t) { return (uint64_t)K; }, lds.search, list);
+        }
         if (tid == 0) list.count = 0;
         __syncthreads();
         loop.each_floats([&](int, int id, float (&z)[RowVec<T>::n]) {

@@ -249,6 +249,12 @@ struct Pow2 {
     }
 };
 
+// log2 x of x > 0 that is near to what a float can be: that of the float nearest, and of what 2 to its power lacks
+__device__ __forceinline__ double log2_of(const Pow2& pow2, double x) {
+    const double near = __builtin_amdgcn_logf((float)x), left = x * pow2(-near) - 1;  // some 1e-7
+    return near + left * (1 - 0.5 * left) * kLog2eD;
+}
+
 // An element's place in the order: of two, the one in front has the larger key
 __device__ __forceinline__ uint64_t order_key(float z, int id) { return (uint64_t)rising_bits(z) << 32 | (uint32_t)~id; }
 __device__ __forceinline__ float key_logit(uint64_t key) {
@@ -423,6 +429,19 @@ template <int W, int BITS, typename Weight = uint64_t> struct Search {
     Place last;
 };
 
+// Before each search: the least logit of the order, and empty bins.  A barrier has to follow.
+template <typename T, int BITS, int W, typename Weight, typename Source> __device__ __forceinline__ void begin_search(const Source& source, Search<W, BITS, Weight>& h) {
+    constexpr int N = RowVec<T>::n;
+    float low = kInf;
+    source.logits([&](int, float (&z)[N]) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) low = fminf(low, z[e] > -kInf ? z[e] : kInf);
+    });
+    low = wave_min(low);
+    if ((threadIdx.x & 63) == 0) h.low[threadIdx.x >> 6] = low;
+    for (int i = threadIdx.x; i < 1 << BITS; i += 64 * W) h.sum[i] = 0;
+}
+
 // source.each(f): f(first id, logits, weights) for every vector of the row; what weighs 0 takes no part (minus infinity and NaN among it, and something has
 // to take part); source.logits(f): f(first id, logits) for every vector; source.logit(id), source.weight(logit, id): of one element.  target_of(all): the least
 // sum of weights that the part up to its last element reaches, of the sum of all; 0 is as good as 1, and what is more than there is counts as all.  span: what
@@ -437,21 +456,10 @@ __device__ __forceinline__ Place find_last(const Source& source, float top, floa
     uint32_t bits = 0, id_bits = 0;      // digits found so far
     int known = 32, id_known = kIdBits;  // and how many bits are below them
     uint64_t passed = 0, target = 0;     // passed: in front of the bin
-    float rate;
-    {
-        float low = kInf;  // of those in the order
-        source.logits([&](int, float (&z)[N]) {
+    float low = h.low[0];
 #pragma unroll
-            for (int e = 0; e < N; ++e) low = fminf(low, z[e] > -kInf ? z[e] : kInf);
-        });
-        low = wave_min(low);
-        if (lane == 0) h.low[wave] = low;
-        for (int i = tid; i < kBins; i += kThreads) h.sum[i] = 0;
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < W; ++i) low = fminf(low, h.low[i]);
-        rate = (float)kBins / fminf(fmaxf(top - low, 0x1p-100f), span);
-    }
+    for (int i = 1; i < W; ++i) low = fminf(low, h.low[i]);
+    const float rate = (float)kBins / fminf(fmaxf(top - low, 0x1p-100f), span);
     auto bin_of = [&](float z) { return (int)fminf((top - z) * rate, (float)(kBins - 1)); };
     auto in_bin = [&](float z, int id) {
         if (known == 32) return bin_of(z) == bin0;
@@ -584,9 +592,7 @@ __device__ __forceinline__ Place find_last(const Source& source, float top, floa
         }
     }
     __syncthreads();
-    const Place last = h.last;
-    __syncthreads();  // list and histogram may be used again
-    return last;
+    return h.last;
 }
 
 }  // namespace aed
