@@ -13,10 +13,11 @@
 //   sums    whatever is left is added up by runs of one wavefront's vector (256 or 512 ids in a row); the run that the random number falls into is
 //           then gone through by one wavefront
 //
-// Bound by latency in small calls (1 row of 4096: 4.6 us without filters, 6.4 by top-k 50, 11 by top-p 0.9 of a flat row, of which 4 are a launch and its first
-// access: some fifteen barriers, each with a trip to LDS) and by vector instructions in large ones: some 22 a weight, made once without filters (1024 rows
-// of 4096 in float32: 9.2 us), twice in a search, whose histogram's additions cost as much as a weight (128 of 32768 in bfloat16 by top-p: 40 us, of which the weights
-// are 12, the histogram's additions 6, the row's bound 2, gathering and comparing the border's bin 5; half of the compute units have no row).
+// Bound by latency in small calls (1 row of 4096: 4.5 us without filters, 6.2 by top-k 50, 9.7 by top-p 0.9, of which 4 are a launch and its first
+// access; a search goes through some ten barriers, and what lies between them is a hundred or two of instructions of eight wavefronts that wait for each other) and by
+// vector instructions in large ones: some 22 a weight, made once without filters (1024 rows of 4096 in float32: 9.1 us), twice in a search, once for the
+// histogram and once for the runs (128 of 32768 in bfloat16 by top-p: 40 us; histogram 11, runs 10, whether a list will do 4, the row's bound, its least logit and
+// the border's bin 9; half of the compute units have no row).
 #include "vocab_rows.h"
 
 namespace aed {
@@ -25,7 +26,7 @@ namespace {
 
 constexpr int kWanted = 64;  // gathered for top-p: a nucleus of a trained model's row is seldom larger
 // Rows of up to 4096, two a compute unit, have eight wavefronts each, whose threads hold their weights in registers.  Of 4096 in float32, by top-p: 256 rows with
-// eight 12.0 us, with four 16.5; 512 rows 15.9 and 19.2; 1024 rows 28.9 and 25.9, by top-k 15.4 and 9.7, without filters 11.4 and 9.2.
+// eight 10.7 us, with four 16.5; 512 rows 15.9 and 19.2; 1024 rows 28.9 and 25.1, by top-k 15.4 and 9.7, without filters 11.4 and 9.2.
 constexpr int kFewRows = 512;
 constexpr int kMostListed = 128;  // top-k above it goes by search: half a list, as the bound lets more in than are asked for
 
