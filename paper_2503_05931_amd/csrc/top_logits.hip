@@ -125,7 +125,8 @@ template <typename T, int W, int S> __global__ __launch_bounds__(64 * W) void to
         asm volatile("" : "+v"(sum));  // it is made here, not where it is used: there the row would have to be kept
     };
     take(row);
-    if (list.count > kList) {
+    const bool again = list.count > kList;
+    if (again) {
         bound = listed_bound<W>(row.p, list, K);
         take(Row<T, W, 0>(row.p, row.n));
     }
@@ -175,10 +176,10 @@ template <typename T, int W, int S> __global__ __launch_bounds__(64 * W) void to
         __syncthreads();
         // listed, but not among the first: in their order, as the list has none
         for (int i = K + tid; i < n; i += kThreads) sum += __builtin_amdgcn_exp2f(fmaf(lds.over[i], a.scale, -border));
-        sum = searched ? 0.f : block_sum<W>(sum, lds.part);
+        sum = searched || (again && W > 1) ? 0.f : block_sum<W>(sum, lds.part);  // the second bound is that of what was listed first, by whichever wavefront
         if (sum >= 0x1p-60f && sum < 0x1p100f) {
             rest = kLn2 * (border + __builtin_amdgcn_logf(sum));
-        } else {  // nothing, or far from the border: relative to its own largest
+        } else {  // nothing, or far from the border, or by another one each time: relative to its own largest
             last = lds.search.last;
             float m = -kInf;
             loop.each([&](float z, int id) { m = up_to(z, id, last) ? m : fmaxf(m, z); });

@@ -51,6 +51,42 @@ def test_wide_vocabularies(vocab, dtype):
         check(rows(1, vocab, seed=vocab + top), top, dtype)
 
 
+def test_same_bits_where_a_wavefront_knows_little():
+    """A quarter of a row's lanes hold small logits only, so far more are listed than there is room for, in another order each time."""
+    from paper_2503_05931_amd import vocabulary as L
+    g = torch.Generator().manual_seed(21)
+    z = torch.randn((40, 16384), generator=g)
+    z.view(40, 16, 4, 256)[:, :, 3] -= 10                     # every fourth wavefront's vectors
+    for top in (2, 4, 8):
+        z_d = z.cuda()
+        plan = L.TopLogits(16384, top, torch.float32, temperature=3.0)
+        first = plan.aed_top_logits(z_d)
+        for _ in range(30):
+            assert all(torch.equal(a, b) for a, b in zip(plan.aed_top_logits(z_d), first))
+        check(z[:8], top, "fp32", t=3.0)
+
+
+@pytest.mark.parametrize("dtype,vocab", [("fp32", 40003), ("bf16", 70001)])
+def test_many_wide_rows(vocab, dtype):
+    """More rows than have sixteen wavefronts each: as the definition says, and lists as with a few rows at a time (what is summed, in another order)."""
+    from paper_2503_05931_amd import vocabulary as L
+    z = rows(258, vocab, seed=9).to(TYPE[dtype])
+    z[1], z[2, 100:] = 0.5, -math.inf
+    z[3, ::2], z[4] = math.nan, -math.inf
+    for top in (8, 128):
+        plan = L.TopLogits(vocab, top, TYPE[dtype], temperature=2.0)
+        values, ids, rest = plan.aed_top_logits(z.cuda())
+        parts = [plan.aed_top_logits(z[i:i + 129].cuda()) for i in (0, 129)]
+        assert torch.equal(values, torch.cat([p[0] for p in parts])) and torch.equal(ids, torch.cat([p[1] for p in parts]))
+        other = torch.cat([p[2] for p in parts])
+        assert torch.equal(rest.isinf(), other.isinf())
+        assert ((rest - other).abs()[~rest.isinf()] <= 2 * (2.4e-6 + 2 ** -23 * other.abs()[~rest.isinf()])).all()
+        for r in range(6):
+            v, i, o = R.top_logits(z[r].float().numpy(), top, 2.0)
+            assert ids[r].tolist() == i and values[r].tolist() == v
+            assert float(rest[r]) == o or abs(float(rest[r]) - o) <= 2.4e-6 + 2 * 2 ** -24 * abs(o)
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("vocab", [100, 2048, 5000, 33000])
 def test_equal_logits(vocab, dtype):
