@@ -402,7 +402,7 @@ template <typename T, int W, int S, typename F> __device__ __forceinline__ void 
 }
 
 // Of a list that is cut off: the logit of its k-th element (k <= kList), a bound that k of the row are not below as well, and k / kList of those that the last one
-// let in.  The list is empty then.  One row of 200 of 30000 whose lanes' maxima gave no good bound had made top-k 50 of them last 29 us, not 9.
+// let in.  The list is empty then.  One row of 200 of 30000 whose lanes' maxima gave no good bound had made top-k 50 of them last 29 us, not 14.
 template <int W, typename T> __device__ __forceinline__ float listed_bound(const T* p, List& list, int k) {
     read_keys<W>(p, list, kList);
     __syncthreads();
