@@ -120,6 +120,19 @@ def test_rows_that_lack_logits(vocab, dtype):
         check(z, top, dtype)
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("vocab", [1, 64, 500, 4000, 16000, 30000, 70001])
+def test_rows_with_nothing_in_the_order(vocab, dtype):
+    """Every number of wavefronts; rows that have logits between them."""
+    z = rows(6, vocab, seed=vocab).to(TYPE[dtype])
+    z[0] = z[2] = z[5] = -math.inf
+    z[2, ::2] = z[3] = math.nan
+    for top in sorted({min(vocab, k) for k in (1, 20, 128)}):
+        values, ids, rest = check(z, top, dtype)
+        for r in (0, 2, 3, 5):
+            assert (values[r] == -math.inf).all() and (ids[r] == -1).all() and float(rest[r]) == -math.inf
+
+
 @pytest.mark.parametrize("t", [1e-3, 0.05, 30.0, 1e4])
 def test_temperatures(t):
     """What is left lies far below the list, or all weights are alike."""
