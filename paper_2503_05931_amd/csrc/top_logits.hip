@@ -141,6 +141,7 @@ template <typename T, int W, int S> __global__ __launch_bounds__(64 * W) void to
             __syncthreads();
             last = find_last<T>(source, top, kInf, [&](uint64_t) { return (uint64_t)K; }, lds.search, list);
         }
+        __syncthreads();  // every wavefront has come here by the count
         if (tid == 0) list.count = 0;
         __syncthreads();
         loop.each_floats([&](int, int id, float (&z)[RowVec<T>::n]) {

@@ -133,6 +133,26 @@ def test_rows_with_nothing_in_the_order(vocab, dtype):
             assert (values[r] == -math.inf).all() and (ids[r] == -1).all() and float(rest[r]) == -math.inf
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("vocab", [2048, 4096, 8192, 30000, 70001])
+def test_rows_of_nan_at_high_temperatures(vocab, dtype):
+    """More NaN than a list holds and nothing in the order, where exponents relative to the list's end are finite: whether such a row is searched is the count's
+    decision alone."""
+    from paper_2503_05931_amd import vocabulary as L
+    z = rows(8, vocab, seed=vocab).to(TYPE[dtype])
+    z[0] = z[4] = math.nan
+    z[1], z[1, 7::3] = -math.inf, math.nan
+    z[2, ::2], z[2, 1::2] = math.nan, -math.nan
+    z[3], z[3, :vocab // 2] = -math.inf, math.nan
+    z[5, 1:] = math.nan
+    for t in (60.0, 100.0, 1e4):
+        for top in (1, 32, 128):
+            check(z, top, dtype, t=t)
+    many = z[[0, 1, 2, 3]].repeat(80, 1).cuda()
+    values, ids, rest = L.TopLogits(vocab, 32, TYPE[dtype], temperature=100.0).aed_top_logits(many)
+    assert (values == -math.inf).all() and (ids == -1).all() and (rest == -math.inf).all()
+
+
 @pytest.mark.parametrize("t", [1e-3, 0.05, 30.0, 1e4])
 def test_temperatures(t):
     """What is left lies far below the list, or all weights are alike."""
