@@ -110,9 +110,11 @@ template <typename T, int W, int S> __global__ __launch_bounds__(64 * W) void to
     auto take = [&](const auto& from) {
         // Exponents relative to a border that the bound's own product, rounded, is not below.  Where a product could be infinite, the row is searched; where the
         // sum is (what is listed may lie far above the border, if that is large), it is made again below.
+        // The border is never within 2^-41 of 0.  So what is below it is by 2^-89 at least (a product of two floats at 2^-42 is a multiple of that, the
+        // border of 2^-65), and counts whole: 2^100 times as much is above 1.  What lies around 0 is listed then; a row that has nothing else is searched.
         bound = gather_bound(bound);
         const float scaled = bound * a.scale;
-        border = scaled - fabsf(scaled) * 0x1p-22f - 0x1p-126f;
+        border = fabsf(scaled) >= 0x1p-40f ? scaled - fabsf(scaled) * 0x1p-22f : -0x1p-39f;
         fits = fabsf(scaled) < 1e37f;
         sum = 0.f;
         gather(from, list, [&](float (&z)[RowVec<T>::n]) {

@@ -163,6 +163,17 @@ def test_temperatures(t):
         check(z, top, "fp32", t=t)
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("size,t", [(1e-20, 1.0), (1e-31, 1.0), (1e-33, 1.0), (1e-36, 1.0), (1e-39, 1.0), (1e-12, 1e20), (1e-16, 1e20), (1e-25, 1e20), (1.0, 1e20), (1.0, 1e-20),
+                                    (1e-19, 1e-20)])
+@pytest.mark.parametrize("vocab", [300, 2048, 16384, 70001])
+def test_tiny_differences(vocab, size, t, dtype):
+    """Exponents that lie by 2^-60 to 2^-130 from each other, and the ends of the temperature's range: what is not listed counts 1 each, or next to nothing."""
+    z = (size * rows(2, vocab, seed=vocab).double()).float()
+    for top in (1, 16, 128):
+        check(z, top, dtype, t=t)
+
+
 @pytest.mark.parametrize("fill", [-3e4, -1e9, -7e19, -3e37, 2e9])
 def test_others_at_one_large_value(fill):
     """Masks of many sizes, few enough of them to be listed, where a list reaches into them and where it does not."""
