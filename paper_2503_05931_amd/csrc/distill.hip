@@ -293,13 +293,14 @@ template <typename T, int W, int S, bool STREAM> __global__ __launch_bounds__(64
         for (int e = 0; e < N; ++e)
             if (begin + e >= first && begin + e < vocab) d[begin + e] = y[e];
     };
-    if (w == 0.f) {
+    // Nothing outside of the list: of a row that forward has left out, the logits may be anything, and are not looked at.
+    const bool none = w == 0.f || stats[1] == 0.f;
+    if (none)
         for (int v = tid; v < vecs; v += kThreads) put(v, (V)(from_f32<T>(0.f)));
-        return;
-    }
+    if (w == 0.f) return;
     const float scale = (float)a.scale_d, slope = w * a.temperature * (a.d_loss ? a.d_loss[0] : 1.f);
     const float s0 = stats[0], s1 = slope * stats[1];
-    for (int v0 = tid; v0 < vecs; v0 += kThreads * S) {
+    for (int v0 = none ? vecs : tid; v0 < vecs; v0 += kThreads * S) {
         V x[S];
 #pragma unroll
         for (int i = 0; i < S; ++i) {

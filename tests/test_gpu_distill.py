@@ -127,6 +127,26 @@ def test_unscored_rows_hold_anything(dtype):
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("rest", [True, False])
+@pytest.mark.parametrize("vocab", [90, 4097, 20001])
+def test_rows_with_neither_an_entry_nor_a_rest(vocab, rest, dtype):
+    """Their loss and gradient are 0, whatever their logits hold."""
+    from paper_2503_05931_amd import vocabulary as L
+    c = make(7, vocab, 5, dtype, t=0.25, rest=rest, seed=vocab, unscored=0)
+    c["ids"][:3] = -1
+    c["values"][3:6] = -math.inf
+    if rest:
+        c["rest"][:6] = -math.inf
+    for i, fill in enumerate((200.0, math.nan, math.inf, torch.finfo(TYPE[dtype]).max, -math.inf)):
+        c["z"][i] = fill
+    for weights in (c["weights"], None):
+        _, (z, _, ids, _, w), (loss, row_loss, stats, grad) = check(c | dict(weights=weights), dtype, t=0.25)
+        assert not grad[:6].any() and not row_loss[:6].any() and grad[6].any() and torch.isfinite(loss)
+        place = L.Distillation(vocab, 5, TYPE[dtype], temperature=0.25).aed_distill_backward(z, ids, stats, weights=w, d_logits=z)
+        assert place is z and torch.equal(place, grad)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("rest", [True, False])
 def test_students_without_mass(rest, dtype):
     """Ids that the student excludes, listed and not; a student without any logit; only the list, only others."""
     c = make(6, 250, 9, dtype, rest=rest, seed=4, unscored=0)
