@@ -101,9 +101,10 @@ aed_status aed_top_logits(aed_top *plan, const void *logits, int64_t row_stride,
  *                    = weight_r T p_i (1 - q_R / p_R)                       for others (without rest: q_R = 0)
  * An id may stand in a list more than once.  A row of weight 0 has L_r 0 and
  * gradient 0, whatever its logits and list hold, and so has one with neither
- * an entry nor (finite) rest.  Student's logits of minus infinity have p = 0 (L_r is
- * infinite where q is not 0 there); NaN and plus infinity give NaN.  p's
- * sums are float32: L_r is good to some 2^-22 T^2. */
+ * an entry nor a finite rest.  Student's logits of minus infinity have p = 0 (L_r is
+ * infinite where q is not 0 there); NaN and plus infinity, the student's, an
+ * entry's or, beside an entry, the rest's, give NaN.  p's sums are float32:
+ * L_r is good to some 2^-22 T^2. */
 typedef struct aed_distill aed_distill; /* opaque */
 
 typedef struct aed_distill_config {

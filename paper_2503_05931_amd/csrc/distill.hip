@@ -160,7 +160,10 @@ template <typename T, int W, int S, int E, bool OTHERS> __global__ __launch_boun
     value_top = wave_max(value_top);
     at_top = wave_max(at_top);
     const double lead = fmax((double)value_top * c, rest);
-    if (lead == -(double)kInf) {  // neither an entry nor a rest
+    bool entry = false;
+#pragma unroll
+    for (int i = 0; i < E; ++i) entry = entry || valid[i];
+    if (!__any(entry) && !(fabs(rest) < (double)kInf)) {  // neither an entry nor a finite rest; an entry that is NaN is one
 #pragma unroll
         for (int i = 0; i < E; ++i)
             if (64 * i + lane < K) stats[2 + 64 * i + lane] = kLeftOut;

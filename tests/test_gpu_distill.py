@@ -147,6 +147,37 @@ def test_rows_with_neither_an_entry_nor_a_rest(vocab, rest, dtype):
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("rest", [True, False])
+@pytest.mark.parametrize("vocab,top", [(300, 6), (300, 70), (20001, 6)])
+def test_teachers_that_are_not_numbers(vocab, top, rest, dtype):
+    """Entries that are NaN or infinite make their row's loss NaN, and its gradient by their ids, also where the list has no others; a rest that is neither
+    counts as none where there is no entry.  Other rows are as they would be without them."""
+    from paper_2503_05931_amd import vocabulary as L
+    c = make(9, vocab, top, dtype, rest=rest, seed=vocab + top, unscored=0)
+    c["values"][0] = math.nan
+    c["values"][1, 3] = math.nan
+    c["values"][2] = math.nan
+    c["values"][3], c["ids"][3, 1:] = math.nan, -1
+    c["values"][4] = math.inf
+    c["ids"][5:8] = -1
+    bad, empty = [0, 1, 2, 3, 4], [5, 6, 7]
+    if rest:
+        c["rest"][2] = c["rest"][3] = -math.inf
+        c["rest"][5:8] = torch.tensor([math.inf, math.nan, -math.inf])
+    z, ids = c["z"].cuda(), c["ids"].cuda()
+    on = dict(values=c["values"].cuda(), ids=ids, rest=c["rest"].cuda() if rest else None)
+    plan = L.Distillation(vocab, top, TYPE[dtype])
+    loss, rows, stats = plan.aed_distill_forward(z, **on)
+    grad = plan.aed_distill_backward(z, ids, stats)
+    assert loss.isnan() and rows[bad].isnan().all() and not rows[empty].any() and not grad[empty].any()
+    for r in bad:
+        assert grad[r][ids[r][ids[r] >= 0].long()].isnan().all(), r
+    check({n: None if v is None else v[8:] for n, v in c.items()}, dtype)
+    alone = plan.aed_distill_forward(z[8:], **{n: None if v is None else v[8:] for n, v in on.items()})[1]
+    assert torch.equal(rows[8:], alone)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("rest", [True, False])
 def test_students_without_mass(rest, dtype):
     """Ids that the student excludes, listed and not; a student without any logit; only the list, only others."""
     c = make(6, 250, 9, dtype, rest=rest, seed=4, unscored=0)
