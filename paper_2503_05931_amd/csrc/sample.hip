@@ -37,7 +37,8 @@ template <int W, int RUNS> struct SampleLds {
     Search<W, kBits> search;
     uint64_t w[kList];    // by id
     uint64_t key[kList];  // by place
-    int by_place[kList], by_id[kList];
+    int by_place[kList];
+    uint64_t by_id[kList];  // keys
     uint64_t run[RUNS];
     float2 estimate[W];
 };
@@ -83,13 +84,11 @@ struct Weigh {
     }
 };
 
-// log(part / all) of whole numbers, 0 < part <= all
-__device__ __forceinline__ float log_ratio(const Pow2& pow2, uint64_t part, uint64_t all) {
-    const double d = (double)all, n = (double)part;
-    double r = __builtin_amdgcn_rcp(d);  // to some 2^-20; each step doubles the digits
-    r = fma(fma(-d, r, 1.0), r, r);
-    r = fma(fma(-d, r, 1.0), r, r);
-    return part == all ? 0.f : (float)(log2_of(pow2, n * r) * (1 / kLog2eD));
+// log(weight of z / all), of which `part` whole multiples are counted, 0 < part <= all; bits: what they are multiples of.  From the logit itself: of a weight of
+// 2^-40 its multiples of 2^-50 have three digits.
+__device__ __forceinline__ float log_ratio(const Weigh& weigh, float z, uint64_t part, uint64_t all, int bits) {
+    const double of_z = z == weigh.top_f ? 0.0 : ((double)z - weigh.top) * weigh.c;
+    return part == all ? 0.f : (float)((of_z - log2_of(weigh.pow2, ldexp((double)all, -bits))) * (1 / kLog2eD));
 }
 
 // floor(f n) or (UP) its ceiling, exactly; f in [0, 1]
@@ -237,6 +236,7 @@ template <typename T, int W, int S, int RUNS> __global__ __launch_bounds__(64 * 
     const RowLoop<T, W> loop{row.p, row.n};
     uint64_t held[kHeld ? S : 1][N];
     int token = -1;  // of the lane that finds it
+    float its_z = 0.f;
     uint64_t its = 0, left = 0;
 
     Place last{-kInf, INT_MAX};  // of A, then of B
@@ -334,7 +334,7 @@ template <typename T, int W, int S, int RUNS> __global__ __launch_bounds__(64 * 
                     if (tid % kShare == 0) {
                         lds.key[place] = key;
                         lds.by_place[place] = by_id;
-                        lds.by_id[by_id] = key_id(key);
+                        lds.by_id[by_id] = key;
                     }
                 }
             }
@@ -372,14 +372,16 @@ template <typename T, int W, int S, int RUNS> __global__ __launch_bounds__(64 * 
                 if (64 * i >= n) continue;
                 const uint64_t v = 64 * i + lane < n ? lds.w[64 * i + lane] : 0, through = at + wave_prefix(v);
                 if (through - v <= target && target < through) {
-                    token = lds.by_id[64 * i + lane];
+                    const uint64_t key = lds.by_id[64 * i + lane];
+                    token = key_id(key);
+                    its_z = key_logit(key);
                     its = v;
                 }
                 at = lane_of(through, 63);
             }
             if (token >= 0) {  // one lane
                 a.tokens[r] = token;
-                a.logp[r] = log_ratio(weigh.pow2, its, left);
+                a.logp[r] = log_ratio(weigh, its_z, its, left, a.weight_bits);
             }
             return;
         }
@@ -489,13 +491,14 @@ template <typename T, int W, int S, int RUNS> __global__ __launch_bounds__(64 * 
     for (int e = 0; e < N; ++e) {
         if (at <= target && target < at + w[e]) {
             token = id + e;
+            its_z = z[e];
             its = w[e];
         }
         at += w[e];
     }
     if (token >= 0) {  // one lane
         a.tokens[r] = token;
-        a.logp[r] = log_ratio(weigh.pow2, its, left);
+        a.logp[r] = log_ratio(weigh, its_z, its, left, a.weight_bits);
     }
 }
 

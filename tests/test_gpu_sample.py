@@ -140,6 +140,28 @@ def test_uniforms():
     check(z.repeat(6, 1), torch.tensor([0.0, 1 - 2 ** -24, 1.0, 7.0, -1.0, math.nan]), "fp32")
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("vocab,far", [(300, (5, 15, 25, 33)), (4096, (5, 15, 25, 33)), (9001, (25, 30)), (65541, (15, 28)), (262144, (15, 28))])
+def test_unlikely_tokens(vocab, far, dtype):
+    """A number of 0 draws the first id, whose weight may be a few multiples of what weights are rounded to: its logp comes from its logit.  Of what is left the
+    sum is rounded by 2^-45 a logit at most, 1e-11 of it here and less, as roundings have either sign.  An id that weighs less than half of a multiple is not
+    drawn: at t = 0.9, 33 from the largest, 2^-52.9 of multiples of 2^-50, and from 28 on 2^-44.9 of such of 2^-44 and 2^-45.  Then the next one is."""
+    bits = 50 if vocab <= 4096 else 62 - (vocab - 1).bit_length()
+    for d in far:
+        z, _ = rows(3, vocab, seed=vocab + d)
+        z[:, 0] = z[:, 1:].max(1).values + 1 - d - torch.tensor([0.0, 0.3, 0.7])
+        z[:, 1:] += 1
+        for how in (dict(), dict(t=0.9, min_p=1e-30), dict(top_k=vocab - 1), dict(top_p=1 - 2 ** -24)):
+            below = z.to(TYPE[dtype]).double()
+            below = (below[:, 0] - below.max(1).values) / how.get("t", 1.0) / math.log(2) < -bits - 1
+            tokens, logp = check(torch.where(below[:, None] & (torch.arange(vocab) == 0), -math.inf, z), torch.zeros(3), dtype, **how)
+            again = draw(z.to(TYPE[dtype]), torch.zeros(3), dtype, **how)
+            assert torch.equal(tokens, again[0]) and torch.equal(logp, again[1])
+        z[:, 20:] = -math.inf
+        for how in (dict(top_k=20), dict(top_k=40, top_p=1 - 2 ** -24), dict(top_p=1 - 2 ** -24)):
+            check(z, torch.zeros(3), dtype, **how)
+
+
 def test_extreme_temperatures_and_logits():
     z, u = rows(6, 1000, seed=11)
     for t in (1e-38, 1e-3, 100.0, 3e38):
