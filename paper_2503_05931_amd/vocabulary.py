@@ -115,7 +115,7 @@ class Sampler(_RowsPlan):
     def aed_sample(self, logits, uniforms, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
         """logits: [rows, vocab]; uniforms: float32 [rows], random numbers in [0, 1).  temperature (0: the largest logit), top_k (0: all), top_p (1:
         all) and min_p (0: all): numbers, or tensors [rows] (top_k: int32, the others float32).
-        Returns (tokens int32 [rows], logp float32 [rows]: log-probability among the tokens that were left)."""
+        Returns (tokens int32 [rows], logp float32 [rows]: log-probability among the tokens that were left).  Neither has a gradient by the logits."""
         f32, rows = self.torch.float32, _rows(logits)
         pz, stride = self._logits(logits, "logits", rows)
         pu = self._flat(uniforms, "uniforms", f32, (rows,))
@@ -142,7 +142,7 @@ class TopLogits(_RowsPlan):
 
     def aed_top_logits(self, logits):
         """Returns (values float32 [rows, top], falling; ids int32 [rows, top]; rest float32 [rows]: log of the sum of exp(logit /
-        temperature) over the ids that are not listed)."""
+        temperature) over the ids that are not listed).  None has a gradient by the logits."""
         rows = _rows(logits)
         pz, stride = self._logits(logits, "logits", rows)
         new = self._f32.new_empty
@@ -200,8 +200,9 @@ class Distillation(_RowsPlan):
         return d_logits
 
     def loss(self, logits, values, ids, rest=None, weights=None):
-        """The loss, for torch's autograd: its gradient by the logits (once: second derivatives are refused)."""
-        return _autograd().apply(self, logits, values, ids, rest, weights)
+        """The loss, for torch's autograd: its gradient by the logits (once: second derivatives are refused).  The teacher's list and the weights are constants:
+        those that require a gradient are refused."""
+        return _autograd().of(self, logits, values, ids, rest, weights)
 
 
 _function = None
@@ -214,6 +215,13 @@ def _autograd():
         import torch
 
         class Loss(torch.autograd.Function):
+            @classmethod
+            def of(cls, plan, logits, values, ids, rest, weights):
+                for name, t in (("values", values), ("rest", rest), ("weights", weights)):
+                    if t is not None and t.requires_grad and torch.is_grad_enabled():
+                        _t._refuse(f"{name} requires a gradient, and the loss has none by it")
+                return cls.apply(plan, logits, values, ids, rest, weights)
+
             @staticmethod
             def forward(ctx, plan, logits, values, ids, rest, weights):
                 loss, _, stats = plan.aed_distill_forward(logits, values, ids, rest, weights)

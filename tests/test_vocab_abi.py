@@ -180,6 +180,23 @@ def test_second_derivatives_are_refused():
         (loss + g.square().sum()).backward()
 
 
+def test_constants_that_require_a_gradient_are_refused():
+    """A gradient that is not computed is not silently left out; without autograd, or of a copy that is cut off, nothing is asked for."""
+    import torch
+    z, ids = torch.randn(3, 7, requires_grad=True), torch.tensor([[0, 2], [1, 3], [6, 5]], dtype=torch.int32)
+    given = dict(values=torch.ones(3, 2), rest=torch.zeros(3), weights=torch.ones(3))
+    plan = HostDistillation()
+    for name in given:
+        with_one = given | {name: given[name].clone().requires_grad_(True)}
+        with pytest.raises(binding.AedError, match=f"{name} requires a gradient") as e:
+            plan.loss(z, ids=ids, **with_one)
+        assert e.value.status == E
+        with torch.no_grad():
+            assert torch.isfinite(plan.loss(z, ids=ids, **with_one))
+        plan.loss(z, ids=ids, **(given | {name: with_one[name].detach()})).backward()
+    assert z.grad.abs().sum() > 0
+
+
 class Recorder:
     def __init__(self, status, device, stream):
         import types
