@@ -129,3 +129,13 @@ def test_example(dtype):
     for name, p in model.named_parameters():
         assert p.grad is not None and torch.isfinite(p.grad).all(), name
     assert sum(float(p.grad.float().abs().sum()) > 0 for p in model.parameters()) >= 0.9 * len(list(model.parameters()))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_every_parameter_of_the_example_has_a_gradient(dtype):
+    """None is all zeros, without an exception."""
+    spec = importlib.util.spec_from_file_location("distillation", os.path.join(ROOT, "examples", "distillation.py"))
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    model, _, _ = example.main(steps=1, dtype=dtype, say=lambda s: None)
+    assert not [name for name, p in model.named_parameters() if p.grad is None or not p.grad.any()]
