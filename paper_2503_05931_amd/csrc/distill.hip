@@ -240,7 +240,7 @@ template <typename T, int W, int S, int E, bool OTHERS> __global__ __launch_boun
         if (64 * i + lane < K) stats[2 + 64 * i + lane] = valid[i] ? (float)(p[i] * total_inverse - same[i] * n_inverse) : kLeftOut;
     if (lane == 0) {
         stats[0] = some ? mine.top : 0.f;
-        stats[1] = some ? (float)outside : 0.f;
+        stats[1] = (float)(some ? outside : mine.sum);  // 0, or NaN if the row has one
         a.row_loss[r] = (float)(a.factor * row);
     }
 }

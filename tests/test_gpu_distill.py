@@ -178,6 +178,30 @@ def test_teachers_that_are_not_numbers(vocab, top, rest, dtype):
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("rest", [True, False])
+@pytest.mark.parametrize("vocab", [90, 4097, 20001])
+def test_students_that_are_not_numbers(vocab, rest, dtype):
+    """NaN and plus infinity give NaN: the row's loss, and its gradient by the list and by all others that are not minus infinity; also where the row, or what
+    is outside of the list, has no number at all."""
+    from paper_2503_05931_amd import vocabulary as L
+    c = make(7, vocab, 5, dtype, rest=rest, seed=vocab, unscored=0)
+    z, ids = c["z"], c["ids"].long()
+    keep = torch.gather(z, 1, ids)
+    z[0] = math.nan
+    z[1], z[1, ::2] = -math.inf, math.nan
+    z[2], z[3] = math.nan, math.inf
+    z[4, vocab // 2] = math.nan
+    z[5, 0] = math.inf
+    z[2].scatter_(0, ids[2], keep[2])
+    z = z.cuda()
+    plan = L.Distillation(vocab, 5, TYPE[dtype])
+    loss, rows, stats = plan.aed_distill_forward(z, c["values"].cuda(), c["ids"].cuda(), rest=c["rest"].cuda() if rest else None)
+    grad = plan.aed_distill_backward(z, c["ids"].cuda(), stats)
+    assert loss.isnan() and rows[:6].isnan().all() and torch.isfinite(rows[6])
+    assert (grad[:6].isnan() | (z[:6] == -math.inf)).all() and torch.isfinite(grad[6]).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("rest", [True, False])
 def test_students_without_mass(rest, dtype):
     """Ids that the student excludes, listed and not; a student without any logit; only the list, only others."""
     c = make(6, 250, 9, dtype, rest=rest, seed=4, unscored=0)
