@@ -153,9 +153,16 @@ __device__ __forceinline__ float fold_norm(int rms, float K, float eps, float m2
     return 1.0f / sqrtf(m2 / K + eps);
 }
 
-// sum over the 64 lanes of a wavefront; every lane gets the total
+// sum, largest over the 64 lanes of a wavefront; every lane gets it
 __device__ __forceinline__ float wave_sum(float v) {
     return rows4_sum(row16_sum(v));
+}
+__device__ __forceinline__ float wave_max(float v) {
+    v = fmaxf(v, dpp_mov<0xB1>(v));
+    v = fmaxf(v, dpp_mov<0x4E>(v));
+    v = fmaxf(v, dpp_mov<0x141>(v));
+    v = fmaxf(v, dpp_mov<0x140>(v));
+    return rows4_max(v);
 }
 
 }  // namespace aed

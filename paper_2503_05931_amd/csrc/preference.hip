@@ -24,13 +24,6 @@ template <typename T> struct Vec;
 template <> struct Vec<bf16_t> { typedef bf16x8 type; static constexpr int n = 8; };
 template <> struct Vec<float> { typedef f32x4 type; static constexpr int n = 4; };
 
-__device__ __forceinline__ float wave_max(float v) {
-    v = fmaxf(v, dpp_mov<0xB1>(v));
-    v = fmaxf(v, dpp_mov<0x4E>(v));
-    v = fmaxf(v, dpp_mov<0x141>(v));
-    v = fmaxf(v, dpp_mov<0x140>(v));
-    return rows4_max(v);
-}
 // A row of any alignment: `head` elements up to a 16-byte boundary, `vecs` whole vectors, then the rest
 template <typename T> struct RowParts {
     int head, vecs, tail;  // tail: first element behind the vectors

@@ -118,13 +118,6 @@ template <typename T, int W> struct RowLoop {
     template <typename F> __device__ __forceinline__ void each(F f) const { Row<T, W, 0>(p, n).each(f); }
 };
 
-__device__ __forceinline__ float wave_max(float v) {
-    v = fmaxf(v, dpp_mov<0xB1>(v));
-    v = fmaxf(v, dpp_mov<0x4E>(v));
-    v = fmaxf(v, dpp_mov<0x141>(v));
-    v = fmaxf(v, dpp_mov<0x140>(v));
-    return rows4_max(v);
-}
 __device__ __forceinline__ float wave_min(float v) { return -wave_max(-v); }
 
 // 64-bit sums over a wavefront, whole numbers: in any order the same
