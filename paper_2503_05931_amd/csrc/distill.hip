@@ -7,8 +7,8 @@
 // thousands) is made in forward in 64 bits where it is a small difference of large numbers, its gradients too; backward writes p's multiple
 // everywhere and then the list's own.  p_R is the sum over what is not in the list, found by a bit for each id in LDS, and never a difference to 1: of
 // a student that is sure of the list it is 1e-10 and less.  What lies outside is taken relative to its own largest logit, so that p_i / p_R keeps its digits too.
-// 8448 rows of 4096 in bfloat16, lists of 32 and others: forward 21 us (3.3 TB/s; exponentials and the list's 64 bits, between them, cost as much as the reading),
-// sum of the rows 4, backward 24 (5.8 TB/s: much of the logits is still in the memory-side cache).  2048 rows of 33000 in float32: 48 us (5.6 TB/s) and 89 (6.1).
+// 8448 rows of 4096 in bfloat16, lists of 32 and others: forward 22 us (3.2 TB/s; exponentials and the list's 64 bits, between them, cost as much as the reading),
+// sum of the rows 4, backward 25 (5.6 TB/s: much of the logits is still in the memory-side cache).  2048 rows of 33000 in float32: 48 us (5.6 TB/s) and 90 (6.0).
 #include <algorithm>
 
 #include "vocab_rows.h"

@@ -2,8 +2,8 @@
 //
 // Bound by memory: a row is read once, into registers.  Its lanes' maxima give a bound that a few more elements than are asked for are not below; those are
 // gathered in LDS and placed by comparing each with each.  Everything below the bound adds to the rest's sum in the same pass, relative to the
-// bound, so nothing is subtracted from a whole row's sum, however little is left of it.  32 of 4096 in bfloat16, 8448 rows: 18.7 us, 3.8 TB/s with a launch's 4 us;
-// 64 of 32768, 2048 rows: 33 us, 4.1 TB/s.  With 128 asked for comparisons count: 45 us for the former.
+// bound, so nothing is subtracted from a whole row's sum, however little is left of it.  32 of 4096 in bfloat16, 8448 rows: 18.9 us, 3.8 TB/s with a launch's 4 us;
+// 64 of 32768, 2048 rows: 33 us, 4.1 TB/s.  With 128 asked for comparisons count: 44 us for the former.
 #include "vocab_rows.h"
 
 namespace aed {
